@@ -292,6 +292,115 @@ int vs_sparse_prefill_tiles(const void* ws, size_t ws_bytes, void* stream, int64
  */
 int vs_sparse_prefill_counters(const void* ws, size_t ws_bytes, void* stream, int64_t* counters_host);
 
+/*
+ * ---- Around the prefill: from a layer's projection to the calls above, and single tokens after the prompt ----
+ *
+ * One convention holds for the four calls below: `lens` [batch] int32 (device) is the number of tokens that each sequence
+ * holds, the new ones among them, and a call's `rows` (or n_q) rows of a sequence are its LAST tokens: row r is position
+ * lens[b] - rows + r.  One array serves a whole decoding step; a slot with lens 0 is idle; a batch of prompts of different
+ * lengths is padded in front (rows of negative position have no token).  `lens` and page tables may begin at any element of an
+ * array (4-byte alignment).
+ */
+
+/* Rows of 128 bf16 elements: head h of token t at data + t * token_stride + h * head_stride (strides in elements, multiples of 8,
+ * at least 128; data 16-byte aligned).  A part of a packed projection [tokens, heads, 128] as well as [heads, tokens, 128]. */
+typedef struct {
+    const void* data;
+    int64_t token_stride, head_stride;
+} vs_rows_t;
+
+/* Rotation of the first rot_dim elements of a head (a multiple of 8, 8..128); the others keep their values.  Host struct. */
+typedef struct {
+    const double* freq; /* [rot_dim / 2] device: angle in radians per position of every plane (vs_rope_frequencies or any other) */
+    int rot_dim;
+    int pairing;        /* 0: plane p couples elements (2p, 2p+1);  1: (p, p + rot_dim / 2) */
+    float magnitude;    /* factor of the rotated elements, 1 for a pure rotation */
+} vs_rotation_t;
+
+/*
+ * The frequencies theta_base^(-2p / rot_dim), p < rot_dim / 2, scaled for contexts longer than the model was trained on, into HOST
+ * memory (the caller copies them to the device once).
+ *   scaling  0: as they are (the other arguments are ignored)
+ *            1: divided by factor (positions shrunk)
+ *            2: by wavelength.  A plane turns `original` * f / (2 pi) times over the original context: with `low` turns or fewer it
+ *               is divided by factor, with `high` or more it is kept, in between the two are mixed linearly in the turns.
+ */
+int vs_rope_frequencies(double theta_base, int rot_dim, int scaling, double factor, double low, double high, double original,
+                        double* freq_host);
+
+/*
+ * Norm of queries and keys per head and rotary embedding in one pass, with the change of layout from a projection's output:
+ *     y = x * w / sqrt(mean(x^2) + eps)  over the 128 elements of a head (w_q / w_k [128] fp32, or NULL: y = x),
+ *     planes (a, b) of y -> magnitude * (a cos t - b sin t, a sin t + b cos t),  t = position * freq[plane].
+ *   q, k, v     batch * rows tokens (sequence after sequence) of q_heads / kv_heads heads; v may be NULL (then v_out, too); v is copied
+ *   lens, pos0  row r of sequence b is position lens[b] - rows + r, or pos0 + r where lens is NULL (rows of negative position are
+ *               computed like the others)
+ *   q_out [batch, q_heads, rows, 128], k_out, v_out [batch, kv_heads, rows, 128] bf16.  An output may be its own input where both
+ *               have the same layout; otherwise they must not overlap.
+ *   eps         > 0 (ignored without w_q and w_k)
+ * Arithmetic: angles reduced in fp64, sine, cosine, norm and rotation in fp32, one rounding to bf16.
+ */
+int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_rows_t* v, int batch, int64_t rows, int q_heads, int kv_heads,
+                    const float* w_q, const float* w_k, float eps, const vs_rotation_t* rotation, const int32_t* lens, int64_t pos0,
+                    void* q_out, void* k_out, void* v_out, void* stream);
+
+/*
+ * Paged cache of keys and values in 4 bits.  An element is held as an E2M1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign), 32 channels of
+ * a token share a scale 2^(E - 127), E one byte: 136 bytes per token and head for K and V together, against 512 in bf16.  The
+ * scale is the smallest power of two s with max |x| <= 7 s (2 <= E <= 252; a group of zeros has E = 0), the code the number nearest to
+ * x / s, ties to the even one, 6 beyond 6.  A group with a NaN or an infinity in it is held as NaN (E = 255).
+ * Memory is divided in pages of page_size tokens (a multiple of 64), each [kv_heads, page_size / 64] blocks of VS_CACHE_BLOCK_BYTES.
+ * A page that is taken into use need not be cleared.  Host struct.
+ */
+#define VS_CACHE_BLOCK 64
+#define VS_CACHE_BLOCK_BYTES 8704
+typedef struct {
+    void* data;           /* [pages, kv_heads, page_size / 64, VS_CACHE_BLOCK_BYTES] device */
+    int64_t pages;
+    int kv_heads;
+    int page_size;
+    const int32_t* table; /* [batch, max_pages] device: page number of tokens i * page_size .. of sequence b; NULL: b * max_pages + i */
+    int max_pages;
+} vs_cache_t;
+
+size_t vs_cache_bytes(int64_t pages, int kv_heads, int page_size);
+
+/*
+ * Shared by the three calls on a cache:
+ *   lens   [batch] int32 (device), values outside [0, max_n] count as the nearer end; NULL: every sequence holds max_n tokens
+ *   max_n  bound of lens that the host knows, at most max_pages * page_size
+ * Entries of the table that name no page (outside [0, pages)) are legal: their tokens are not written, not read and not attended to.
+ * Sequences may share pages that are only read; no page may be written for two sequences in one call.
+ *
+ * Writes the last `rows` tokens of each sequence; rows of negative position are skipped and all other tokens keep what they hold.
+ *   k, v  [batch, kv_heads, rows, 128] bf16 (k carries RoPE)
+ */
+int vs_cache_write(const vs_cache_t* cache, const void* k, const void* v, int batch, int64_t rows, const int32_t* lens, int64_t max_n,
+                   void* stream);
+
+/*
+ * Reads the last `rows` tokens of each sequence back (exactly what the cache holds); rows of negative position and of missing pages are left
+ * as they were.  With lens = NULL, max_n = the end and rows = its distance from the beginning it reads any range, for instance all keys
+ * in front of a chunk for vs_sparse_prefill_chunk.
+ *   k, v  [batch, kv_heads, rows, 128] bf16 out; one of the two may be NULL
+ */
+int vs_cache_read(const vs_cache_t* cache, int batch, int64_t rows, const int32_t* lens, int64_t max_n, void* k, void* v, void* stream);
+
+/*
+ * Attention of the last n_q tokens (1 .. VS_CACHE_MAX_NEW) of each sequence over the cache, which already holds them:
+ *     o[b, h, r] = sum_j softmax_j(scale * q[b, h, r] . K_j) V_j  over  j <= lens[b] - n_q + r.
+ *   q, o  [batch, q_heads, n_q, 128] bf16 (not overlapping);  lse [batch, q_heads, n_q] fp32 out or NULL
+ * A row without a key (negative position, idle slot, missing pages only) gives zeros and lse = -inf.  Longer chunks: vs_cache_read, then
+ * vs_sparse_prefill_chunk or vs_dense_prefill_chunk.
+ * Arithmetic: K and V are exact in bf16; bf16 MFMA, fp32 accumulation and softmax, P rounded to bf16.  The same call always gives
+ * the same bits.  Workspace: vs_cache_attend_workspace; the answer for max_n is enough for every smaller max_n of the same call.
+ */
+#define VS_CACHE_MAX_NEW 128
+size_t vs_cache_attend_workspace(int batch, int q_heads, int kv_heads, int n_q, int64_t max_n);
+
+int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch, int q_heads, int n_q, const int32_t* lens, int64_t max_n,
+                    float scale, void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 const char* vs_strerror(int status);
 int vs_last_hip_error(void);
 const char* vs_version(void);

@@ -16,6 +16,8 @@ EXPORTS = [
     "vs_sparse_prefill_static", "vs_dense_prefill", "vs_dense_prefill_chunk", "vs_validate_lists",
     "vs_sparse_prefill_tiles", "vs_sparse_prefill_counters", "vs_aggregate_workspace", "vs_aggregate",
     "vs_index_train_workspace", "vs_index_train_step",
+    "vs_rope_frequencies", "vs_qk_norm_rope", "vs_cache_bytes", "vs_cache_write", "vs_cache_read", "vs_cache_attend_workspace",
+    "vs_cache_attend",
     "vs_strerror", "vs_last_hip_error", "vs_version",
 ]
 
@@ -38,6 +40,24 @@ class _Budget(ctypes.Structure):
     _fields_ = [("mode", ctypes.c_int), ("tau_v", ctypes.c_double), ("tau_s", ctypes.c_double),
                 ("k_v", ctypes.c_int), ("k_s", ctypes.c_int), ("n_sink", ctypes.c_int), ("n_local", ctypes.c_int),
                 ("cap_v", ctypes.c_int), ("cap_s", ctypes.c_int)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int), ("pairing", ctypes.c_int), ("magnitude", ctypes.c_float)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("kv_heads", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("table", ctypes.c_void_p), ("max_pages", ctypes.c_int)]
+
+
+CACHE_BLOCK = 64                # tokens of a cache block
+CACHE_BLOCK_BYTES = 8704
+CACHE_MAX_NEW = 128             # new tokens of a cache_attend call
 
 
 def library_path():
@@ -79,6 +99,15 @@ def _load():
     L.vs_index_train_workspace.argtypes = [i32, i64, i32]
     L.vs_index_train_workspace.restype = sz
     L.vs_index_train_step.argtypes = [vp, vp, i32, i64, ctypes.POINTER(_Indexer), vp, vp, f32, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.vs_rope_frequencies.argtypes = [f64, i32, i32, f64, f64, f64, f64, vp]
+    L.vs_qk_norm_rope.argtypes = [vp, vp, vp, i32, i64, i32, i32, vp, vp, f32, vp, vp, i64, vp, vp, vp, vp]
+    L.vs_cache_bytes.argtypes = [i64, i32, i32]
+    L.vs_cache_bytes.restype = sz
+    L.vs_cache_write.argtypes = [vp, vp, vp, i32, i64, vp, i64, vp]
+    L.vs_cache_read.argtypes = [vp, i32, i64, vp, i64, vp, vp, vp]
+    L.vs_cache_attend_workspace.argtypes = [i32, i32, i32, i32, i64]
+    L.vs_cache_attend_workspace.restype = sz
+    L.vs_cache_attend.argtypes = [vp, vp, i32, i32, i32, vp, i64, f32, vp, vp, vp, sz, vp]
     L.vs_strerror.argtypes = [i32]
     L.vs_strerror.restype = ctypes.c_char_p
     L.vs_last_hip_error.restype = i32
@@ -120,6 +149,15 @@ def _dev(t, dtype, what):
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype == dtype):
         raise TypeError("%s must be a contiguous CUDA tensor of dtype %s" % (what, dtype))
     return t
+
+
+def _here(*tensors):
+    """All on the current device: the launch goes there, whatever device a tensor is on."""
+    import torch
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != at:
+            raise ValueError("tensor on %s, current device cuda:%d" % (t.device, at))
 
 
 class IndexerWeights:
@@ -374,4 +412,147 @@ def dense_prefill(q, k, v, o, lse=None, scale=None, stream=None, pos0=None):
     else:
         _check(_load().vs_dense_prefill_chunk(_ptr(q), _ptr(k), _ptr(v), q_heads, kv_heads, n_q, n, int(pos0), scale, _ptr(o),
                                               _ptr(lse), _stream(stream)), "vs_dense_prefill_chunk")
+    return o
+
+
+def rope_frequencies(theta_base, rot_dim=128, scaling=0, factor=1.0, low=1.0, high=4.0, original=8192.0):
+    """Angles per position of the rot_dim / 2 planes, a float64 tensor on the host (copy it to the GPU for Rope).
+    scaling 0: plain, 1: divided by factor, 2: by wavelength (see vs_rope_frequencies)."""
+    import torch
+    f = torch.empty(max(0, int(rot_dim)) // 2, dtype=torch.float64)
+    _check(_load().vs_rope_frequencies(theta_base, int(rot_dim), int(scaling), factor, low, high, original, _ptr(f)), "vs_rope_frequencies")
+    return f
+
+
+class Rope:
+    """Rotation of the first 2 * len(freq) elements of every head.  freq: float64 on the GPU (rope_frequencies(...).cuda())."""
+
+    def __init__(self, freq, pairing=0, magnitude=1.0):
+        import torch
+        self.freq = _dev(freq, torch.float64, "freq")
+        assert freq.dim() == 1
+        self.pairing, self.magnitude = int(pairing), float(magnitude)
+        self._c = _Rotation(freq.data_ptr(), 2 * freq.numel(), self.pairing, self.magnitude)
+        self._ref = ctypes.byref(self._c)
+
+    def c_struct(self):
+        return self._c
+
+
+def _rows(x, what):
+    """A [tokens, heads, 128] tensor with any strides of tokens and heads."""
+    import torch
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 3):
+        raise TypeError("%s must be a CUDA tensor [tokens, heads, 128] of dtype torch.bfloat16" % what)
+    tokens, heads, d = x.shape
+    st, sh, sd = x.stride()
+    assert d == 128 and sd == 1, "%s: elements of a head must be contiguous" % what
+    # a stride that no step uses may be anything
+    return _Rows(x.data_ptr(), st if tokens > 1 else 128, sh if heads > 1 else 128)
+
+
+def qk_norm_rope(q, k, q_out, k_out, rope, v=None, v_out=None, w_q=None, w_k=None, eps=1e-6, lens=None, pos0=0, stream=None):
+    """q [tokens, q_heads, 128], k, v [tokens, kv_heads, 128] (views of a projection, any strides of tokens and heads) ->
+    q_out [batch, q_heads, rows, 128], k_out, v_out [batch, kv_heads, rows, 128] (or without the batch dimension for one
+    sequence), tokens = batch * rows.  w_q, w_k [128] fp32 or None: no norm.  lens [batch] int32: row r of sequence b is position
+    lens[b] - rows + r; None: pos0 + r."""
+    import torch
+    _dev(q_out, torch.bfloat16, "q_out"); _dev(k_out, torch.bfloat16, "k_out")
+    batch, q_heads, rows, d = q_out.shape if q_out.dim() == 4 else (1,) + tuple(q_out.shape)
+    kv_heads = k.shape[1]
+    assert d == 128 and q.shape == (batch * rows, q_heads, 128) and k.shape == (batch * rows, kv_heads, 128)
+    assert k_out.numel() == batch * kv_heads * rows * 128 and k_out.shape[-2] == rows and k_out.shape[-3] == kv_heads
+    assert (v is None) == (v_out is None)
+    cq, ck, cv = _rows(q, "q"), _rows(k, "k"), None
+    if v is not None:
+        _dev(v_out, torch.bfloat16, "v_out")
+        assert v.shape == k.shape and v_out.shape == k_out.shape
+        cv = _rows(v, "v")
+    for name, w in (("w_q", w_q), ("w_k", w_k)):
+        if w is not None:
+            assert _dev(w, torch.float32, name).numel() == 128
+    if lens is not None:
+        assert _dev(lens, torch.int32, "lens").numel() == batch
+    _here(q, k, v, q_out, k_out, v_out, w_q, w_k, lens, rope.freq)
+    _check(_load().vs_qk_norm_rope(ctypes.byref(cq), ctypes.byref(ck), None if cv is None else ctypes.byref(cv), batch, rows, q_heads,
+                                   kv_heads, _ptr(w_q), _ptr(w_k), eps, rope._ref, _ptr(lens), int(pos0), _ptr(q_out), _ptr(k_out),
+                                   _ptr(v_out), _stream(stream)), "vs_qk_norm_rope")
+    return q_out, k_out
+
+
+def cache_bytes(pages, kv_heads, page_size):
+    return _load().vs_cache_bytes(pages, kv_heads, page_size)
+
+
+class Cache:
+    """The paged 4-bit cache of a layer: data [pages, kv_heads, page_size / 64, 8704] uint8 and the page table [batch, max_pages]
+    int32, or max_pages alone: sequence b then has the pages b * max_pages .. (b + 1) * max_pages - 1."""
+
+    def __init__(self, data, table=None, max_pages=None):
+        import torch
+        _dev(data, torch.uint8, "data")
+        assert data.dim() == 4 and data.shape[3] == CACHE_BLOCK_BYTES and (table is None) != (max_pages is None)
+        if table is not None:
+            _dev(table, torch.int32, "table")
+            assert table.dim() == 2
+            max_pages = table.shape[1]
+        self.data, self.table, self.max_pages = data, table, int(max_pages)
+        self.pages, self.kv_heads, self.page_size = data.shape[0], data.shape[1], data.shape[2] * CACHE_BLOCK
+        self._c = _Cache(data.data_ptr(), self.pages, self.kv_heads, self.page_size, None if table is None else table.data_ptr(),
+                         self.max_pages)
+        self._ref = ctypes.byref(self._c)
+
+    def c_struct(self):
+        return self._c
+
+    def _batch(self, x, heads, lens, what):
+        import torch
+        _dev(x, torch.bfloat16, what)
+        batch, h, rows, d = x.shape if x.dim() == 4 else (1,) + tuple(x.shape)
+        assert d == 128 and (heads is None or h == heads)
+        assert self.table is None or self.table.shape[0] == batch
+        if lens is not None:
+            assert _dev(lens, torch.int32, "lens").numel() == batch
+        _here(x, lens, self.data, self.table)
+        return batch, h, rows
+
+
+def cache_write(cache, k, v, max_n, lens=None, stream=None):
+    """Quantises k, v [batch, kv_heads, rows, 128] (or without the batch dimension) into the cache as the last tokens of sequences
+    that then hold lens [batch] int32 tokens each (None: max_n)."""
+    batch, _, rows = cache._batch(k, cache.kv_heads, lens, "k")
+    cache._batch(v, cache.kv_heads, None, "v")
+    assert v.shape == k.shape
+    _check(_load().vs_cache_write(cache._ref, _ptr(k), _ptr(v), batch, rows, _ptr(lens), int(max_n), _stream(stream)), "vs_cache_write")
+    return cache
+
+
+def cache_read(cache, k, v, max_n, lens=None, stream=None):
+    """The last tokens of each sequence as the cache holds them, into k, v [batch, kv_heads, rows, 128] bf16 (one may be None)."""
+    x = k if k is not None else v
+    batch, _, rows = cache._batch(x, cache.kv_heads, lens, "k" if k is not None else "v")
+    if k is not None and v is not None:
+        cache._batch(v, cache.kv_heads, None, "v")
+        assert v.shape == k.shape
+    _check(_load().vs_cache_read(cache._ref, batch, rows, _ptr(lens), int(max_n), _ptr(k), _ptr(v), _stream(stream)), "vs_cache_read")
+    return k, v
+
+
+def cache_attend_workspace(batch, q_heads, kv_heads, n_q, max_n):
+    return _load().vs_cache_attend_workspace(batch, q_heads, kv_heads, n_q, max_n)
+
+
+def cache_attend(q, cache, o, max_n, lens=None, lse=None, ws=None, scale=None, stream=None):
+    """Attention of the last n_q tokens of each sequence over the cache (which holds them): q, o [batch, q_heads, n_q, 128] (or without
+    the batch dimension), lse [batch, q_heads, n_q] fp32 or None."""
+    import torch
+    batch, q_heads, n_q = cache._batch(q, None, lens, "q")
+    _dev(o, torch.bfloat16, "o")
+    assert o.shape == q.shape
+    if lse is not None:
+        assert _dev(lse, torch.float32, "lse").numel() == batch * q_heads * n_q
+    _here(o, lse, ws)
+    scale = 128 ** -0.5 if scale is None else scale
+    _check(_load().vs_cache_attend(_ptr(q), cache._ref, batch, q_heads, n_q, _ptr(lens), int(max_n), scale, _ptr(o), _ptr(lse), _ptr(ws),
+                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "vs_cache_attend")
     return o

@@ -10,6 +10,7 @@ namespace vs {
 void set_hip_error(hipError_t e);
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // vs_index_score; keep_split: also leaves W_U, split into two bf16 matrices [d_h, 256] (k contiguous), in the workspace: hi at
