@@ -8,7 +8,9 @@
 // pairing the pieces are rot_dim / 2 apart), the others plain elements, so that a rotation needs no lane's neighbour.  The angle
 // is reduced to a fraction of a turn in fp64 (positions reach 2^20), its sine and cosine are fp32: within 2^-23 of the
 // rotated pair's size, 2^14 times finer than a bf16 step.  They serve all heads of a position that a thread walks over.
-// Bound by the memory: every element is read and written once.
+// A head's row costs a norm and four products a plane: the weights are folded into the angles' sines and cosines.
+// Bound by the memory: every element is read and written once.  131072 positions of 32 / 8 heads 675 us (4.8 TB/s; a large copy reaches 5.1),
+// with one row's loads in flight, weights apart and all parts in one loop 860.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -19,7 +21,8 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSlots = kThreads / 16;          // rows of 128 that a workgroup holds at a time
+constexpr int kPositions = kThreads / 16;      // of a workgroup
+constexpr int kBatch = 4;                      // heads of a position whose loads are in flight together
 
 struct Part {                                  // q, k or v
     const uint16_t* x;
@@ -27,12 +30,12 @@ struct Part {                                  // q, k or v
     const float* w;                            // null: no norm
     int64_t token, head;                       // strides of x in elements
     int heads;
+    int groups;                                // workgroups that share the heads
+    int plain;                                 // copied as it is
 };
 
 struct NormRopeParams {
     Part part[3];
-    int heads;                                 // of all parts together
-    int heads_per_group;                       // heads that a workgroup walks over
     uint32_t tokens, rows;                     // batch * rows, rows per sequence
     const int32_t* lens;
     int64_t pos0;
@@ -52,83 +55,131 @@ __device__ __forceinline__ float row16_sum(float x) {
     return x;
 }
 
-// POSITIONS positions per workgroup, 16 / POSITIONS heads of each at a time
-template <int POSITIONS>
+// one row: norm, then the planes (x, y) -> (x ca - y sb, x sa + y cb) where ca .. sb are cosine and sine times the weights of x and y
+struct Turn {
+    float ca[4], cb[4], sa[4], sb[4];
+};
+
+template <bool PAIRED_HALVES>
+__device__ __forceinline__ void norm_turn(uint2& u0, uint2& u1, const Turn& t, bool norm, float eps, bool turned) {
+    float e[8];
+    const uint32_t word[4] = {u0.x, u0.y, u1.x, u1.y};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        e[2 * i] = __uint_as_float(word[i] << 16);
+        e[2 * i + 1] = __uint_as_float(word[i] & 0xffff0000u);
+    }
+    float inv = 1.0f;
+    if (norm) {
+        float sum = 0.0f, other = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            sum = fmaf(e[i], e[i], sum);
+            other = fmaf(e[i + 1], e[i + 1], other);
+        }
+        sum = row16_sum(sum + other);
+        inv = rsqrtf(fmaf(sum, 1.0f / 128.0f, eps));
+        if (!(sum < INFINITY)) {                  // squares past fp32: again with the row scaled down (eps is nothing beside it)
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                e[i] *= 8.470329472543003e-22f;                              // 2^-70
+                sum = fmaf(e[i], e[i], sum);
+            }
+            inv = rsqrtf(row16_sum(sum) * (1.0f / 128.0f));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float& a = PAIRED_HALVES ? e[i] : e[2 * i];
+        float& b = PAIRED_HALVES ? e[4 + i] : e[2 * i + 1];
+        const float x = a * inv, y = b * inv;
+        a = x * t.ca[i];
+        b = y * t.cb[i];
+        if (turned) {
+            a = fmaf(-y, t.sb[i], a);
+            b = fmaf(x, t.sa[i], b);
+        }
+    }
+    u0 = make_uint2(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]));
+    u1 = make_uint2(pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+}
+
+// Workgroup (x, y): 16 positions, the y-th group of heads of q, k or v.
+template <bool PAIRED_HALVES>
 __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormRopeParams p) {
-    constexpr int kHeads = kSlots / POSITIONS;
-    const int l = threadIdx.x & 15, slot = threadIdx.x >> 4;
-    const uint32_t t = blockIdx.x * POSITIONS + slot % POSITIONS;
+    const int l = threadIdx.x & 15;
+    const uint32_t t = blockIdx.x * kPositions + (threadIdx.x >> 4);
     if (t >= p.tokens) return;
+    int group = blockIdx.y, which = 0;
+    while (group >= p.part[which].groups) group -= p.part[which++].groups;
+    const Part part = p.part[which];
     const uint32_t b = t / p.rows, r = t - b * p.rows;
     const bool turned = 8 * l < p.rot_dim;
     // the two pieces of four elements
-    const int at0 = turned && p.pairing ? 4 * l : 8 * l;
-    const int at1 = turned && p.pairing ? p.rot_dim / 2 + 4 * l : 8 * l + 4;
+    const int at0 = turned && PAIRED_HALVES ? 4 * l : 8 * l;
+    const int at1 = turned && PAIRED_HALVES ? p.rot_dim / 2 + 4 * l : 8 * l + 4;
+    const int per = (part.heads + part.groups - 1) / part.groups;
+    const int h0 = group * per, h1 = min(group * per + per, part.heads);
+    const uint16_t* x = part.x + t * part.token;
+    uint16_t* out = part.out + (static_cast<int64_t>(b) * part.heads * p.rows + r) * 128;
+    const int64_t out_head = static_cast<int64_t>(p.rows) * 128;
 
-    float c[4], s[4];
-    if (turned) {
-        const double pos = static_cast<double>(p.lens ? static_cast<int64_t>(p.lens[b]) - p.rows + r : p.pos0 + r);
+    uint2 u[kBatch][2];
+    auto load = [&](int h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const uint16_t* from = x + min(h + j, part.heads - 1) * part.head;
+            u[j][0] = *reinterpret_cast<const uint2*>(from + at0);
+            u[j][1] = *reinterpret_cast<const uint2*>(from + at1);
+        }
+    };
+    auto store = [&](int h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (h + j < h1) {
+                uint16_t* to = out + (h + j) * out_head;
+                *reinterpret_cast<uint2*>(to + at0) = u[j][0];
+                *reinterpret_cast<uint2*>(to + at1) = u[j][1];
+            }
+    };
+    load(h0);                                      // requested before the angles are evaluated
+    Turn turn;
+    if (!part.plain) {
+        float w0[4] = {1.0f, 1.0f, 1.0f, 1.0f}, w1[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+        if (part.w) {
+            const float4 a = *reinterpret_cast<const float4*>(part.w + at0), c = *reinterpret_cast<const float4*>(part.w + at1);
+            w0[0] = a.x, w0[1] = a.y, w0[2] = a.z, w0[3] = a.w;
+            w1[0] = c.x, w1[1] = c.y, w1[2] = c.z, w1[3] = c.w;
+        }
+        double pos = 0.0;
+        if (turned) pos = static_cast<double>(p.lens ? static_cast<int64_t>(p.lens[b]) - p.rows + r : p.pos0 + r);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const double turns = pos * p.freq[4 * l + i] * 0.15915494309189533577;   // 1 / (2 pi)
-            const float f = static_cast<float>(turns - rint(turns));
-            sincospif(2.0f * f, &s[i], &c[i]);
-            c[i] *= p.magnitude;
-            s[i] *= p.magnitude;
+            float s = 0.0f, c = 1.0f;
+            if (turned) {
+                const double turns = pos * p.freq[4 * l + i] * 0.15915494309189533577;   // 1 / (2 pi)
+                sincospif(2.0f * static_cast<float>(turns - rint(turns)), &s, &c);
+                c *= p.magnitude;
+                s *= p.magnitude;
+            }
+            const float wa = PAIRED_HALVES ? w0[i] : i < 2 ? w0[2 * i] : w1[2 * i - 4];
+            const float wb = PAIRED_HALVES ? w1[i] : i < 2 ? w0[2 * i + 1] : w1[2 * i - 3];
+            turn.ca[i] = c * wa;
+            turn.sa[i] = s * wa;
+            turn.cb[i] = c * wb;
+            turn.sb[i] = s * wb;
         }
     }
-
-    const int h0 = blockIdx.y * p.heads_per_group, h1 = min(h0 + p.heads_per_group, p.heads);
-    for (int hh = h0 + slot / POSITIONS; hh < h1; hh += kHeads) {
-        const int which = hh < p.part[0].heads ? 0 : hh < p.part[0].heads + p.part[1].heads ? 1 : 2;
-        const int h = hh - (which > 0 ? p.part[0].heads : 0) - (which > 1 ? p.part[1].heads : 0);
-        const Part& part = p.part[which];
-        const uint16_t* x = part.x + t * part.token + h * part.head;
-        uint2 u0 = *reinterpret_cast<const uint2*>(x + at0), u1 = *reinterpret_cast<const uint2*>(x + at1);
-        if (which < 2) {
-            const uint32_t word[4] = {u0.x, u0.y, u1.x, u1.y};
-            float e[8];
+    for (int h = h0;;) {
+        if (!part.plain) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                e[2 * i] = __uint_as_float(word[i] << 16);
-                e[2 * i + 1] = __uint_as_float(word[i] & 0xffff0000u);
-            }
-            if (part.w) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum = fmaf(e[i], e[i], sum);
-                sum = row16_sum(sum);
-                float inv = rsqrtf(fmaf(sum, 1.0f / 128.0f, p.eps));
-                if (!(sum < INFINITY)) {          // squares past fp32: again with the row scaled down (eps is nothing beside it)
-                    sum = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        e[i] *= 8.470329472543003e-22f;                              // 2^-70
-                        sum = fmaf(e[i], e[i], sum);
-                    }
-                    inv = rsqrtf(row16_sum(sum) * (1.0f / 128.0f));
-                }
-                const float4 w0 = *reinterpret_cast<const float4*>(part.w + at0), w1 = *reinterpret_cast<const float4*>(part.w + at1);
-                const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = e[i] * inv * w[i];
-            }
-            if (turned) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float& a = p.pairing ? e[i] : e[2 * i];
-                    float& d = p.pairing ? e[4 + i] : e[2 * i + 1];
-                    const float a0 = a, d0 = d;
-                    a = fmaf(a0, c[i], -(d0 * s[i]));
-                    d = fmaf(a0, s[i], d0 * c[i]);
-                }
-            }
-            u0 = make_uint2(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]));
-            u1 = make_uint2(pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+            for (int j = 0; j < kBatch; ++j) norm_turn<PAIRED_HALVES>(u[j][0], u[j][1], turn, part.w, p.eps, turned);
         }
-        uint16_t* out = part.out + ((static_cast<int64_t>(b) * part.heads + h) * p.rows + r) * 128;
-        *reinterpret_cast<uint2*>(out + at0) = u0;
-        *reinterpret_cast<uint2*>(out + at1) = u1;
+        store(h);
+        h += kBatch;
+        if (h >= h1) break;
+        load(h);
     }
 }
 
@@ -183,9 +234,9 @@ extern "C" int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_
         p.part[i].head = in[i] ? in[i]->head_stride : 0;
         p.part[i].out = static_cast<uint16_t*>(out[i]);
         p.part[i].w = w[i];
+        p.part[i].plain = i == 2;
         p.part[i].heads = i == 0 ? q_heads : in[i] ? kv_heads : 0;
     }
-    p.heads = p.part[0].heads + p.part[1].heads + p.part[2].heads;
     p.tokens = static_cast<uint32_t>(batch * rows);
     p.rows = static_cast<uint32_t>(rows);
     p.lens = lens;
@@ -195,11 +246,20 @@ extern "C" int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_
     p.pairing = rotation->pairing;
     p.magnitude = rotation->magnitude;
     p.eps = eps;
-    constexpr int kPositions = 16;
     const unsigned blocks = (p.tokens + kPositions - 1) / kPositions;
-    p.heads_per_group = p.heads;
-    const dim3 grid(blocks, 1);
-    hipLaunchKernelGGL(norm_rope_kernel<kPositions>, grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream), p);
+        // Short calls: the heads are shared out over about two workgroups per compute unit, whole batches of heads together; every
+    // workgroup evaluates the angles of its positions.  One workgroup over all heads / shared out: 16 x 1 position, 32 / 8 heads 33.6 / 4.2 us,
+    // 4099 positions 92 / 22.7 (2048 workgroups 23.7, 8192 26.0), 131072 positions the same.
+    unsigned groups = 0;
+    for (Part& x : p.part) {
+        const int most = (x.heads + kBatch - 1) / kBatch;
+        x.groups = static_cast<int>((512ll * x.heads / (q_heads + 2 * kv_heads) + blocks - 1) / blocks);
+        x.groups = x.groups < 1 ? (x.heads > 0) : x.groups > most ? most : x.groups;
+        groups += x.groups;
+    }
+    const dim3 grid(blocks, groups);
+    auto* const kernel = rotation->pairing ? norm_rope_kernel<true> : norm_rope_kernel<false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream), p);
     VS_LAUNCH_CHECK();
     return VS_OK;
 }
