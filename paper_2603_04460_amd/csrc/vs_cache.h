@@ -20,7 +20,8 @@ struct CacheParams {
     uint8_t* data;
     const int32_t* table;          // null: sequence b has the pages b * max_pages ..
     const int32_t* lens;           // null: every sequence holds max_n tokens
-    int64_t pages;
+    int64_t head_bytes;            // of a head in a page
+    int pages;
     int max_pages;                 // of a sequence
     int kv_heads;
     int page_blocks;               // blocks of a page
@@ -40,17 +41,38 @@ constexpr int kBlock = VS_CACHE_BLOCK;
 constexpr int kBlockBytes = VS_CACHE_BLOCK_BYTES;
 constexpr int kVCodes = 4096, kKScales = 8192, kVScales = 8448;
 
+// Element i of an array that no kernel writes while this one runs, i the same for the wavefront: through the scalar cache, so that no wait
+// for it is a wait for the vector loads in flight.
+__device__ __forceinline__ int32_t scalar_load(const int32_t* x, int64_t i) {
+    const auto* at = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(x));
+    return at[i];
+}
+
 __device__ __forceinline__ int cache_length(const CacheParams& p, int b) {
     return p.lens ? min(max(p.lens[b], 0), p.max_n) : p.max_n;
 }
 
+// the same, b the same for the wavefront
+__device__ __forceinline__ int cache_length_scalar(const CacheParams& p, int b) {
+    return p.lens ? min(max(scalar_load(p.lens, b), 0), p.max_n) : p.max_n;
+}
+
+// entry i of sequence b in the page table; outside [0, pages): no page
+__device__ __forceinline__ int cache_page(const CacheParams& p, int b, int i) {
+    const int64_t entry = static_cast<int64_t>(b) * p.max_pages + i;
+    return p.table ? scalar_load(p.table, entry) : static_cast<int>(entry);
+}
+
+__device__ __forceinline__ bool cache_paged(const CacheParams& p, int page) { return static_cast<uint32_t>(page) < static_cast<uint32_t>(p.pages); }
+
+__device__ __forceinline__ int64_t cache_offset(const CacheParams& p, int page, int h, int in_page) {
+    return (static_cast<int64_t>(page) * p.kv_heads + h) * p.head_bytes + static_cast<int64_t>(in_page) * kBlockBytes;
+}
+
 // block `block` of sequence b, head h; null where the page table names no page
 __device__ __forceinline__ uint8_t* cache_block(const CacheParams& p, int b, int h, int block) {
-    const int at = block / p.page_blocks;
-    const int64_t entry = static_cast<int64_t>(b) * p.max_pages + at;
-    const int64_t page = p.table ? static_cast<int64_t>(p.table[entry]) : entry;
-    if (page < 0 || page >= p.pages) return nullptr;
-    return p.data + ((page * p.kv_heads + h) * p.page_blocks + (block - at * p.page_blocks)) * kBlockBytes;
+    const int i = block / p.page_blocks, page = cache_page(p, b, i);
+    return cache_paged(p, page) ? p.data + cache_offset(p, page, h, block - i * p.page_blocks) : nullptr;
 }
 
 __device__ __forceinline__ uint32_t v_word(int channel, int c, int u) {

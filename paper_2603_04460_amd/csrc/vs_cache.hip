@@ -44,7 +44,7 @@ __device__ __forceinline__ uint32_t quantise8(uint4 x, int* e_out) {
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheParams p, const uint16_t* k, const uint16_t* v, int rows) {
     __shared__ uint32_t codes[kBlock][17];               // V: token, piece of eight channels
     const int b = blockIdx.y / p.kv_heads, h = blockIdx.y - b * p.kv_heads;
-    const int len = cache_length(p, b);
+    const int len = cache_length_scalar(p, b);
     const int first = len - rows;                        // position of row 0
     const int block = max(first, 0) / kBlock + blockIdx.x;
     const int lo = max(first, 0) - block * kBlock, hi = len - block * kBlock;   // new tokens of the block: lo <= token < hi
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheParams p, co
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheParams p, uint16_t* k, uint16_t* v, int rows) {
     __shared__ __align__(16) uint8_t held[kBlockBytes - kVCodes];           // V codes, K scales, V scales
     const int b = blockIdx.y / p.kv_heads, h = blockIdx.y - b * p.kv_heads;
-    const int len = cache_length(p, b);
+    const int len = cache_length_scalar(p, b);
     const int first = len - rows;
     const int block = max(first, 0) / kBlock + blockIdx.x;
     const int lo = max(first, 0) - block * kBlock, hi = len - block * kBlock;
@@ -144,7 +144,8 @@ int cache_params(const vs_cache_t* cache, int batch, const int32_t* lens, int64_
     p->data = static_cast<uint8_t*>(cache->data);
     p->table = cache->table;
     p->lens = lens;
-    p->pages = cache->pages;
+    p->pages = static_cast<int>(cache->pages);
+    p->head_bytes = static_cast<int64_t>(cache->page_size / kBlock) * kBlockBytes;
     p->max_pages = cache->max_pages;
     p->kv_heads = cache->kv_heads;
     p->page_blocks = cache->page_size / kBlock;

@@ -10,9 +10,13 @@
 //   up to four query rows of a KV head (FOLD): the 16 columns are four rows x four channel groups; every column has its group's
 //     weights, and of each output tile the columns of its group count
 //   more: 16 rows a tile, four sets of weights
-// Running maximum and sum of the softmax per wavefront, merged in LDS at the end; where there are few (sequence, KV head) pairs, several
-// workgroups share the keys and a second kernel adds their parts up.
-// Bound by the memory for few rows: 136 bytes a key and KV head.
+// A wavefront has the running maximum and sum of its keys' softmax and everything it needs in registers, two blocks of codes among it, so
+// that the next one's loads are in flight while one is worked on.
+//   attend_head_kernel  short sequences: eight wavefronts share a head's keys and add up in LDS
+//   attend_row_kernel   all blocks of all heads and sequences in a row, divided evenly among the wavefronts of the GPU whatever the sequences'
+//                       lengths (which only the GPU knows); attend_join_kernel adds the parts up
+// Bound by the memory for few rows: 136 bytes a key and KV head.  32 / 8 heads, one token of 131072 34 us (142 MB; a plain read of as much
+// 24), of which the loop over the blocks 23, its slowest wavefront 26, the start 2 and the second kernel 5.
 #include <float.h>
 
 #include "vs_cache.h"
@@ -22,18 +26,23 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
+constexpr int kHeadWaves = 8;                              // that share the keys of a head
+constexpr int kDepth = 2;                                  // blocks in a wavefront's registers
+template <bool FOLD>
+constexpr int kRows = FOLD ? 4 : 16;                       // query rows of a tile
+constexpr float kStale = 8.0f;                             // log2 units by which a score may exceed the running maximum
+constexpr int kMaxParts = 256;                             // shares of one sequence and KV head: the threads of the joining kernel
 
 struct AttendParams {
     CacheParams cache;
     const uint16_t* q;
     uint16_t* o;
     float* lse;
-    float* part;                   // [splits][total rows][128] sums, then [splits][total rows] (maximum, sum of weights)
-    int n_q, rows;                 // new tokens; query rows of a KV head (group * n_q)
-    int total_rows;                // of all sequences and heads
-    int splits, units;             // units: sequences x KV heads
+    float* part;                   // [items][rows][128] sums, then [items][rows] (maximum, sum of weights)
+    int batch, n_q, rows;          // sequences; new tokens; query rows of a KV head (group * n_q)
+    int shares;                    // workgroups that divide the blocks among them; 0: one for each sequence and KV head
+    int least;                     // blocks of a workgroup at least
+    int items;                     // room in part: shares + sequences x KV heads
     float c;                       // scale * log2(e)
 };
 
@@ -64,252 +73,494 @@ struct Block {
     uint4 vs[FOLD ? 1 : 4];
 };
 
+// lane's offsets into a block: beside a block's address, the same for the wavefront, they are all that a load needs
 template <bool FOLD>
-__device__ __forceinline__ void load_block(Block<FOLD>& x, const uint8_t* at, int lane) {
-    const int c = lane >> 4, m = lane & 15;
+struct Offsets {
+    uint32_t k, v, ks, vs;
+    __device__ __forceinline__ explicit Offsets(int lane) {
+        const uint32_t c = lane >> 4, m = lane & 15;
+        k = 64 * m + 16 * c;
+        v = kVCodes + 16 * lane;
+        ks = kKScales + 4 * lane;
+        vs = kVScales + 64 * c + (FOLD ? 16 * (m & 3) : 0);
+    }
+};
+
+template <bool FOLD>
+__device__ __forceinline__ void load_block(Block<FOLD>& x, const uint8_t* at, const Offsets<FOLD>& off) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) x.k[t] = *reinterpret_cast<const uint4*>(at + 1024 * t + 64 * m + 16 * c);
+    for (int t = 0; t < 4; ++t) x.k[t] = *reinterpret_cast<const uint4*>(at + off.k + 1024 * t);
 #pragma unroll
-    for (int p = 0; p < 4; ++p) x.v[p] = *reinterpret_cast<const uint4*>(at + kVCodes + 1024 * p + 16 * lane);
-    x.ks = *reinterpret_cast<const uint32_t*>(at + kKScales + 4 * lane);
+    for (int p = 0; p < 4; ++p) x.v[p] = *reinterpret_cast<const uint4*>(at + off.v + 1024 * p);
+    x.ks = *reinterpret_cast<const uint32_t*>(at + off.ks);
 #pragma unroll
-    for (int g = 0; g < (FOLD ? 1 : 4); ++g) x.vs[g] = *reinterpret_cast<const uint4*>(at + kVScales + 64 * c + 16 * (FOLD ? m & 3 : g));
+    for (int g = 0; g < (FOLD ? 1 : 4); ++g) x.vs[g] = *reinterpret_cast<const uint4*>(at + off.vs + 16 * g);
 }
 
-// TILES tiles of query rows: FOLD four rows, else 16 rows each
-template <int TILES, bool FOLD>
-__global__ __launch_bounds__(kThreads) void cache_attend_kernel(AttendParams p) {
-    constexpr int kTileRows = FOLD ? 4 : 16;
-    constexpr int kKept = FOLD ? 2 : 8;                    // output tiles of 16 channels that a lane has values of
-    __shared__ float4 sums[kWaves][kKept][64];
-    __shared__ float2 stat[kWaves][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n = lane & 15, c = lane >> 4;
-    const int unit = blockIdx.x / p.splits, split = blockIdx.x - unit * p.splits;
-    const int b = unit / p.cache.kv_heads, h = unit - b * p.cache.kv_heads;
-    const int len = cache_length(p.cache, b);
-    const int blocks = (len + kBlock - 1) / kBlock;
-    const int per = (blocks + p.splits - 1) / p.splits;
-    const int first = split * per, last = min(first + per, blocks);
-    if (p.splits > 1 && first >= last) return;
+// position of the first key of a block without a page: no row sees it
+constexpr int kNowhere = 1 << 30;
 
-    bf16x8 q[TILES][4];
-    int row[TILES], limit[TILES];                          // last key that the column's row sees
-#pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-        row[i] = (blockIdx.y * TILES + i) * kTileRows + (FOLD ? n >> 2 : n);
-        const int r = min(row[i], p.rows - 1);
-        limit[i] = len - p.n_q + r % p.n_q;
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);    // last of a row of 16 to the next row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);    // last of the lower half to the upper
+    return x;
+}
+
+// The blocks of all sequences and KV heads in a row (sequence, head, block) are divided evenly among the workgroups, whatever the
+// lengths are; a workgroup may end one head and go on with the next.  A (workgroup, head) pair has the slot `workgroup + head's
+// number` for its part: from one pair of the row to the next at least one of the two grows.
+// Every wavefront finds its place by a scan over lens, 64 sequences at a time.
+struct Lengths {
+    int first;                     // of sequence `lane`: the usual batch is read once
+    int total;                     // blocks of one head over all sequences
+    int chunk;                     // blocks of a workgroup
+};
+
+__device__ __forceinline__ int length_at(const AttendParams& p, int b) { return b < p.batch ? cache_length(p.cache, b) : 0; }
+
+__device__ __forceinline__ int blocks_of(int len) { return (len + kBlock - 1) / kBlock; }
+
+__device__ __forceinline__ Lengths look(const AttendParams& p, int lane) {
+    Lengths x;
+    x.first = length_at(p, lane);
+    x.total = __builtin_amdgcn_readlane(wave_scan(blocks_of(x.first)), 63);
+    for (int at = 64; at < p.batch; at += 64) x.total += __builtin_amdgcn_readlane(wave_scan(blocks_of(length_at(p, at + lane))), 63);
+    const int all = x.total * p.cache.kv_heads;            // below 2^31: at most 65535 pairs of at most 16384 blocks
+    x.chunk = max((all + p.shares - 1) / p.shares, p.least);
+    return x;
+}
+
+struct Place {
+    int b, h, len;
+    int block;                     // of the sequence
+    int start;                     // of (b, h) in the row of all blocks
+    int page, in_page;             // entry of the page table and block of the page that `block` is
+};
+
+// place `x` of the row (below its end), or the begin of head h of sequence b (b >= 0)
+__device__ __forceinline__ Place find(const AttendParams& p, const Lengths& lens, int lane, int x, int b, int h) {
+    Place y;
+    int before = 0;
+    for (int at = 0;; at += 64) {
+        const int len = at == 0 ? lens.first : length_at(p, at + lane);
+        const int blocks = blocks_of(len);
+        const int upto = before + wave_scan(blocks);
+        const int l = b >= 0 ? b - at : __popcll(__ballot(upto * p.cache.kv_heads <= x));
+        if (l < 64) {
+            const int of = __builtin_amdgcn_readlane(blocks, l), base = (__builtin_amdgcn_readlane(upto, l) - of) * p.cache.kv_heads;
+            y.b = at + l;
+            y.len = __builtin_amdgcn_readlane(len, l);
+            y.h = b >= 0 ? h : (x - base) / of;
+            y.start = base + y.h * of;
+            y.block = b >= 0 ? 0 : x - y.start;
+            y.page = y.block / p.cache.page_blocks;
+            y.in_page = y.block - y.page * p.cache.page_blocks;
+            return y;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+}
+
+__device__ __forceinline__ float2* part_stat(const AttendParams& p) {
+    return reinterpret_cast<float2*>(p.part + static_cast<int64_t>(p.items) * p.rows * 128);
+}
+
+// What a wavefront knows of its query rows (FOLD: four, else 16) and keeps of the keys so far.
+template <bool FOLD>
+struct Rows {
+    static constexpr int kKept = FOLD ? 2 : 8;             // output tiles of 16 channels that a lane has values of
+    bf16x8 q[4];
+    int row, limit;                                        // of the lane's column; last key that the row sees
+    f32x4 o[8];
+    float top, sum;
+
+    __device__ __forceinline__ void begin(const AttendParams& p, int lane, int unit, int len) {
+        const int n = lane & 15, c = lane >> 4;
+        row = blockIdx.y * kRows<FOLD> + (FOLD ? n >> 2 : n);
+        const int r = min(row, p.rows - 1);
+        limit = len - p.n_q + r % p.n_q;
         const uint16_t* from = p.q + (static_cast<int64_t>(unit) * p.rows + r) * 128 + 32 * c;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[i][j] = operand(*reinterpret_cast<const uint4*>(from + 8 * j));
+        for (int j = 0; j < 4; ++j) q[j] = operand(*reinterpret_cast<const uint4*>(from + 8 * j));
+        top = -FLT_MAX;
+        sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    f32x4 o[TILES][8];
-    float top[TILES], sum[TILES];
-#pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-        top[i] = -FLT_MAX;
-        sum[i] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-
-    for (int block = first + wave; block < last; block += kWaves) {
-        const uint8_t* at = cache_block(p.cache, b, h, block);
-        if (!at) continue;
-        Block<FOLD> x;
-        load_block<FOLD>(x, at, lane);
-        const bool edge = block * kBlock + kBlock - 1 > len - p.n_q;      // some row does not see all of the block
-
-        f32x4 s[TILES][4];
+    // 64 keys from position `key` on; edge: some row does not see all of them
+    __device__ __forceinline__ void take(const AttendParams& p, const Block<FOLD>& x, int lane, int key, bool edge) {
+        const int c = lane >> 4;
+        f32x4 s[4];
+        float scale[4];
+        uint32_t word[4][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const float scale = __uint_as_float(((x.ks >> (8 * t)) & 0xffu) << 23);
-            const uint32_t w[4] = {x.k[t].x, x.k[t].y, x.k[t].z, x.k[t].w};
-#pragma unroll
-            for (int i = 0; i < TILES; ++i) s[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x8 a = operand(dequantise8(w[j], scale));
-#pragma unroll
-                for (int i = 0; i < TILES; ++i) s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[i][j], s[i][t], 0, 0, 0);
-            }
+            scale[t] = __uint_as_float(((x.ks >> (8 * t)) & 0xffu) << 23);
+            word[t][0] = x.k[t].x;
+            word[t][1] = x.k[t].y;
+            word[t][2] = x.k[t].z;
+            word[t][3] = x.k[t].w;
+            s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            if (edge) {
+        for (int j = 0; j < 4; ++j)                        // four independent products at a time
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (block * kBlock + 16 * t + 4 * c + e > limit[i]) s[i][t][e] = -INFINITY;
-            }
-            float m = -FLT_MAX;
+            for (int t = 0; t < 4; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(dequantise8(word[t][j], scale[t])), q[j], s[t], 0, 0, 0);
+        if (edge) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) m = fmaxf(m, s[i][t][e]);
-            m = column_reduce(m, [](float u, float v) { return fmaxf(u, v); });
-            m = fmaxf(top[i], m * p.c);
-            if (__any(m > top[i])) {
-                const float f = __builtin_amdgcn_exp2f(top[i] - m);
-                sum[i] *= f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[i][j] *= f;
-                top[i] = m;
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[i][t][e] = __builtin_amdgcn_exp2f(fmaf(s[i][t][e], p.c, -top[i]));
-                    sum[i] += s[i][t][e];
-                }
+                for (int e = 0; e < 4; ++e)
+                    if (key + 16 * t + 4 * c + e > limit) s[t][e] = -INFINITY;
+            asm volatile("" ::: "memory");                 // (a branch, not selects for every block)
         }
+        float most[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) most[t] = fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3]));
+        float m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * p.c;
+        // The maximum may be exceeded by 2^8: weights relative to a stale one are as exact, and the search across lanes and the rescaling are
+        // left out for most blocks.
+        if (__any(m > top + kStale)) {
+            m = fmaxf(top, column_reduce(m, [](float u, float v) { return fmaxf(u, v); }));
+            const float f = __builtin_amdgcn_exp2f(top - m);
+            sum *= f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] *= f;
+            top = m;
+        }
+        float part[4] = {sum, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], p.c, -top));
+                part[t] += s[t][e];
+            }
+        sum = (part[0] + part[1]) + (part[2] + part[3]);
 
-        bf16x8 w[TILES][2];
+        bf16x8 w[2];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             if (!FOLD || g == 0) {
                 const uint32_t e[4] = {x.vs[FOLD ? 0 : g].x, x.vs[FOLD ? 0 : g].y, x.vs[FOLD ? 0 : g].z, x.vs[FOLD ? 0 : g].w};
 #pragma unroll
-                for (int i = 0; i < TILES; ++i)
+                for (int u = 0; u < 2; ++u) {
+                    float y[8];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        float y[8];
+                    for (int a = 0; a < 8; ++a) y[a] = s[2 * u + (a >> 2)][a & 3] * scale_of(e[2 * u + (a >> 2)], a & 3);
+                    if (edge) {                            // a key that the row does not see has whatever scale the memory holds
 #pragma unroll
-                        for (int a = 0; a < 8; ++a) {
-                            const int t = 2 * u + (a >> 2);
-                            y[a] = s[i][t][a & 3] * scale_of(e[t], a & 3);
-                            // a key that the row does not see has whatever scale the memory holds
-                            if (edge && block * kBlock + 16 * t + 4 * c + (a & 3) > limit[i]) y[a] = 0.0f;
-                        }
-                        w[i][u] = operand(make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])));
+                        for (int a = 0; a < 8; ++a)
+                            if (key + 16 * (2 * u + (a >> 2)) + 4 * c + (a & 3) > limit) y[a] = 0.0f;
+                        asm volatile("" ::: "memory");
                     }
+                    w[u] = operand(make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])));
+                }
             }
             const uint32_t v[4] = {x.v[g].x, x.v[g].y, x.v[g].z, x.v[g].w};
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const bf16x8 a = operand(dequantise8(v[2 * half + u], 1.0f));
-#pragma unroll
-                    for (int i = 0; i < TILES; ++i)
-                        o[i][2 * g + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[i][u], o[i][2 * g + half], 0, 0, 0);
-                }
+                for (int half = 0; half < 2; ++half)
+                    o[2 * g + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(dequantise8(v[2 * half + u], 1.0f)), w[u], o[2 * g + half], 0, 0, 0);
         }
     }
 
-    // the wavefronts' parts
+    // output tile j of those that count in this lane
+    __device__ __forceinline__ float4 kept(int j, int lane) const {
+        f32x4 y = o[j];
+        if (FOLD) {                                        // the tiles of the column's group: 2 g + j
+            const int g = lane & 3;
 #pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-        if (i) __syncthreads();
-        const float all = column_reduce(sum[i], [](float u, float v) { return u + v; });
-        if (c == 0) stat[wave][n] = make_float2(top[i], all);
-#pragma unroll
-        for (int j = 0; j < kKept; ++j) {
-            f32x4 y = o[i][j];
-            if (FOLD) {                                    // the tiles of the column's group: 2 g + j
-                const int g = n & 3;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) y[k] = g == 0 ? o[i][j][k] : g == 1 ? o[i][2 + j][k] : g == 2 ? o[i][4 + j][k] : o[i][6 + j][k];
-            }
-            sums[wave][j][lane] = make_float4(y[0], y[1], y[2], y[3]);
+            for (int k = 0; k < 4; ++k) y[k] = g == 0 ? o[j][k] : g == 1 ? o[2 + j][k] : g == 2 ? o[4 + j][k] : o[6 + j][k];
         }
-        __syncthreads();
-        float m = -FLT_MAX, l = 0.0f, f[kWaves];
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) m = fmaxf(m, stat[k][n].x);
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) {
-            f[k] = __builtin_amdgcn_exp2f(stat[k][n].x - m);
-            l += f[k] * stat[k][n].y;
-        }
-        const bool there = row[i] < p.rows;
-        const int64_t r = static_cast<int64_t>(unit) * p.rows + row[i];
-        for (int j = wave; j < kKept && there; j += kWaves) {
-            float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int k = 0; k < kWaves; ++k) {
-                const float4 z = sums[k][j][lane];
-                y.x = fmaf(z.x, f[k], y.x);
-                y.y = fmaf(z.y, f[k], y.y);
-                y.z = fmaf(z.z, f[k], y.z);
-                y.w = fmaf(z.w, f[k], y.w);
-            }
-            const int channel = (FOLD ? 32 * (n & 3) + 16 * j : 16 * j) + 4 * c;
-            if (p.splits == 1) {
-                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                *reinterpret_cast<uint2*>(p.o + r * 128 + channel) = make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
-            } else {
-                *reinterpret_cast<float4*>(p.part + (static_cast<int64_t>(split) * p.total_rows + r) * 128 + channel) = y;
-            }
-        }
-        if (there && wave == 0 && c == 0 && (!FOLD || (n & 3) == 0)) {
-            if (p.splits == 1) {
-                if (p.lse) p.lse[r] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
-            } else {
-                reinterpret_cast<float2*>(p.part + static_cast<int64_t>(p.splits) * p.total_rows * 128)[static_cast<int64_t>(split) * p.total_rows + r] = make_float2(m, l);
-            }
-        }
+        return make_float4(y[0], y[1], y[2], y[3]);
     }
+    // its first channel
+    static __device__ __forceinline__ int channel(int j, int lane) { return (FOLD ? 32 * (lane & 3) : 0) + 16 * j + 4 * (lane >> 4); }
+    // one lane of those that hold a row's statistics
+    static __device__ __forceinline__ bool speaks(int lane) { return lane < 16 && (!FOLD || (lane & 3) == 0); }
+    __device__ __forceinline__ float total() const {
+        return column_reduce(sum, [](float u, float v) { return u + v; });
+    }
+};
+
+__device__ __forceinline__ void put_row(const AttendParams& p, int64_t r, int channel, float4 y, float l) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    *reinterpret_cast<uint2*>(p.o + r * 128 + channel) = make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
 }
 
-// One row per workgroup: 32 lanes hold its channels, the eight groups of them take the parts in turn.
-__global__ __launch_bounds__(256) void cache_join_kernel(AttendParams p) {
-    __shared__ float4 sums[8][32];
-    const int r = blockIdx.x, lane = threadIdx.x & 31, group = threadIdx.x >> 5;
-    const int b = r / (p.rows * p.cache.kv_heads);
-    const int blocks = (cache_length(p.cache, b) + kBlock - 1) / kBlock;
-    const int per = (blocks + p.splits - 1) / p.splits;
-    const int parts = per ? (blocks + per - 1) / per : 0;
-    const float2* stat = reinterpret_cast<const float2*>(p.part + static_cast<int64_t>(p.splits) * p.total_rows * 128) + r;
-    float m = -FLT_MAX, l = 0.0f;
-    for (int s = 0; s < parts; ++s) m = fmaxf(m, stat[static_cast<int64_t>(s) * p.total_rows].x);
-    for (int s = 0; s < parts; ++s) {
-        const float2 x = stat[static_cast<int64_t>(s) * p.total_rows];
-        l += x.y * __builtin_amdgcn_exp2f(x.x - m);
+__device__ __forceinline__ void put_lse(const AttendParams& p, int64_t r, float m, float l) {
+    if (p.lse) p.lse[r] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+}
+
+// A workgroup for each (sequence, KV head): kHeadWaves wavefronts take its blocks in turn and add up in LDS.
+template <bool FOLD>
+__global__ __launch_bounds__(64 * kHeadWaves) void attend_head_kernel(AttendParams p) {
+    using R = Rows<FOLD>;
+    __shared__ float4 sums[kHeadWaves][R::kKept][64];
+    __shared__ float2 stat[kHeadWaves][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int unit = blockIdx.x, b = unit / p.cache.kv_heads, h = unit - b * p.cache.kv_heads;
+    const int len = cache_length_scalar(p.cache, b), last = blocks_of(len);
+    R rows;
+    rows.begin(p, lane, unit, len);
+
+    // Two blocks in registers: the next one's loads are in flight while one is worked on, and its address is known before.  Loads and
+    // work are unconditional (a branch around them would make the wait for the older loads a wait for all): past the end
+    // the last block is fetched again, without a page the begin of the cache, and no row sees it.
+    const Offsets<FOLD> off(lane);
+    auto address = [&](int i, bool* there) __attribute__((always_inline)) {
+        const uint8_t* x = cache_block(p.cache, b, h, min(i, last - 1));
+        *there = i < last && x;
+        return x ? x : p.cache.data;
+    };
+    auto take = [&](const Block<FOLD>& x, int i, bool there) __attribute__((always_inline)) {
+        const int key = there ? i * kBlock : kNowhere;
+        rows.take(p, x, lane, key, key + kBlock - 1 > len - p.n_q);
+    };
+    if (wave < last) {
+        bool there0, there1, there2;
+        const uint8_t *at0 = address(wave, &there0), *at1 = address(wave + kHeadWaves, &there1);
+        Block<FOLD> x0, x1;
+        load_block<FOLD>(x0, at0, off);
+        for (int block = wave;;) {
+            at0 = address(block + 2 * kHeadWaves, &there2);
+            load_block<FOLD>(x1, at1, off);
+            take(x0, block, there0);
+            there0 = there2;
+            if ((block += kHeadWaves) >= last) break;
+            at1 = address(block + 2 * kHeadWaves, &there2);
+            load_block<FOLD>(x0, at0, off);
+            take(x1, block, there1);
+            there1 = there2;
+            if ((block += kHeadWaves) >= last) break;
+        }
     }
-    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int s = group; s < parts; s += 8) {
-        const float f = __builtin_amdgcn_exp2f(stat[static_cast<int64_t>(s) * p.total_rows].x - m);
-        const float4 z = *reinterpret_cast<const float4*>(p.part + (static_cast<int64_t>(s) * p.total_rows + r) * 128 + 4 * lane);
-        y.x = fmaf(z.x, f, y.x);
-        y.y = fmaf(z.y, f, y.y);
-        y.z = fmaf(z.z, f, y.z);
-        y.w = fmaf(z.w, f, y.w);
-    }
-    sums[group][lane] = y;
-    __syncthreads();
-    if (group) return;
+
+    const float all = rows.total();
+    if (lane < 16) stat[wave][lane] = make_float2(rows.top, all);
 #pragma unroll
-    for (int k = 1; k < 8; ++k) {
-        const float4 z = sums[k][lane];
-        y.x += z.x;
-        y.y += z.y;
-        y.z += z.z;
-        y.w += z.w;
+    for (int j = 0; j < R::kKept; ++j) sums[wave][j][lane] = rows.kept(j, lane);
+    __syncthreads();
+    if (rows.row >= p.rows) return;
+    const int n = lane & 15;
+    float m = -FLT_MAX, l = 0.0f, f[kHeadWaves];
+#pragma unroll
+    for (int k = 0; k < kHeadWaves; ++k) m = fmaxf(m, stat[k][n].x);
+#pragma unroll
+    for (int k = 0; k < kHeadWaves; ++k) {
+        f[k] = __builtin_amdgcn_exp2f(stat[k][n].x - m);
+        l += f[k] * stat[k][n].y;
     }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    *reinterpret_cast<uint2*>(p.o + static_cast<int64_t>(r) * 128 + 4 * lane) = make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
-    if (p.lse && lane == 0) p.lse[r] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+    const int64_t r = static_cast<int64_t>(unit) * p.rows + rows.row;
+    for (int j = wave; j < R::kKept; j += kHeadWaves) {
+        float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < kHeadWaves; ++k) {
+            const float4 z = sums[k][j][lane];
+            y.x = fmaf(z.x, f[k], y.x);
+            y.y = fmaf(z.y, f[k], y.y);
+            y.z = fmaf(z.z, f[k], y.z);
+            y.w = fmaf(z.w, f[k], y.w);
+        }
+        put_row(p, r, R::channel(j, lane), y, l);
+    }
+    if (wave == 0 && R::speaks(lane)) put_lse(p, r, m, l);
+}
+
+// Every wavefront by itself takes `chunk` consecutive blocks of the row of all blocks, from one head and sequence to the next.
+template <bool FOLD>
+__global__ __launch_bounds__(256, 2) void attend_row_kernel(AttendParams p) {
+    using R = Rows<FOLD>;
+    const int lane = threadIdx.x & 63;
+    const int share = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    Place at;
+    int left;
+    {
+        const Lengths lens = look(p, lane);
+        const int begin = share * lens.chunk;              // below 2^31: the last share begins less than `shares` chunks from the end
+        left = min(lens.total * p.cache.kv_heads - begin, lens.chunk);
+        if (left <= 0) return;
+        at = find(p, lens, lane, begin, -1, 0);
+    }
+    // the block behind the one at x; the last one of the share stays
+    auto next = [&](Place& x, int* remain) __attribute__((always_inline)) {
+        if (*remain <= 1) return;
+        --*remain;
+        if (++x.in_page == p.cache.page_blocks) {
+            x.in_page = 0;
+            ++x.page;
+        }
+        if (++x.block < blocks_of(x.len)) return;
+        x.block = x.page = x.in_page = 0;
+        if (++x.h < p.cache.kv_heads) return;
+        x.h = 0;
+        do x.len = cache_length_scalar(p.cache, ++x.b);
+        while (x.len == 0 && x.b < p.batch - 1);
+    };
+    // A block's codes are requested kDepth - 1 blocks ahead, its page one more.  Loads and work are unconditional (a branch around them
+    // would make the wait for the older loads a wait for all): without a page the begin of the cache is fetched and no row sees it.
+    const Offsets<FOLD> off(lane);
+    struct Held {
+        Block<FOLD> x;
+        int unit, block, len, key;
+    };
+    int remain = left, page;
+    auto look_up = [&]() __attribute__((always_inline)) { page = cache_page(p.cache, at.b, at.page); };
+    auto fetch = [&](Held& y) __attribute__((always_inline)) {
+        const bool paged = cache_paged(p.cache, page);
+        load_block<FOLD>(y.x, p.cache.data + (paged ? cache_offset(p.cache, page, at.h, at.in_page) : 0), off);
+        y.unit = at.b * p.cache.kv_heads + at.h;
+        y.block = at.block;
+        y.len = at.len;
+        y.key = paged ? at.block * kBlock : kNowhere;
+        next(at, &remain);
+        look_up();
+    };
+
+    R rows;
+    int unit = -1, from = 0;                               // head at work, its first block here
+    auto finish = [&](int len, int upto) __attribute__((always_inline)) {
+        const bool whole = from == 0 && upto == blocks_of(len);
+        const float l = rows.total();
+        if (rows.row >= p.rows) return;
+        const int64_t r = static_cast<int64_t>(unit) * p.rows + rows.row, slot = static_cast<int64_t>(share + unit) * p.rows + rows.row;
+#pragma unroll
+        for (int j = 0; j < R::kKept; ++j) {
+            const float4 y = rows.kept(j, lane);
+            if (whole) put_row(p, r, R::channel(j, lane), y, l);
+            else *reinterpret_cast<float4*>(p.part + slot * 128 + R::channel(j, lane)) = y;
+        }
+        if (R::speaks(lane)) {
+            if (whole) put_lse(p, r, rows.top, l);
+            else part_stat(p)[slot] = make_float2(rows.top, l);
+        }
+    };
+    int len_at = 0, upto = 0;
+    auto take = [&](const Held& y) __attribute__((always_inline)) {
+        if (y.unit != unit) {
+            if (unit >= 0) finish(len_at, upto);
+            unit = y.unit;
+            from = y.block;
+            len_at = y.len;
+            rows.begin(p, lane, unit, y.len);
+            __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): behind the branch nothing is in flight that it would have to wait for
+        }
+        rows.take(p, y.x, lane, y.key, y.key + kBlock - 1 > y.len - p.n_q);
+        upto = y.block + 1;
+    };
+
+    Held ring[kDepth];
+    look_up();
+    static_for<kDepth - 1>([&](auto k) __attribute__((always_inline)) { fetch(ring[k]); });
+    for (; left >= kDepth; left -= kDepth)
+        static_for<kDepth>([&](auto k) __attribute__((always_inline)) {
+            fetch(ring[(k + kDepth - 1) % kDepth]);
+            take(ring[k]);
+        });
+    static_for<kDepth - 1>([&](auto k) __attribute__((always_inline)) {
+        if (k < left) take(ring[k]);
+    });
+    finish(len_at, upto);
+}
+
+// The parts of a row added up.  A workgroup has SLICE channels of a row: SLICE / 4 lanes hold them, the other lanes are that many groups,
+// which take the parts in turn; their first loads go out together with the statistics, which every thread reads of one part.
+template <int SLICE>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
+    constexpr int kLanes = SLICE / 4, kGroups = 256 / kLanes, kAhead = 4;
+    __shared__ float weight[kMaxParts];
+    __shared__ float4 sums[kGroups][kLanes];
+    __shared__ float2 wave_stat[4];
+    const int unit = blockIdx.x / p.rows, row = blockIdx.x - unit * p.rows;
+    const int64_t r = blockIdx.x;
+    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, b = unit / p.cache.kv_heads;
+    const int channel = blockIdx.y * SLICE + 4 * lane;
+    const Lengths lens = look(p, threadIdx.x & 63);
+    const Place at = find(p, lens, threadIdx.x & 63, 0, b, unit - b * p.cache.kv_heads);
+    const int blocks = blocks_of(at.len);
+    const int from_share = at.start / lens.chunk;
+    const int parts = blocks ? (at.start + blocks - 1) / lens.chunk - from_share + 1 : 0;
+    if (parts == 1) return;                                // written by the wavefront that has all of the keys
+    const int64_t slot = static_cast<int64_t>(from_share + unit) * p.rows + row;
+    const float4* from = reinterpret_cast<const float4*>(p.part + slot * 128 + channel);
+    const int64_t step = static_cast<int64_t>(p.rows) * 32;
+    float4 z[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+        z[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (group + kGroups * k < parts) z[k] = from[(group + kGroups * k) * step];
+    }
+    float2 mine = make_float2(-FLT_MAX, 0.0f);
+    if (static_cast<int>(threadIdx.x) < parts) mine = part_stat(p)[slot + static_cast<int64_t>(threadIdx.x) * p.rows];
+    const float m_wave = wave_max(mine.x);
+    if ((threadIdx.x & 63) == 0) wave_stat[threadIdx.x >> 6].x = m_wave;
+    __syncthreads();
+    const float m = fmaxf(fmaxf(wave_stat[0].x, wave_stat[1].x), fmaxf(wave_stat[2].x, wave_stat[3].x));
+    const float f = __builtin_amdgcn_exp2f(mine.x - m);
+    weight[threadIdx.x] = f;
+    const float l_wave = wave_sum(f * mine.y);
+    if ((threadIdx.x & 63) == 0) wave_stat[threadIdx.x >> 6].y = l_wave;
+    __syncthreads();
+    const float l = (wave_stat[0].y + wave_stat[1].y) + (wave_stat[2].y + wave_stat[3].y);
+    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto add = [&](const float4& x, float g) __attribute__((always_inline)) {
+        y.x = fmaf(x.x, g, y.x);
+        y.y = fmaf(x.y, g, y.y);
+        y.z = fmaf(x.z, g, y.z);
+        y.w = fmaf(x.w, g, y.w);
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+        if (group + kGroups * k < parts) add(z[k], weight[group + kGroups * k]);
+    for (int s = group + kGroups * kAhead; s < parts; s += kGroups) add(from[s * step], weight[s]);
+    sums[group][lane] = y;
+    for (int half = kGroups / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (group < half) {
+            const float4 x = sums[group + half][lane];
+            y.x += x.x;
+            y.y += x.y;
+            y.z += x.z;
+            y.w += x.w;
+            sums[group][lane] = y;
+        }
+    }
+    if (group) return;
+    put_row(p, r, channel, y, l);
+    if (channel == 0) put_lse(p, r, m, l);
 }
 
 struct Plan {
-    int tiles, fold, groups, splits;       // tiles per wavefront, kernel, workgroups over the rows of a unit, workgroups over the keys
+    bool fold;
+    int groups;                    // workgroups over the rows of a sequence and KV head
+    int shares, least;             // see AttendParams
+    int64_t items;
 };
 
 Plan plan(int64_t units, int rows, int64_t max_n) {
     Plan x;
     x.fold = rows <= 4;
-    x.tiles = !x.fold && rows > 16 ? 2 : 1;
-    const int per = (x.fold ? 4 : 16) * x.tiles;
+    const int per = x.fold ? kRows<true> : kRows<false>;
     x.groups = (rows + per - 1) / per;
     const int64_t blocks = (max_n + kBlock - 1) / kBlock;
-    int64_t splits = 1024 / (units * x.groups);
-    if (splits > blocks / (2 * kWaves)) splits = blocks / (2 * kWaves);
-    x.splits = static_cast<int>(splits < 1 ? 1 : splits);
+    // Short sequences: one workgroup for each head, two rounds of its eight wavefronts at most (four where there are many heads), and no second
+    // kernel, which costs 3 to 4 us.  One workgroup a head / blocks in a row, us: 32 / 8 heads, one sequence of 500 tokens 5.5 / 7.9,
+    // 1000 7.0 / 7.9, 2000 9.9 / 8.0, 16 sequences of 1000 7.1 / 9.2, 2000 10.5 / 11.8, 4000 16.9 / 15.4, 64 of 2000 18.7 / 20.8.
+    const bool by_head = blocks <= 2 * kHeadWaves || (blocks <= 4 * kHeadWaves && units * x.groups >= 128);
+    // Otherwise a wavefront for every SIMD: with two blocks in registers each that is enough to keep the memory busy, and more of them only make more
+    // parts.  512 / 1024 / 1536 / 2048 wavefronts, us: 32 / 8 heads, one sequence of 32768 tokens 16.4 / 14.0 / 16.6 / 16.5, 131072 41 / 34 /
+    // 37 / 36, 64 of 8000 59 / 45 / 47 / 44, four new tokens of 131072 54 / 38 / 43 / 41.
+    x.shares = by_head ? 0 : 1024 / x.groups < 4 ? 4 : 1024 / x.groups / 4 * 4;
+    x.least = static_cast<int>((blocks + kMaxParts - 3) / (kMaxParts - 2));
+    x.items = x.shares ? units + x.shares : units;
     return x;
 }
 
@@ -323,7 +574,7 @@ bool sizes_ok(int batch, int q_heads, int kv_heads, int n_q, int64_t max_n) {
 extern "C" size_t vs_cache_attend_workspace(int batch, int q_heads, int kv_heads, int n_q, int64_t max_n) {
     if (!sizes_ok(batch, q_heads, kv_heads, n_q, max_n)) return 0;
     const Plan x = plan(static_cast<int64_t>(batch) * kv_heads, q_heads / kv_heads * n_q, max_n);
-    return x.splits == 1 ? 0 : static_cast<size_t>(x.splits) * batch * q_heads * n_q * (VS_HEAD_DIM + 2) * sizeof(float);
+    return x.shares ? static_cast<size_t>(x.items) * (q_heads / kv_heads * n_q) * (VS_HEAD_DIM + 2) * sizeof(float) : 0;
 }
 
 extern "C" int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch, int q_heads, int n_q, const int32_t* lens, int64_t max_n,
@@ -338,24 +589,29 @@ extern "C" int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch
     p.rows = q_heads / cache->kv_heads * n_q;
     if (units * p.rows > (1 << 26)) return VS_ERR_UNSUPPORTED;
     const Plan x = plan(units, p.rows, max_n);
-    if (x.splits > 1 && (!ws || ws_bytes < vs_cache_attend_workspace(batch, q_heads, cache->kv_heads, n_q, max_n))) return VS_ERR_WORKSPACE;
+    if (x.shares && (!ws || ws_bytes < vs_cache_attend_workspace(batch, q_heads, cache->kv_heads, n_q, max_n))) return VS_ERR_WORKSPACE;
     p.q = static_cast<const uint16_t*>(q);
     p.o = static_cast<uint16_t*>(o);
     p.lse = lse;
     p.part = static_cast<float*>(ws);
+    p.batch = batch;
     p.n_q = n_q;
-    p.units = static_cast<int>(units);
-    p.total_rows = static_cast<int>(units * p.rows);
-    p.splits = x.splits;
+    p.shares = x.shares;
+    p.least = x.least;
+    p.items = static_cast<int>(x.items);
     p.c = scale * 1.44269504088896340736f;
-    const dim3 grid(static_cast<unsigned>(units * x.splits), x.groups);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    auto* const kernel = x.fold ? cache_attend_kernel<1, true> : x.tiles == 1 ? cache_attend_kernel<1, false> : cache_attend_kernel<2, false>;
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, p);
-    VS_LAUNCH_CHECK();
-    if (x.splits > 1) {
-        hipLaunchKernelGGL(cache_join_kernel, dim3(p.total_rows), dim3(256), 0, s, p);
+    if (!x.shares) {
+        hipLaunchKernelGGL(x.fold ? attend_head_kernel<true> : attend_head_kernel<false>, dim3(static_cast<unsigned>(units), x.groups),
+                           dim3(64 * kHeadWaves), 0, s, p);
         VS_LAUNCH_CHECK();
+        return VS_OK;
     }
+    hipLaunchKernelGGL(x.fold ? attend_row_kernel<true> : attend_row_kernel<false>, dim3(x.shares / 4, x.groups), dim3(256), 0, s, p);
+    VS_LAUNCH_CHECK();
+    const unsigned total = static_cast<unsigned>(units * p.rows);
+    if (total < 512) hipLaunchKernelGGL(attend_join_kernel<32>, dim3(total, 4), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(attend_join_kernel<128>, dim3(total), dim3(256), 0, s, p);
+    VS_LAUNCH_CHECK();
     return VS_OK;
 }

@@ -244,6 +244,19 @@ def test_attend_bound_far_above_the_lengths():
     check(*call(c, q, lens, max_n), q, k, v, lens)
 
 
+@pytest.mark.parametrize("batch, hq, hk, n_q", [(65, 4, 1, 1), (150, 2, 2, 1), (130, 8, 1, 3)])
+@pytest.mark.parametrize("max_n", [700, 20000])
+def test_attend_many_sequences(batch, hq, hk, n_q, max_n):
+    """More sequences than a wavefront has lanes, of all lengths, idle ones at both ends and in the middle."""
+    rng = np.random.default_rng(batch)
+    lens = np.where(rng.random(batch) < 0.3, 0, np.exp(rng.uniform(0, np.log(700), batch)).astype(int))
+    lens[[0, 1, 63, 64, -1]] = 0
+    lens[2] = 700
+    lens = [int(x) for x in lens]
+    c, q, k, v, n = attend_case(100 + batch, hq, hk, n_q, lens, 64, max_n=max_n)
+    check(*call(c, q, lens, n), q, k, v, lens)
+
+
 def test_attend_large_scores_and_scale():
     """A softmax that one key owns, and one that is flat."""
     for q_scale, scale in ((30.0, None), (1.0, 1e-4), (1.0, 3.0)):
