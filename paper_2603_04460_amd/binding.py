@@ -129,14 +129,15 @@ def version():
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream):
     if stream is None:
         import torch
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+        # the handle of torch.cuda.current_stream() without the object around it, which costs more than a launch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _check(rc, where):
@@ -151,13 +152,14 @@ def _dev(t, dtype, what):
     return t
 
 
-def _here(*tensors):
-    """All on the current device: the launch goes there, whatever device a tensor is on."""
+def _on(at, t, dtype, what):
+    """_dev, and on device `at`, the current one: the launch goes there, whatever device a tensor is on."""
     import torch
-    at = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != at:
-            raise ValueError("tensor on %s, current device cuda:%d" % (t.device, at))
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_cuda and t.is_contiguous()):
+        raise TypeError("%s must be a contiguous CUDA tensor of dtype %s" % (what, dtype))
+    if t.get_device() != at:
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (what, t.device, at))
+    return t
 
 
 class IndexerWeights:
@@ -439,16 +441,21 @@ class Rope:
         return self._c
 
 
-def _rows(x, what):
-    """A [tokens, heads, 128] tensor with any strides of tokens and heads."""
+def _rows(at, x, shape, what):
+    """Address and strides (a vs_rows_t) of a [tokens, heads, 128] tensor with any strides of tokens and heads."""
     import torch
-    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 3):
+    if not (isinstance(x, torch.Tensor) and x.dtype == torch.bfloat16 and x.is_cuda):
         raise TypeError("%s must be a CUDA tensor [tokens, heads, 128] of dtype torch.bfloat16" % what)
-    tokens, heads, d = x.shape
+    if x.get_device() != at:
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (what, x.device, at))
+    assert x.shape == shape, "%s must be [%d, %d, 128]" % ((what,) + shape[:2])
     st, sh, sd = x.stride()
-    assert d == 128 and sd == 1, "%s: elements of a head must be contiguous" % what
+    assert sd == 1, "%s: elements of a head must be contiguous" % what
     # a stride that no step uses may be anything
-    return _Rows(x.data_ptr(), st if tokens > 1 else 128, sh if heads > 1 else 128)
+    return x.data_ptr(), st if shape[0] > 1 else 128, sh if shape[1] > 1 else 128
+
+
+_ThreeRows = ctypes.c_int64 * (3 * ctypes.sizeof(_Rows) // 8)
 
 
 def qk_norm_rope(q, k, q_out, k_out, rope, v=None, v_out=None, w_q=None, w_k=None, eps=1e-6, lens=None, pos0=0, stream=None):
@@ -457,25 +464,28 @@ def qk_norm_rope(q, k, q_out, k_out, rope, v=None, v_out=None, w_q=None, w_k=Non
     sequence), tokens = batch * rows.  w_q, w_k [128] fp32 or None: no norm.  lens [batch] int32: row r of sequence b is position
     lens[b] - rows + r; None: pos0 + r."""
     import torch
-    _dev(q_out, torch.bfloat16, "q_out"); _dev(k_out, torch.bfloat16, "k_out")
-    batch, q_heads, rows, d = q_out.shape if q_out.dim() == 4 else (1,) + tuple(q_out.shape)
-    kv_heads = k.shape[1]
-    assert d == 128 and q.shape == (batch * rows, q_heads, 128) and k.shape == (batch * rows, kv_heads, 128)
-    assert k_out.numel() == batch * kv_heads * rows * 128 and k_out.shape[-2] == rows and k_out.shape[-3] == kv_heads
-    assert (v is None) == (v_out is None)
-    cq, ck, cv = _rows(q, "q"), _rows(k, "k"), None
+    at = torch.cuda.current_device()
+    shape = _on(at, q_out, torch.bfloat16, "q_out").shape
+    batch, q_heads, rows, d = shape if len(shape) == 4 else (1,) + tuple(shape)
+    kv_heads, tokens = k.shape[1], batch * rows
+    assert d == 128 and (v is None) == (v_out is None)
+    k_shape, k_in = shape[:-3] + (kv_heads, rows, 128), (tokens, kv_heads, 128)
+    assert _on(at, k_out, torch.bfloat16, "k_out").shape == k_shape
+    x = _rows(at, q, (tokens, q_heads, 128), "q") + _rows(at, k, k_in, "k")
     if v is not None:
-        _dev(v_out, torch.bfloat16, "v_out")
-        assert v.shape == k.shape and v_out.shape == k_out.shape
-        cv = _rows(v, "v")
-    for name, w in (("w_q", w_q), ("w_k", w_k)):
-        if w is not None:
-            assert _dev(w, torch.float32, name).numel() == 128
+        assert _on(at, v_out, torch.bfloat16, "v_out").shape == k_shape
+        x += _rows(at, v, k_in, "v")
+    x = _ThreeRows(*x)
+    if w_q is not None:
+        assert _on(at, w_q, torch.float32, "w_q").numel() == 128
+    if w_k is not None:
+        assert _on(at, w_k, torch.float32, "w_k").numel() == 128
     if lens is not None:
-        assert _dev(lens, torch.int32, "lens").numel() == batch
-    _here(q, k, v, q_out, k_out, v_out, w_q, w_k, lens, rope.freq)
-    _check(_load().vs_qk_norm_rope(ctypes.byref(cq), ctypes.byref(ck), None if cv is None else ctypes.byref(cv), batch, rows, q_heads,
-                                   kv_heads, _ptr(w_q), _ptr(w_k), eps, rope._ref, _ptr(lens), int(pos0), _ptr(q_out), _ptr(k_out),
+        assert _on(at, lens, torch.int32, "lens").numel() == batch
+    _on(at, rope.freq, torch.float64, "freq")
+    rows_at, size = ctypes.addressof(x), ctypes.sizeof(_Rows)
+    _check(_load().vs_qk_norm_rope(rows_at, rows_at + size, None if v is None else rows_at + 2 * size, batch, rows, q_heads, kv_heads,
+                                   _ptr(w_q), _ptr(w_k), eps, rope._ref, _ptr(lens), pos0, q_out.data_ptr(), k_out.data_ptr(),
                                    _ptr(v_out), _stream(stream)), "vs_qk_norm_rope")
     return q_out, k_out
 
@@ -505,36 +515,38 @@ class Cache:
     def c_struct(self):
         return self._c
 
-    def _batch(self, x, heads, lens, what):
+    def _batch(self, at, x, heads, lens, what):
         import torch
-        _dev(x, torch.bfloat16, what)
-        batch, h, rows, d = x.shape if x.dim() == 4 else (1,) + tuple(x.shape)
+        shape = _on(at, x, torch.bfloat16, what).shape
+        batch, h, rows, d = shape if len(shape) == 4 else (1,) + tuple(shape)
         assert d == 128 and (heads is None or h == heads)
-        assert self.table is None or self.table.shape[0] == batch
+        _on(at, self.data, torch.uint8, "data")
+        if self.table is not None:
+            assert _on(at, self.table, torch.int32, "table").shape[0] == batch
         if lens is not None:
-            assert _dev(lens, torch.int32, "lens").numel() == batch
-        _here(x, lens, self.data, self.table)
+            assert _on(at, lens, torch.int32, "lens").numel() == batch
         return batch, h, rows
 
 
 def cache_write(cache, k, v, max_n, lens=None, stream=None):
     """Quantises k, v [batch, kv_heads, rows, 128] (or without the batch dimension) into the cache as the last tokens of sequences
     that then hold lens [batch] int32 tokens each (None: max_n)."""
-    batch, _, rows = cache._batch(k, cache.kv_heads, lens, "k")
-    cache._batch(v, cache.kv_heads, None, "v")
-    assert v.shape == k.shape
-    _check(_load().vs_cache_write(cache._ref, _ptr(k), _ptr(v), batch, rows, _ptr(lens), int(max_n), _stream(stream)), "vs_cache_write")
+    import torch
+    at = torch.cuda.current_device()
+    batch, _, rows = cache._batch(at, k, cache.kv_heads, lens, "k")
+    assert _on(at, v, torch.bfloat16, "v").shape == k.shape
+    _check(_load().vs_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), batch, rows, _ptr(lens), max_n, _stream(stream)), "vs_cache_write")
     return cache
 
 
 def cache_read(cache, k, v, max_n, lens=None, stream=None):
     """The last tokens of each sequence as the cache holds them, into k, v [batch, kv_heads, rows, 128] bf16 (one may be None)."""
-    x = k if k is not None else v
-    batch, _, rows = cache._batch(x, cache.kv_heads, lens, "k" if k is not None else "v")
+    import torch
+    at = torch.cuda.current_device()
+    batch, _, rows = cache._batch(at, k if k is not None else v, cache.kv_heads, lens, "k" if k is not None else "v")
     if k is not None and v is not None:
-        cache._batch(v, cache.kv_heads, None, "v")
-        assert v.shape == k.shape
-    _check(_load().vs_cache_read(cache._ref, batch, rows, _ptr(lens), int(max_n), _ptr(k), _ptr(v), _stream(stream)), "vs_cache_read")
+        assert _on(at, v, torch.bfloat16, "v").shape == k.shape
+    _check(_load().vs_cache_read(cache._ref, batch, rows, _ptr(lens), max_n, _ptr(k), _ptr(v), _stream(stream)), "vs_cache_read")
     return k, v
 
 
@@ -546,13 +558,14 @@ def cache_attend(q, cache, o, max_n, lens=None, lse=None, ws=None, scale=None, s
     """Attention of the last n_q tokens of each sequence over the cache (which holds them): q, o [batch, q_heads, n_q, 128] (or without
     the batch dimension), lse [batch, q_heads, n_q] fp32 or None."""
     import torch
-    batch, q_heads, n_q = cache._batch(q, None, lens, "q")
-    _dev(o, torch.bfloat16, "o")
-    assert o.shape == q.shape
+    at = torch.cuda.current_device()
+    batch, q_heads, n_q = cache._batch(at, q, None, lens, "q")
+    assert _on(at, o, torch.bfloat16, "o").shape == q.shape
     if lse is not None:
-        assert _dev(lse, torch.float32, "lse").numel() == batch * q_heads * n_q
-    _here(o, lse, ws)
+        assert _on(at, lse, torch.float32, "lse").numel() == batch * q_heads * n_q
+    if ws is not None and ws.get_device() != at:
+        raise ValueError("ws is on %s, the current device is cuda:%d" % (ws.device, at))
     scale = 128 ** -0.5 if scale is None else scale
-    _check(_load().vs_cache_attend(_ptr(q), cache._ref, batch, q_heads, n_q, _ptr(lens), int(max_n), scale, _ptr(o), _ptr(lse), _ptr(ws),
+    _check(_load().vs_cache_attend(q.data_ptr(), cache._ref, batch, q_heads, n_q, _ptr(lens), max_n, scale, o.data_ptr(), _ptr(lse), _ptr(ws),
                                    0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "vs_cache_attend")
     return o
