@@ -39,10 +39,35 @@ __device__ __forceinline__ uint32_t quantise8(uint4 x, int* e_out) {
     return r;
 }
 
-// Workgroup (x, y): the x-th block that the new tokens of sequence b touch, of head h (y = b kv_heads + h).  A word of V
-// codes that also holds other tokens keeps their nibbles; it belongs to one thread.
+// Eight codes of V for each of 64 tokens in `codes` -> the four words of piece (p, c, m) of the block: channels 32 p + m and 16 more, u = 0, 1;
+// `mine`: nibbles of tokens in [lo, hi).
+__device__ __forceinline__ uint4 v_piece(const uint32_t (*codes)[17], int piece, int lo, int hi, uint4* mine) {
+    const int p = piece >> 6, c = (piece >> 4) & 3, m = piece & 15;
+    uint32_t value[4] = {0, 0, 0, 0}, mask[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int token = 32 * u + (e < 4 ? 0 : 16) + 4 * c + (e & 3);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                value[2 * b + u] |= ((codes[token][4 * p + 2 * b + (m >> 3)] >> (4 * (m & 7))) & 15u) << (4 * e);
+            if (token >= lo && token < hi) {
+                mask[u] |= 15u << (4 * e);
+                mask[2 + u] |= 15u << (4 * e);
+            }
+        }
+    *mine = make_uint4(mask[0], mask[1], mask[2], mask[3]);
+    return make_uint4(value[0], value[1], value[2], value[3]);
+}
+
+// Workgroup (x, y): the x-th block that the new tokens of sequence b touch, of head h (y = b kv_heads + h).  A block of new tokens
+// only is put together in LDS and written in pieces of 16 bytes; of others every thread writes what belongs to new tokens, and a word of
+// V codes, which belongs to one thread, keeps the other tokens' nibbles.
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheParams p, const uint16_t* k, const uint16_t* v, int rows) {
+    __shared__ __align__(16) uint32_t k_codes[kBlock][16];
     __shared__ uint32_t codes[kBlock][17];               // V: token, piece of eight channels
+    __shared__ __align__(16) uint8_t scales[512];
     const int b = blockIdx.y / p.kv_heads, h = blockIdx.y - b * p.kv_heads;
     const int len = cache_length_scalar(p, b);
     const int first = len - rows;                        // position of row 0
@@ -51,44 +76,54 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheParams p, co
     if (hi <= 0) return;
     uint8_t* const to = cache_block(p, b, h, block);
     if (!to) return;
-    const int l = threadIdx.x & 15;
+    const int l = threadIdx.x & 15, g = l >> 2, token0 = threadIdx.x >> 4;
     const int64_t head = static_cast<int64_t>(blockIdx.y) * rows;
+    const uint16_t* const from_k = k + (head + block * kBlock - first) * 128 + 8 * l;
+    const uint16_t* const from_v = v + (head + block * kBlock - first) * 128 + 8 * l;
+    if (lo <= 0 && hi >= kBlock) {
+        uint4 x[kBlock / 16][2];
 #pragma unroll
-    for (int i = 0; i < kBlock / 16; ++i) {
-        const int token = (threadIdx.x >> 4) + 16 * i;
-        if (token >= lo && token < hi) {
-            const int64_t at = (head + (block * kBlock + token - first)) * 128 + 8 * l;
+        for (int i = 0; i < kBlock / 16; ++i) {
+            x[i][0] = *reinterpret_cast<const uint4*>(from_k + (token0 + 16 * i) * 128);
+            x[i][1] = *reinterpret_cast<const uint4*>(from_v + (token0 + 16 * i) * 128);
+        }
+#pragma unroll
+        for (int i = 0; i < kBlock / 16; ++i) {
+            const int token = token0 + 16 * i;
             int ek, ev;
-            const uint32_t kw = quantise8(*reinterpret_cast<const uint4*>(k + at), &ek);
-            const uint32_t vw = quantise8(*reinterpret_cast<const uint4*>(v + at), &ev);
-            *reinterpret_cast<uint32_t*>(to + token * 64 + 4 * l) = kw;
-            codes[token][l] = vw;
+            k_codes[token][l] = quantise8(x[i][0], &ek);
+            codes[token][l] = quantise8(x[i][1], &ev);
             if ((l & 3) == 0) {
-                const int g = l >> 2;
-                to[kKScales + 4 * (16 * g + (token & 15)) + (token >> 4)] = static_cast<uint8_t>(ek);
-                to[kVScales + 16 * (4 * ((token >> 2) & 3) + g) + 4 * (token >> 4) + (token & 3)] = static_cast<uint8_t>(ev);
+                scales[4 * (16 * g + (token & 15)) + (token >> 4)] = static_cast<uint8_t>(ek);
+                scales[256 + 16 * (4 * ((token >> 2) & 3) + g) + 4 * (token >> 4) + (token & 3)] = static_cast<uint8_t>(ev);
             }
+        }
+        __syncthreads();
+        uint4 mine;
+        reinterpret_cast<uint4*>(to)[threadIdx.x] = reinterpret_cast<const uint4*>(k_codes)[threadIdx.x];
+        reinterpret_cast<uint4*>(to + kVCodes)[threadIdx.x] = v_piece(codes, threadIdx.x, 0, kBlock, &mine);
+        if (threadIdx.x < 32) reinterpret_cast<uint4*>(to + kKScales)[threadIdx.x] = reinterpret_cast<const uint4*>(scales)[threadIdx.x];
+        return;
+    }
+    const int begin = max(lo, 0), end = min(hi, kBlock);
+    for (int token = begin + token0; token < end; token += 16) {
+        int ek, ev;
+        const uint4 xk = *reinterpret_cast<const uint4*>(from_k + token * 128), xv = *reinterpret_cast<const uint4*>(from_v + token * 128);
+        *reinterpret_cast<uint32_t*>(to + token * 64 + 4 * l) = quantise8(xk, &ek);
+        codes[token][l] = quantise8(xv, &ev);
+        if ((l & 3) == 0) {
+            to[kKScales + 4 * (16 * g + (token & 15)) + (token >> 4)] = static_cast<uint8_t>(ek);
+            to[kVScales + 16 * (4 * ((token >> 2) & 3) + g) + 4 * (token >> 4) + (token & 3)] = static_cast<uint8_t>(ev);
         }
     }
     __syncthreads();
+    uint4 mine;
+    const uint4 value = v_piece(codes, threadIdx.x, lo, hi, &mine);
+    const uint32_t w[4] = {value.x, value.y, value.z, value.w}, mask[4] = {mine.x, mine.y, mine.z, mine.w};
+    uint32_t* const at = reinterpret_cast<uint32_t*>(to + kVCodes) + 4 * threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < 1024 / kThreads; ++i) {
-        const int word = threadIdx.x + kThreads * i;     // V word in the block's order: p, c, m, b, u
-        const int u = word & 1, ch = 32 * (word >> 8) + 16 * ((word >> 1) & 1) + ((word >> 2) & 15), c = (word >> 6) & 3;
-        uint32_t value = 0, mine = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int token = 32 * u + (e < 4 ? 0 : 16) + 4 * c + (e & 3);
-            if (token >= lo && token < hi) {
-                value |= ((codes[token][ch >> 3] >> (4 * (ch & 7))) & 15u) << (4 * e);
-                mine |= 15u << (4 * e);
-            }
-        }
-        if (mine) {
-            uint32_t* const at = reinterpret_cast<uint32_t*>(to + kVCodes) + word;
-            *at = mine == 0xffffffffu ? value : (*at & ~mine) | value;
-        }
-    }
+    for (int i = 0; i < 4; ++i)
+        if (mask[i]) at[i] = mask[i] == 0xffffffffu ? w[i] : (at[i] & ~mask[i]) | (w[i] & mask[i]);
 }
 
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheParams p, uint16_t* k, uint16_t* v, int rows) {
