@@ -17,34 +17,16 @@
 //                       lengths (which only the GPU knows); attend_join_kernel adds the parts up
 // Bound by the memory for few rows: 136 bytes a key and KV head.  32 / 8 heads, one token of 131072 34 us (142 MB; a plain read of as much
 // 24), of which the loop over the blocks 23, its slowest wavefront 26, the start 2 and the second kernel 5.
-#include <float.h>
-
-#include "vs_cache.h"
+#include "vs_cache_attend.h"
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kHeadWaves = 8;                              // that share the keys of a head
 constexpr int kDepth = 2;                                  // blocks in a wavefront's registers
 template <bool FOLD>
 constexpr int kRows = FOLD ? 4 : 16;                       // query rows of a tile
-constexpr float kStale = 8.0f;                             // log2 units by which a score may exceed the running maximum
-constexpr int kMaxParts = 256;                             // shares of one sequence and KV head: the threads of the joining kernel
-
-struct AttendParams {
-    CacheParams cache;
-    const uint16_t* q;
-    uint16_t* o;
-    float* lse;
-    float* part;                   // [items][rows][128] sums, then [items][rows] (maximum, sum of weights)
-    int batch, n_q, rows;          // sequences; new tokens; query rows of a KV head (group * n_q)
-    int shares;                    // workgroups that divide the blocks among them; 0: one for each sequence and KV head
-    int least;                     // blocks of a workgroup at least
-    int items;                     // room in part: shares + sequences x KV heads
-    float c;                       // scale * log2(e)
-};
 
 // over the four lanes that hold the same column
 template <typename F>
@@ -56,15 +38,6 @@ __device__ __forceinline__ float column_reduce(float x, F op) {
     const unsigned q0 = q[0], q1 = q[1];
     return op(__builtin_bit_cast(float, q0), __builtin_bit_cast(float, q1));
 }
-
-// Scale byte i of a word as a number.  The lowest bit of the fraction makes the byte 255 a NaN instead of an infinity and is
-// far below the weights' rounding.
-__device__ __forceinline__ float scale_of(uint32_t w, int i) {
-    const uint32_t field = i == 0 ? w << 23 : i == 1 ? w << 15 : i == 2 ? w << 7 : w >> 1;
-    return __uint_as_float((field & 0x7f800000u) | 1u);
-}
-
-__device__ __forceinline__ bf16x8 operand(uint4 x) { return __builtin_bit_cast(bf16x8, x); }
 
 template <bool FOLD>
 struct Block {
@@ -95,79 +68,6 @@ __device__ __forceinline__ void load_block(Block<FOLD>& x, const uint8_t* at, co
     x.ks = *reinterpret_cast<const uint32_t*>(at + off.ks);
 #pragma unroll
     for (int g = 0; g < (FOLD ? 1 : 4); ++g) x.vs[g] = *reinterpret_cast<const uint4*>(at + off.vs + 16 * g);
-}
-
-// position of the first key of a block without a page: no row sees it
-constexpr int kNowhere = 1 << 30;
-
-// inclusive sum over the lanes up to this one
-__device__ __forceinline__ int wave_scan(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);    // last of a row of 16 to the next row
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);    // last of the lower half to the upper
-    return x;
-}
-
-// The blocks of all sequences and KV heads in a row (sequence, head, block) are divided evenly among the workgroups, whatever the
-// lengths are; a workgroup may end one head and go on with the next.  A (workgroup, head) pair has the slot `workgroup + head's
-// number` for its part: from one pair of the row to the next at least one of the two grows.
-// Every wavefront finds its place by a scan over lens, 64 sequences at a time.
-struct Lengths {
-    int first;                     // of sequence `lane`: the usual batch is read once
-    int total;                     // blocks of one head over all sequences
-    int chunk;                     // blocks of a workgroup
-};
-
-__device__ __forceinline__ int length_at(const AttendParams& p, int b) { return b < p.batch ? cache_length(p.cache, b) : 0; }
-
-__device__ __forceinline__ int blocks_of(int len) { return (len + kBlock - 1) / kBlock; }
-
-__device__ __forceinline__ Lengths look(const AttendParams& p, int lane) {
-    Lengths x;
-    x.first = length_at(p, lane);
-    x.total = __builtin_amdgcn_readlane(wave_scan(blocks_of(x.first)), 63);
-    for (int at = 64; at < p.batch; at += 64) x.total += __builtin_amdgcn_readlane(wave_scan(blocks_of(length_at(p, at + lane))), 63);
-    const int all = x.total * p.cache.kv_heads;            // below 2^31: at most 65535 pairs of at most 16384 blocks
-    x.chunk = max((all + p.shares - 1) / p.shares, p.least);
-    return x;
-}
-
-struct Place {
-    int b, h, len;
-    int block;                     // of the sequence
-    int start;                     // of (b, h) in the row of all blocks
-    int page, in_page;             // entry of the page table and block of the page that `block` is
-};
-
-// place `x` of the row (below its end), or the begin of head h of sequence b (b >= 0)
-__device__ __forceinline__ Place find(const AttendParams& p, const Lengths& lens, int lane, int x, int b, int h) {
-    Place y;
-    int before = 0;
-    for (int at = 0;; at += 64) {
-        const int len = at == 0 ? lens.first : length_at(p, at + lane);
-        const int blocks = blocks_of(len);
-        const int upto = before + wave_scan(blocks);
-        const int l = b >= 0 ? b - at : __popcll(__ballot(upto * p.cache.kv_heads <= x));
-        if (l < 64) {
-            const int of = __builtin_amdgcn_readlane(blocks, l), base = (__builtin_amdgcn_readlane(upto, l) - of) * p.cache.kv_heads;
-            y.b = at + l;
-            y.len = __builtin_amdgcn_readlane(len, l);
-            y.h = b >= 0 ? h : (x - base) / of;
-            y.start = base + y.h * of;
-            y.block = b >= 0 ? 0 : x - y.start;
-            y.page = y.block / p.cache.page_blocks;
-            y.in_page = y.block - y.page * p.cache.page_blocks;
-            return y;
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
-    }
-}
-
-__device__ __forceinline__ float2* part_stat(const AttendParams& p) {
-    return reinterpret_cast<float2*>(p.part + static_cast<int64_t>(p.items) * p.rows * 128);
 }
 
 // What a wavefront knows of its query rows (FOLD: four, else 16) and keeps of the keys so far.
@@ -290,15 +190,6 @@ struct Rows {
         return column_reduce(sum, [](float u, float v) { return u + v; });
     }
 };
-
-__device__ __forceinline__ void put_row(const AttendParams& p, int64_t r, int channel, float4 y, float l) {
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    *reinterpret_cast<uint2*>(p.o + r * 128 + channel) = make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
-}
-
-__device__ __forceinline__ void put_lse(const AttendParams& p, int64_t r, float m, float l) {
-    if (p.lse) p.lse[r] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
-}
 
 // A workgroup for each (sequence, KV head): kHeadWaves wavefronts take its blocks in turn and add up in LDS.
 template <bool FOLD>
@@ -540,6 +431,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
 
 struct Plan {
     bool fold;
+    bool many;                     // rows: the kernel of vs_cache_tile.hip
     int groups;                    // workgroups over the rows of a sequence and KV head
     int shares, least;             // see AttendParams
     int64_t items;
@@ -560,6 +452,16 @@ Plan plan(int64_t units, int rows, int64_t max_n) {
     // 37 / 36, 64 of 8000 59 / 45 / 47 / 44, four new tokens of 131072 54 / 38 / 43 / 41.
     x.shares = by_head ? 0 : 1024 / x.groups < 4 ? 4 : 1024 / x.groups / 4 * 4;
     x.least = static_cast<int>((blocks + kMaxParts - 3) / (kMaxParts - 2));
+    // Many rows: every workgroup turns a block into bf16 once for 256 rows; one workgroup on every compute unit, twelve blocks for each at least (its
+    // start and its larger parts cost about as much as six).  16 rows a wavefront / 256 a workgroup, us: 32 / 8 heads, 32768 tokens, 16 new ones (64 rows)
+    // 32.7 / 37.0, 20 41.5 / 38.1, 32 54 / 41, 64 99 / 54, 100 156 / 85, 8 heads, 100 of 30000 48.5 / 41.0; four sequences of 5000, 32 new ones (10 blocks
+    // for each workgroup) 24.9 / 27.7, one head, 128 of 30000 (2) 16.1 / 18.7.
+    const int tile_groups = (rows + vs::kTileRows - 1) / vs::kTileRows;
+    x.many = x.shares && rows > 72 && units * blocks * tile_groups >= 12 * 256;
+    if (x.many) {
+        x.groups = tile_groups;
+        x.shares = 256 / tile_groups < 1 ? 1 : 256 / tile_groups;
+    }
     x.items = x.shares ? units + x.shares : units;
     return x;
 }
@@ -607,8 +509,13 @@ extern "C" int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch
         VS_LAUNCH_CHECK();
         return VS_OK;
     }
-    hipLaunchKernelGGL(x.fold ? attend_row_kernel<true> : attend_row_kernel<false>, dim3(x.shares / 4, x.groups), dim3(256), 0, s, p);
-    VS_LAUNCH_CHECK();
+    if (x.many) {
+        const int tile_rc = vs::launch_attend_tile(p, x.groups, s);
+        if (tile_rc != VS_OK) return tile_rc;
+    } else {
+        hipLaunchKernelGGL(x.fold ? attend_row_kernel<true> : attend_row_kernel<false>, dim3(x.shares / 4, x.groups), dim3(256), 0, s, p);
+        VS_LAUNCH_CHECK();
+    }
     const unsigned total = static_cast<unsigned>(units * p.rows);
     if (total < 512) hipLaunchKernelGGL(attend_join_kernel<32>, dim3(total, 4), dim3(256), 0, s, p);
     else hipLaunchKernelGGL(attend_join_kernel<128>, dim3(total), dim3(256), 0, s, p);

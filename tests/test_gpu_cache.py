@@ -234,6 +234,39 @@ def test_attend_one_long_sequence(n_q, n, page):
     check(*call(c, q, None, max_n), q, k, v, [n])
 
 
+@pytest.mark.parametrize("n_q, lens, max_n, hq, hk", [(100, [13001], 13001, 32, 4), (128, [30001], 60000, 8, 2), (73, [3000, 0, 40, 5001, 73], 60000, 16, 16),
+                                                     (128, [20000, 100, 64, 0], 20000, 33, 11)])
+def test_attend_many_rows(n_q, lens, max_n, hq, hk):
+    """Chunks of a hundred rows and more over long contexts: row blocks that are not full, several sequences in a share, idle ones."""
+    c, q, k, v, n = attend_case(200 + n_q + hq, hq, hk, n_q, lens, 192, max_n=max_n)
+    rows = hq // hk * n_q
+    # the kernel for many rows: 256 rows a workgroup, its parts and one for each head
+    assert vs.cache_attend_workspace(len(lens), hq, hk, n_q, n) == (len(lens) * hk + 256 // -(-rows // 256)) * rows * 130 * 4
+    check(*call(c, q, lens, n), q, k, v, lens, heads=range(min(hk, 2)))
+
+
+def test_attend_many_rows_missing_pages_and_values_that_are_not_finite():
+    n, n_q, hq, hk = 50000, 100, 8, 4
+    at = [n - 30, 77]
+    k, v = tokens(301, 1, hk, n), tokens(302, 1, hk, n)
+    v[0, 0, at[0], 40] = float("nan")
+    k[0, 1, at[0], 3] = float("inf")
+    c, q, _, _, _ = attend_case(300, hq, hk, n_q, [n], 256, k=k, v=v)
+    o, lse = call(c, q, [n], n)
+    o, lse = o.float().view(hk, hq // hk, n_q, 128), lse.view(hk, hq // hk, n_q)
+    sees = torch.arange(n - n_q, n) >= at[0]
+    assert torch.isnan(o[0][:, sees][..., 32:64]).all() and torch.isfinite(o[0][..., :32]).all() and torch.isfinite(o[0][..., 64:]).all()
+    assert torch.isfinite(o[0][:, ~sees]).all() and torch.isfinite(lse[0]).all()
+    assert torch.isnan(o[1][:, sees]).all() and torch.isnan(lse[1][:, sees]).all()
+    assert torch.isfinite(o[1][:, ~sees]).all() and torch.isfinite(lse[1][:, ~sees]).all() and torch.isfinite(o[2:]).all()
+    check(*call(c, q, [n], n), q, k, v, [n], heads=[2])
+    table = c.table.clone()
+    table[0, 3], table[0, -1], table[0, 100] = -1, c.pages, 2 ** 31 - 1
+    pages = [3, table.shape[1] - 1, 100]
+    dead = [np.concatenate([np.arange(256 * i, min(256 * i + 256, n)) for i in pages])]
+    check(*call(vs.Cache(c.data, table), q, [n], n), q, k, v, [n], heads=[3], dead=dead)
+
+
 def test_attend_bound_far_above_the_lengths():
     """Lengths far below max_n: workgroups without keys, parts that nobody writes; a full slot among idle ones."""
     lens = [5, 0, 30000, 64, 1000]
