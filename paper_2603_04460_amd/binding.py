@@ -132,11 +132,11 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream(stream):
+def _stream(stream, at=None):
     if stream is None:
         import torch
         # the handle of torch.cuda.current_stream() without the object around it, which costs more than a launch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if at is None else at)
     return stream.cuda_stream
 
 
@@ -154,12 +154,13 @@ def _dev(t, dtype, what):
 
 def _on(at, t, dtype, what):
     """_dev, and on device `at`, the current one: the launch goes there, whatever device a tensor is on."""
-    import torch
-    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_cuda and t.is_contiguous()):
-        raise TypeError("%s must be a contiguous CUDA tensor of dtype %s" % (what, dtype))
-    if t.get_device() != at:
-        raise ValueError("%s is on %s, the current device is cuda:%d" % (what, t.device, at))
-    return t
+    try:
+        if t.dtype is dtype and t.get_device() == at and t.is_contiguous():
+            return t
+    except AttributeError:
+        pass
+    _dev(t, dtype, what)
+    raise ValueError("%s is on %s, the current device is cuda:%d" % (what, t.device, at))
 
 
 class IndexerWeights:
@@ -435,17 +436,20 @@ class Rope:
         assert freq.dim() == 1
         self.pairing, self.magnitude = int(pairing), float(magnitude)
         self._c = _Rotation(freq.data_ptr(), 2 * freq.numel(), self.pairing, self.magnitude)
-        self._ref = ctypes.byref(self._c)
+        self._ref, self._device = ctypes.byref(self._c), freq.get_device()
+
+    def _on(self, at):
+        if self._device != at:
+            raise ValueError("freq is on %s, the current device is cuda:%d" % (self.freq.device, at))
 
     def c_struct(self):
         return self._c
 
 
-def _rows(at, x, shape, what):
+def _rows(at, x, dtype, shape, what):
     """Address and strides (a vs_rows_t) of a [tokens, heads, 128] tensor with any strides of tokens and heads."""
-    import torch
-    if not (isinstance(x, torch.Tensor) and x.dtype == torch.bfloat16 and x.is_cuda):
-        raise TypeError("%s must be a CUDA tensor [tokens, heads, 128] of dtype torch.bfloat16" % what)
+    if not (getattr(x, "dtype", None) is dtype and x.is_cuda):
+        raise TypeError("%s must be a CUDA tensor [tokens, heads, 128] of dtype %s" % (what, dtype))
     if x.get_device() != at:
         raise ValueError("%s is on %s, the current device is cuda:%d" % (what, x.device, at))
     assert x.shape == shape, "%s must be [%d, %d, 128]" % ((what,) + shape[:2])
@@ -464,29 +468,29 @@ def qk_norm_rope(q, k, q_out, k_out, rope, v=None, v_out=None, w_q=None, w_k=Non
     sequence), tokens = batch * rows.  w_q, w_k [128] fp32 or None: no norm.  lens [batch] int32: row r of sequence b is position
     lens[b] - rows + r; None: pos0 + r."""
     import torch
-    at = torch.cuda.current_device()
-    shape = _on(at, q_out, torch.bfloat16, "q_out").shape
+    at, bf16, fp32 = torch.cuda.current_device(), torch.bfloat16, torch.float32
+    shape = _on(at, q_out, bf16, "q_out").shape
     batch, q_heads, rows, d = shape if len(shape) == 4 else (1,) + tuple(shape)
     kv_heads, tokens = k.shape[1], batch * rows
     assert d == 128 and (v is None) == (v_out is None)
     k_shape, k_in = shape[:-3] + (kv_heads, rows, 128), (tokens, kv_heads, 128)
-    assert _on(at, k_out, torch.bfloat16, "k_out").shape == k_shape
-    x = _rows(at, q, (tokens, q_heads, 128), "q") + _rows(at, k, k_in, "k")
+    assert _on(at, k_out, bf16, "k_out").shape == k_shape
+    x = _rows(at, q, bf16, (tokens, q_heads, 128), "q") + _rows(at, k, bf16, k_in, "k")
     if v is not None:
-        assert _on(at, v_out, torch.bfloat16, "v_out").shape == k_shape
-        x += _rows(at, v, k_in, "v")
+        assert _on(at, v_out, bf16, "v_out").shape == k_shape
+        x += _rows(at, v, bf16, k_in, "v")
     x = _ThreeRows(*x)
     if w_q is not None:
-        assert _on(at, w_q, torch.float32, "w_q").numel() == 128
+        assert _on(at, w_q, fp32, "w_q").numel() == 128
     if w_k is not None:
-        assert _on(at, w_k, torch.float32, "w_k").numel() == 128
+        assert _on(at, w_k, fp32, "w_k").numel() == 128
     if lens is not None:
         assert _on(at, lens, torch.int32, "lens").numel() == batch
-    _on(at, rope.freq, torch.float64, "freq")
-    rows_at, size = ctypes.addressof(x), ctypes.sizeof(_Rows)
-    _check(_load().vs_qk_norm_rope(rows_at, rows_at + size, None if v is None else rows_at + 2 * size, batch, rows, q_heads, kv_heads,
-                                   _ptr(w_q), _ptr(w_k), eps, rope._ref, _ptr(lens), pos0, q_out.data_ptr(), k_out.data_ptr(),
-                                   _ptr(v_out), _stream(stream)), "vs_qk_norm_rope")
+    rope._on(at)
+    rows_at = ctypes.addressof(x)
+    _check((_lib or _load()).vs_qk_norm_rope(rows_at, rows_at + 24, None if v is None else rows_at + 48, batch, rows, q_heads, kv_heads, _ptr(w_q),
+                                             _ptr(w_k), eps, rope._ref, _ptr(lens), pos0, q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out),
+                                             _stream(stream, at)), "vs_qk_norm_rope")
     return q_out, k_out
 
 
@@ -510,21 +514,22 @@ class Cache:
         self.pages, self.kv_heads, self.page_size = data.shape[0], data.shape[1], data.shape[2] * CACHE_BLOCK
         self._c = _Cache(data.data_ptr(), self.pages, self.kv_heads, self.page_size, None if table is None else table.data_ptr(),
                          self.max_pages)
-        self._ref = ctypes.byref(self._c)
+        self._ref, self._device = ctypes.byref(self._c), data.get_device()
+        if table is not None and table.get_device() != self._device:
+            raise ValueError("data is on %s, table on %s" % (data.device, table.device))
 
     def c_struct(self):
         return self._c
 
-    def _batch(self, at, x, heads, lens, what):
-        import torch
-        shape = _on(at, x, torch.bfloat16, what).shape
+    def _batch(self, at, x, bf16, heads, lens, int32, what):
+        shape = _on(at, x, bf16, what).shape
         batch, h, rows, d = shape if len(shape) == 4 else (1,) + tuple(shape)
         assert d == 128 and (heads is None or h == heads)
-        _on(at, self.data, torch.uint8, "data")
-        if self.table is not None:
-            assert _on(at, self.table, torch.int32, "table").shape[0] == batch
+        if self._device != at:
+            raise ValueError("the cache is on %s, the current device is cuda:%d" % (self.data.device, at))
+        assert self.table is None or self.table.shape[0] == batch
         if lens is not None:
-            assert _on(at, lens, torch.int32, "lens").numel() == batch
+            assert _on(at, lens, int32, "lens").numel() == batch
         return batch, h, rows
 
 
@@ -532,21 +537,22 @@ def cache_write(cache, k, v, max_n, lens=None, stream=None):
     """Quantises k, v [batch, kv_heads, rows, 128] (or without the batch dimension) into the cache as the last tokens of sequences
     that then hold lens [batch] int32 tokens each (None: max_n)."""
     import torch
-    at = torch.cuda.current_device()
-    batch, _, rows = cache._batch(at, k, cache.kv_heads, lens, "k")
-    assert _on(at, v, torch.bfloat16, "v").shape == k.shape
-    _check(_load().vs_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), batch, rows, _ptr(lens), max_n, _stream(stream)), "vs_cache_write")
+    at, bf16 = torch.cuda.current_device(), torch.bfloat16
+    batch, _, rows = cache._batch(at, k, bf16, cache.kv_heads, lens, torch.int32, "k")
+    assert _on(at, v, bf16, "v").shape == k.shape
+    _check((_lib or _load()).vs_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), batch, rows, _ptr(lens), max_n, _stream(stream, at)),
+           "vs_cache_write")
     return cache
 
 
 def cache_read(cache, k, v, max_n, lens=None, stream=None):
     """The last tokens of each sequence as the cache holds them, into k, v [batch, kv_heads, rows, 128] bf16 (one may be None)."""
     import torch
-    at = torch.cuda.current_device()
-    batch, _, rows = cache._batch(at, k if k is not None else v, cache.kv_heads, lens, "k" if k is not None else "v")
+    at, bf16 = torch.cuda.current_device(), torch.bfloat16
+    batch, _, rows = cache._batch(at, v if k is None else k, bf16, cache.kv_heads, lens, torch.int32, "v" if k is None else "k")
     if k is not None and v is not None:
-        assert _on(at, v, torch.bfloat16, "v").shape == k.shape
-    _check(_load().vs_cache_read(cache._ref, batch, rows, _ptr(lens), max_n, _ptr(k), _ptr(v), _stream(stream)), "vs_cache_read")
+        assert _on(at, v, bf16, "v").shape == k.shape
+    _check((_lib or _load()).vs_cache_read(cache._ref, batch, rows, _ptr(lens), max_n, _ptr(k), _ptr(v), _stream(stream, at)), "vs_cache_read")
     return k, v
 
 
@@ -558,14 +564,14 @@ def cache_attend(q, cache, o, max_n, lens=None, lse=None, ws=None, scale=None, s
     """Attention of the last n_q tokens of each sequence over the cache (which holds them): q, o [batch, q_heads, n_q, 128] (or without
     the batch dimension), lse [batch, q_heads, n_q] fp32 or None."""
     import torch
-    at = torch.cuda.current_device()
-    batch, q_heads, n_q = cache._batch(at, q, None, lens, "q")
-    assert _on(at, o, torch.bfloat16, "o").shape == q.shape
+    at, bf16 = torch.cuda.current_device(), torch.bfloat16
+    batch, q_heads, n_q = cache._batch(at, q, bf16, None, lens, torch.int32, "q")
+    assert _on(at, o, bf16, "o").shape == q.shape
     if lse is not None:
         assert _on(at, lse, torch.float32, "lse").numel() == batch * q_heads * n_q
     if ws is not None and ws.get_device() != at:
         raise ValueError("ws is on %s, the current device is cuda:%d" % (ws.device, at))
-    scale = 128 ** -0.5 if scale is None else scale
-    _check(_load().vs_cache_attend(q.data_ptr(), cache._ref, batch, q_heads, n_q, _ptr(lens), max_n, scale, o.data_ptr(), _ptr(lse), _ptr(ws),
-                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "vs_cache_attend")
+    _check((_lib or _load()).vs_cache_attend(q.data_ptr(), cache._ref, batch, q_heads, n_q, _ptr(lens), max_n, 128 ** -0.5 if scale is None else scale,
+                                             o.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream, at)),
+           "vs_cache_attend")
     return o
