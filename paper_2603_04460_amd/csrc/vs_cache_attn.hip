@@ -44,18 +44,20 @@ struct Block {
     uint4 k[4], v[4];
     uint32_t ks;
     uint4 vs[FOLD ? 1 : 4];
+    uint32_t any[FOLD ? 0 : 1];                            // four of V's scales, all of the block's over the wavefront
 };
 
 // lane's offsets into a block: beside a block's address, the same for the wavefront, they are all that a load needs
 template <bool FOLD>
 struct Offsets {
-    uint32_t k, v, ks, vs;
+    uint32_t k, v, ks, vs, any;
     __device__ __forceinline__ explicit Offsets(int lane) {
         const uint32_t c = lane >> 4, m = lane & 15;
         k = 64 * m + 16 * c;
         v = kVCodes + 16 * lane;
         ks = kKScales + 4 * lane;
         vs = kVScales + 64 * c + (FOLD ? 16 * (m & 3) : 0);
+        any = kVScales + 4 * lane;
     }
 };
 
@@ -68,6 +70,18 @@ __device__ __forceinline__ void load_block(Block<FOLD>& x, const uint8_t* at, co
     x.ks = *reinterpret_cast<const uint32_t*>(at + off.ks);
 #pragma unroll
     for (int g = 0; g < (FOLD ? 1 : 4); ++g) x.vs[g] = *reinterpret_cast<const uint4*>(at + off.vs + 16 * g);
+    if (!FOLD) x.any[0] = *reinterpret_cast<const uint32_t*>(at + off.any);
+}
+
+// A pair of bf16 weights times 2^(e - 127), e bytes 0, 1 or 2, 3 of a word of scales: the bytes are added to the exponents, both halves of the word at once,
+// and what falls below the smallest number becomes zero.  A weight of zero counts as 2^-127, like any other below fp32's normal numbers
+// nothing beside the row's largest, which is 2^-8 at least.  Not for the byte 255, and for small ones, where weights that count would be
+// lost, neither.
+__device__ __forceinline__ uint32_t scaled_pair(uint32_t weights, uint32_t e, int high) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const uint32_t exponents = __builtin_amdgcn_perm(e, e, high ? 0x030c020cu : 0x010c000cu) >> 1;
+    const u16x2 up = __builtin_bit_cast(u16x2, weights) + __builtin_bit_cast(u16x2, exponents);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(up, u16x2{0x3f80, 0x3f80}));
 }
 
 // What a wavefront knows of its query rows (FOLD: four, else 16) and keeps of the keys so far.
@@ -145,23 +159,39 @@ struct Rows {
         sum = (part[0] + part[1]) + (part[2] + part[3]);
 
         bf16x8 w[2];
+        uint32_t pair[8];                                  // 16 rows: the weights as they are, keys 2 i and 2 i + 1 of the lane's 16
+        bool plain = true;
+        if (!FOLD) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pair[i] = pack_bf16(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
+            // no scale byte is 255 (a byte of ~e would be zero) or below 40
+            const uint32_t e = x.any[0];
+            plain = !__any(((((0xfefefefeu - e) & e) | ((e - 0x28282828u) & ~e)) & 0x80808080u) != 0);
+        }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             if (!FOLD || g == 0) {
                 const uint32_t e[4] = {x.vs[FOLD ? 0 : g].x, x.vs[FOLD ? 0 : g].y, x.vs[FOLD ? 0 : g].z, x.vs[FOLD ? 0 : g].w};
+                uint32_t y[8];
+                if (FOLD || !plain) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    float y[8];
+                    for (int i = 0; i < 8; ++i)
+                        y[i] = pack_bf16(s[i >> 1][2 * (i & 1)] * scale_of(e[i >> 1], 2 * (i & 1)), s[i >> 1][2 * (i & 1) + 1] * scale_of(e[i >> 1], 2 * (i & 1) + 1));
+                } else {
 #pragma unroll
-                    for (int a = 0; a < 8; ++a) y[a] = s[2 * u + (a >> 2)][a & 3] * scale_of(e[2 * u + (a >> 2)], a & 3);
-                    if (edge) {                            // a key that the row does not see has whatever scale the memory holds
-#pragma unroll
-                        for (int a = 0; a < 8; ++a)
-                            if (key + 16 * (2 * u + (a >> 2)) + 4 * c + (a & 3) > limit) y[a] = 0.0f;
-                        asm volatile("" ::: "memory");
-                    }
-                    w[u] = operand(make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])));
+                    for (int i = 0; i < 8; ++i) y[i] = scaled_pair(pair[i], e[i >> 1], i & 1);
                 }
+                if (edge) {                                // a key that the row does not see has whatever scale the memory holds
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int at = key + 16 * (i >> 1) + 4 * c + 2 * (i & 1);
+                        if (at > limit) y[i] = 0;
+                        if (at + 1 > limit) y[i] &= 0xffffu;
+                    }
+                    asm volatile("" ::: "memory");
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) w[u] = operand(make_uint4(y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]));
             }
             const uint32_t v[4] = {x.v[g].x, x.v[g].y, x.v[g].z, x.v[g].w};
 #pragma unroll
