@@ -22,6 +22,8 @@ EXTRA_FLAGS = {
     "vs_dense.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     # the same: 280 fewer register copies per 32-token block
     "vs_train.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    # score and output accumulators in the registers that the conversions and the softmax use
+    "vs_cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "vs_cache_tile.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 

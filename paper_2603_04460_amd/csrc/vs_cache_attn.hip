@@ -107,7 +107,9 @@ struct Rows {
         for (int j = 0; j < 8; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    // 64 keys from position `key` on; edge: some row does not see all of them
+    // 64 keys from position `key` on; edge: some row does not see all of them.  STRAIGHT: the second products of an ordinary block without
+    // branches between them, for more registers.
+    template <bool STRAIGHT>
     __device__ __forceinline__ void take(const AttendParams& p, const Block<FOLD>& x, int lane, int key, bool edge) {
         const int c = lane >> 4;
         f32x4 s[4];
@@ -158,7 +160,6 @@ struct Rows {
             }
         sum = (part[0] + part[1]) + (part[2] + part[3]);
 
-        bf16x8 w[2];
         uint32_t pair[8];                                  // 16 rows: the weights as they are, keys 2 i and 2 i + 1 of the lane's 16
         bool plain = true;
         if (!FOLD) {
@@ -168,38 +169,45 @@ struct Rows {
             const uint32_t e = x.any[0];
             plain = !__any(((((0xfefefefeu - e) & e) | ((e - 0x28282828u) & ~e)) & 0x80808080u) != 0);
         }
+        // kind 0: every row sees every key and no scale is out of the ordinary, 1: not so, 2: as it turns out
+        auto products = [&](auto kind) __attribute__((always_inline)) {
+            bf16x8 w[2];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            if (!FOLD || g == 0) {
-                const uint32_t e[4] = {x.vs[FOLD ? 0 : g].x, x.vs[FOLD ? 0 : g].y, x.vs[FOLD ? 0 : g].z, x.vs[FOLD ? 0 : g].w};
-                uint32_t y[8];
-                if (FOLD || !plain) {
+            for (int g = 0; g < 4; ++g) {
+                if (!FOLD || g == 0) {
+                    const uint32_t e[4] = {x.vs[FOLD ? 0 : g].x, x.vs[FOLD ? 0 : g].y, x.vs[FOLD ? 0 : g].z, x.vs[FOLD ? 0 : g].w};
+                    uint32_t y[8];
+                    if (!FOLD && (kind == 0 || (kind == 2 && plain))) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        y[i] = pack_bf16(s[i >> 1][2 * (i & 1)] * scale_of(e[i >> 1], 2 * (i & 1)), s[i >> 1][2 * (i & 1) + 1] * scale_of(e[i >> 1], 2 * (i & 1) + 1));
-                } else {
+                        for (int i = 0; i < 8; ++i) y[i] = scaled_pair(pair[i], e[i >> 1], i & 1);
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = scaled_pair(pair[i], e[i >> 1], i & 1);
-                }
-                if (edge) {                                // a key that the row does not see has whatever scale the memory holds
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int at = key + 16 * (i >> 1) + 4 * c + 2 * (i & 1);
-                        if (at > limit) y[i] = 0;
-                        if (at + 1 > limit) y[i] &= 0xffffu;
+                        for (int i = 0; i < 8; ++i)
+                            y[i] = pack_bf16(s[i >> 1][2 * (i & 1)] * scale_of(e[i >> 1], 2 * (i & 1)),
+                                             s[i >> 1][2 * (i & 1) + 1] * scale_of(e[i >> 1], 2 * (i & 1) + 1));
                     }
-                    asm volatile("" ::: "memory");
+                    if (kind == 1 || (kind == 2 && edge)) {    // a key that the row does not see has whatever scale the memory holds
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int at = key + 16 * (i >> 1) + 4 * c + 2 * (i & 1);
+                            if (at > limit) y[i] = 0;
+                            if (at + 1 > limit) y[i] &= 0xffffu;
+                        }
+                        asm volatile("" ::: "memory");
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) w[u] = operand(make_uint4(y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]));
                 }
+                const uint32_t v[4] = {x.v[g].x, x.v[g].y, x.v[g].z, x.v[g].w};
 #pragma unroll
-                for (int u = 0; u < 2; ++u) w[u] = operand(make_uint4(y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]));
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        o[2 * g + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(dequantise8(v[2 * half + u], 1.0f)), w[u], o[2 * g + half], 0, 0, 0);
             }
-            const uint32_t v[4] = {x.v[g].x, x.v[g].y, x.v[g].z, x.v[g].w};
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    o[2 * g + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(dequantise8(v[2 * half + u], 1.0f)), w[u], o[2 * g + half], 0, 0, 0);
-        }
+        };
+        if (STRAIGHT && plain && !edge) products(std::integral_constant<int, 0>{});
+        else products(std::integral_constant<int, STRAIGHT ? 1 : 2>{});
     }
 
     // output tile j of those that count in this lane
@@ -244,7 +252,7 @@ __global__ __launch_bounds__(64 * kHeadWaves) void attend_head_kernel(AttendPara
     };
     auto take = [&](const Block<FOLD>& x, int i, bool there) __attribute__((always_inline)) {
         const int key = there ? i * kBlock : kNowhere;
-        rows.take(p, x, lane, key, key + kBlock - 1 > len - p.n_q);
+        rows.template take<false>(p, x, lane, key, key + kBlock - 1 > len - p.n_q);
     };
     if (wave < last) {
         bool there0, there1, there2;
@@ -298,7 +306,7 @@ __global__ __launch_bounds__(64 * kHeadWaves) void attend_head_kernel(AttendPara
 
 // Every wavefront by itself takes `chunk` consecutive blocks of the row of all blocks, from one head and sequence to the next.
 template <bool FOLD>
-__global__ __launch_bounds__(256, 2) void attend_row_kernel(AttendParams p) {
+__global__ __launch_bounds__(256, FOLD ? 2 : 1) void attend_row_kernel(AttendParams p) {
     using R = Rows<FOLD>;
     const int lane = threadIdx.x & 63;
     const int share = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
@@ -374,7 +382,7 @@ __global__ __launch_bounds__(256, 2) void attend_row_kernel(AttendParams p) {
             rows.begin(p, lane, unit, y.len);
             __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): behind the branch nothing is in flight that it would have to wait for
         }
-        rows.take(p, y.x, lane, y.key, y.key + kBlock - 1 > y.len - p.n_q);
+        rows.template take<!FOLD>(p, y.x, lane, y.key, y.key + kBlock - 1 > y.len - p.n_q);
         upto = y.block + 1;
     };
 
