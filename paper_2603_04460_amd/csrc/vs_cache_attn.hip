@@ -373,15 +373,16 @@ __global__ __launch_bounds__(256, FOLD ? 2 : 1) void attend_row_kernel(AttendPar
         }
     };
     int len_at = 0, upto = 0;
+    // in front of the request for a later block, so that waiting for the rows is no wait for that block
+    auto enter = [&](const Held& y) __attribute__((always_inline)) {
+        if (y.unit == unit) return;
+        if (unit >= 0) finish(len_at, upto);
+        unit = y.unit;
+        from = y.block;
+        len_at = y.len;
+        rows.begin(p, lane, unit, y.len);
+    };
     auto take = [&](const Held& y) __attribute__((always_inline)) {
-        if (y.unit != unit) {
-            if (unit >= 0) finish(len_at, upto);
-            unit = y.unit;
-            from = y.block;
-            len_at = y.len;
-            rows.begin(p, lane, unit, y.len);
-            __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): behind the branch nothing is in flight that it would have to wait for
-        }
         rows.template take<!FOLD>(p, y.x, lane, y.key, y.key + kBlock - 1 > y.len - p.n_q);
         upto = y.block + 1;
     };
@@ -391,11 +392,15 @@ __global__ __launch_bounds__(256, FOLD ? 2 : 1) void attend_row_kernel(AttendPar
     static_for<kDepth - 1>([&](auto k) __attribute__((always_inline)) { fetch(ring[k]); });
     for (; left >= kDepth; left -= kDepth)
         static_for<kDepth>([&](auto k) __attribute__((always_inline)) {
+            enter(ring[k]);
             fetch(ring[(k + kDepth - 1) % kDepth]);
             take(ring[k]);
         });
     static_for<kDepth - 1>([&](auto k) __attribute__((always_inline)) {
-        if (k < left) take(ring[k]);
+        if (k < left) {
+            enter(ring[k]);
+            take(ring[k]);
+        }
     });
     finish(len_at, upto);
 }
