@@ -337,7 +337,7 @@ int vs_rope_frequencies(double theta_base, int rot_dim, int scaling, double fact
  *               computed like the others)
  *   q_out [batch, q_heads, rows, 128], k_out, v_out [batch, kv_heads, rows, 128] bf16.  An output may be its own input where both
  *               have the same layout; otherwise they must not overlap.
- *   eps         > 0 (ignored without w_q and w_k)
+ *   eps         FLT_MIN .. 1 (ignored without w_q and w_k);  pos0 + rows at most 2^31
  * Arithmetic: angles reduced in fp64, sine, cosine, norm and rotation in fp32, one rounding to bf16.
  */
 int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_rows_t* v, int batch, int64_t rows, int q_heads, int kv_heads,
@@ -393,7 +393,8 @@ int vs_cache_read(const vs_cache_t* cache, int batch, int64_t rows, const int32_
  * A row without a key (negative position, idle slot, missing pages only) gives zeros and lse = -inf.  Longer chunks: vs_cache_read, then
  * vs_sparse_prefill_chunk or vs_dense_prefill_chunk.
  * Arithmetic: K and V are exact in bf16; bf16 MFMA, fp32 accumulation and softmax, P rounded to bf16.  The same call always gives
- * the same bits.  Workspace: vs_cache_attend_workspace; the answer for max_n is enough for every smaller max_n of the same call.
+ * the same bits.  A score has to lie within fp32's range, and so do sums of V times weights of up to 2^8 (they do for |V| < 2^96).
+ * At most 2^24 - 1 rows in a call (batch * q_heads * n_q).  Workspace: vs_cache_attend_workspace; the answer for max_n is enough for every smaller max_n of the same call.
  */
 #define VS_CACHE_MAX_NEW 128
 size_t vs_cache_attend_workspace(int batch, int q_heads, int kv_heads, int n_q, int64_t max_n);

@@ -17,7 +17,7 @@ struct AttendParams {
     int shares;                    // workers (workgroups or wavefronts) that divide the blocks among them; 0: one for each head
     int least;                     // blocks of a worker at least
     int items;                     // room in part: shares + sequences x KV heads
-    float c;                       // scale * log2(e)
+    float c, inverse_c;            // scale * log2(e), 1 / c
 };
 
 // many query rows of a KV head (vs_cache_tile.hip): a workgroup has eight wavefronts of 32 rows, `groups` workgroups all rows
@@ -33,6 +33,7 @@ using vs::AttendParams;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kStale = 8.0f;                             // log2 units by which a score may exceed the running maximum
+constexpr float kLarge = 16777216.0f;                      // 2^24: from here on a score's rounding, times log2(e) and scale, is a unit and more
 constexpr int kMaxParts = 256;                             // shares of one sequence and KV head: the threads of the joining kernel
 
 // Scale byte i of a word as a number.  The lowest bit of the fraction makes the byte 255 a NaN instead of an infinity and is

@@ -75,8 +75,8 @@ __device__ __forceinline__ void load_block(Block<FOLD>& x, const uint8_t* at, co
 
 // A pair of bf16 weights times 2^(e - 127), e bytes 0, 1 or 2, 3 of a word of scales: the bytes are added to the exponents, both halves of the word at once,
 // and what falls below the smallest number becomes zero.  A weight of zero counts as 2^-127, like any other below fp32's normal numbers
-// nothing beside the row's largest, which is 2^-8 at least.  Not for the byte 255, and for small ones, where weights that count would be
-// lost, neither.
+// nothing beside the row's largest, which is 2^-8 at least.  Not for the byte 255, nor for ones whose sum with a weight of 2^8 would carry into
+// the sign, nor for small ones, where weights that count would be lost.
 __device__ __forceinline__ uint32_t scaled_pair(uint32_t weights, uint32_t e, int high) {
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     const uint32_t exponents = __builtin_amdgcn_perm(e, e, high ? 0x030c020cu : 0x010c000cu) >> 1;
@@ -92,6 +92,8 @@ struct Rows {
     int row, limit;                                        // of the lane's column; last key that the row sees
     f32x4 o[8];
     float top, sum;
+    float less;                                            // top, or 0 where it is taken off the scores before their weights are evaluated
+    bool large;                                            // some column's running maximum is past kLarge
 
     __device__ __forceinline__ void begin(const AttendParams& p, int lane, int unit, int len) {
         const int n = lane & 15, c = lane >> 4;
@@ -101,8 +103,9 @@ struct Rows {
         const uint16_t* from = p.q + (static_cast<int64_t>(unit) * p.rows + r) * 128 + 32 * c;
 #pragma unroll
         for (int j = 0; j < 4; ++j) q[j] = operand(*reinterpret_cast<const uint4*>(from + 8 * j));
-        top = -FLT_MAX;
+        top = less = -FLT_MAX;
         sum = 0.0f;
+        large = false;
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
@@ -142,20 +145,29 @@ struct Rows {
         float m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * p.c;
         // The maximum may be exceeded by 2^8: weights relative to a stale one are as exact, and the search across lanes and the rescaling are
         // left out for most blocks.
-        if (__any(m > top + kStale)) {
+        if (large || __any(m > top + kStale)) {
             m = fmaxf(top, column_reduce(m, [](float u, float v) { return fmaxf(u, v); }));
             const float f = __builtin_amdgcn_exp2f(top - m);
             sum *= f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] *= f;
             top = m;
+            large = __any(fabsf(m) > kLarge && m > -FLT_MAX);
+            less = top;
+            if (large) {                                   // (the row's largest weight is to be 1)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[t][e] = (s[t][e] * p.c - top) * p.inverse_c;
+                less = 0.0f;
+            }
         }
         float part[4] = {sum, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], p.c, -top));
+                s[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], p.c, -less));
                 part[t] += s[t][e];
             }
         sum = (part[0] + part[1]) + (part[2] + part[3]);
@@ -165,9 +177,9 @@ struct Rows {
         if (!FOLD) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) pair[i] = pack_bf16(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
-            // no scale byte is 255 (a byte of ~e would be zero) or below 40
+            // no scale byte is above 240 or below 40
             const uint32_t e = x.any[0];
-            plain = !__any(((((0xfefefefeu - e) & e) | ((e - 0x28282828u) & ~e)) & 0x80808080u) != 0);
+            plain = !__any(((((0xf0f0f0f0u - e) & e) | ((e - 0x28282828u) & ~e)) & 0x80808080u) != 0);
         }
         // kind 0: every row sees every key and no scale is out of the ordinary, 1: not so, 2: as it turns out
         auto products = [&](auto kind) __attribute__((always_inline)) {
@@ -503,7 +515,7 @@ Plan plan(int64_t units, int rows, int64_t max_n) {
     x.many = x.shares && rows > 72 && units * blocks * tile_groups >= 12 * 256;
     if (x.many) {
         x.groups = tile_groups;
-        x.shares = 256 / tile_groups < 1 ? 1 : 256 / tile_groups;
+        x.shares = 256 / tile_groups < 4 ? 4 : 256 / tile_groups;     // (no fewer than above: shorter sequences need no larger workspace)
     }
     x.items = x.shares ? units + x.shares : units;
     return x;
@@ -525,14 +537,16 @@ extern "C" size_t vs_cache_attend_workspace(int batch, int q_heads, int kv_heads
 extern "C" int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch, int q_heads, int n_q, const int32_t* lens, int64_t max_n,
                                float scale, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
     if (!q || !o || !vs::aligned16(q) || !vs::aligned16(o) || !vs::aligned16(lse) || !vs::aligned16(ws)) return VS_ERR_INVALID_ARG;
-    if (q_heads <= 0 || n_q <= 0 || !(scale > 0.0f) || !(scale < INFINITY)) return VS_ERR_INVALID_ARG;
     AttendParams p;
+    p.c = scale * 1.44269504088896340736f;
+    p.inverse_c = 1.0f / p.c;
+    if (q_heads <= 0 || n_q <= 0 || !(scale > 0.0f) || !(p.c < INFINITY)) return VS_ERR_INVALID_ARG;
     const int rc = vs::cache_params(cache, batch, lens, max_n, &p.cache);
     if (rc != VS_OK) return rc;
     if (!sizes_ok(batch, q_heads, cache->kv_heads, n_q, max_n)) return VS_ERR_UNSUPPORTED;
     const int64_t units = static_cast<int64_t>(batch) * cache->kv_heads;
     p.rows = q_heads / cache->kv_heads * n_q;
-    if (units * p.rows > (1 << 26)) return VS_ERR_UNSUPPORTED;
+    if (units * p.rows >= 1 << 24) return VS_ERR_UNSUPPORTED;     // threads of the joining kernel: 256 a row, 32 bits
     const Plan x = plan(units, p.rows, max_n);
     if (x.shares && (!ws || ws_bytes < vs_cache_attend_workspace(batch, q_heads, cache->kv_heads, n_q, max_n))) return VS_ERR_WORKSPACE;
     p.q = static_cast<const uint16_t*>(q);
@@ -544,7 +558,6 @@ extern "C" int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch
     p.shares = x.shares;
     p.least = x.least;
     p.items = static_cast<int>(x.items);
-    p.c = scale * 1.44269504088896340736f;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (!x.shares) {
         hipLaunchKernelGGL(x.fold ? attend_head_kernel<true> : attend_head_kernel<false>, dim3(static_cast<unsigned>(units), x.groups),

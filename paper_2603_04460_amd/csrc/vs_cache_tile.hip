@@ -140,7 +140,8 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
 
     bf16x8 q[8];
     f32x16 o[4];
-    float top = -FLT_MAX, sum = 0.0f;
+    float top = -FLT_MAX, less = -FLT_MAX, sum = 0.0f;     // less: top, or 0 where it is taken off before
+    bool large = false;                                    // some row's running maximum is past kLarge
     int limit = -1, unit = -1, from_block = 0;             // last key that the row sees; head at work, its first block here
     auto begin = [&](const Tag& y) __attribute__((always_inline)) {
         unit = y.unit;
@@ -150,7 +151,8 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
         const uint16_t* from = p.q + (static_cast<int64_t>(unit) * p.rows + r) * 128 + 8 * half;
 #pragma unroll
         for (int j = 0; j < 8; ++j) q[j] = operand(*reinterpret_cast<const uint4*>(from + 16 * j));
-        top = -FLT_MAX;
+        top = less = -FLT_MAX;
+        large = false;
         sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -216,13 +218,22 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
             for (int i = 0; i < 8; ++i) most[k] = fmaxf(most[k], s[k >> 1][8 * (k & 1) + i]);
         }
         float m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * p.c;
-        if (__any(m > top + kStale)) {                     // the maximum may be exceeded by 2^8, as in the kernels for few rows
+        if (large || __any(m > top + kStale)) {                     // the maximum may be exceeded by 2^8, as in the kernels for few rows
             m = fmaxf(top, half_reduce_max(m));
             const float f = __builtin_amdgcn_exp2f(top - m);
             sum *= f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[j] *= f;
             top = m;
+            large = __any(fabsf(m) > kLarge && m > -FLT_MAX);
+            less = top;
+            if (large) {                                   // (the row's largest weight is to be 1)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[t][i] = (s[t][i] * p.c - top) * p.inverse_c;
+                less = 0.0f;
+            }
         }
         float part[4] = {sum, 0.0f, 0.0f, 0.0f};
         bf16x8 w[4];
@@ -231,8 +242,8 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
             uint32_t word[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float a = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][8 * (k & 1) + 2 * i], p.c, -top));
-                const float b = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][8 * (k & 1) + 2 * i + 1], p.c, -top));
+                const float a = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][8 * (k & 1) + 2 * i], p.c, -less));
+                const float b = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][8 * (k & 1) + 2 * i + 1], p.c, -less));
                 part[k] += a + b;
                 word[i] = pack_bf16(a, b);
             }

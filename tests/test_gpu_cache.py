@@ -298,6 +298,33 @@ def test_attend_large_scores_and_scale():
         check(*call(c, q, lens, n, scale=scale), q, k, v, lens, scale=scale or 128 ** -0.5)
 
 
+@pytest.mark.parametrize("hq, hk, n_q, n", [(4, 1, 1, 900), (4, 1, 5, 900), (8, 2, 1, 20001), (8, 2, 5, 20001), (8, 8, 100, 30001)])
+def test_attend_scores_whose_rounding_exceeds_a_unit(hq, hk, n_q, n):
+    """Scores of 2^35 and more, whose last place is 2^11: one key has a score a half above all others (their sums are good to 128 roundings,
+    2^-17), so it has all of the weight and the output is its value; rows of ordinary size beside them stay what they are."""
+    g = torch.Generator().manual_seed(n_q)
+    size = torch.tensor([0.5, 1.0, 1.5, 2.0, 3.0, 4.0])[torch.randint(0, 6, (1, hk, n), generator=g)]
+    peak = n // 3
+    size[:, :, peak] = 6.0
+    size[:, :, n - 1] = 12.0                                # the last row's
+    k = (size * 2.0 ** 13).unsqueeze(3).expand(1, hk, n, 128).bfloat16().cuda().contiguous()
+    c, _, _, v, _ = attend_case(65, hq, hk, n_q, [n], 64, k=k)
+    q = (2.0 ** 15 * (1 + torch.rand(1, hq, n_q, 128, generator=g))).bfloat16()
+    q[:, 1::2] *= 2.0 ** -33
+    q = q.cuda()
+    o, lse = call(c, q, [n], n)
+    for head in range(0, hq, 2):
+        h = head * hk // hq
+        vv = plain.values(*plain.quantise(f64(v[0, h])))
+        for r in range(n_q):
+            at = n - 1 if r == n_q - 1 else peak
+            # weights of zero may count as 2^-126 (see check); a value of three bits keeps its bits beside that
+            assert (np.abs(f64(o[0, head, r]) - vv[at]) <= 2.0 ** -126 * n * np.abs(vv).max()).all(), (head, r)
+            want = f64(q[0, head, r]).sum() * float(k[0, h, at, 0]) * 128 ** -0.5
+            assert abs(float(lse[0, head, r]) - want) <= 2.0 ** -16 * want, (head, r)
+    check(o, lse, q, k, v, [n], heads=range(min(hk, 2)))     # (its bound for a large row allows anything)
+
+
 def test_attend_rising_maximum():
     """Every block has a larger score than the ones before it, and the other way round."""
     n = 1500

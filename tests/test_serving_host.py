@@ -124,6 +124,27 @@ def test_workspace_for_the_longest_sequence(batch, hq, hk, n_q):
     assert all(a <= b for a, b in zip(sizes, sizes[1:]))
 
 
+@pytest.mark.parametrize("hq, n_q", [(150, 128), (256, 64), (513, 128), (4096, 128)])
+def test_workspace_of_ten_thousand_rows(hq, n_q):
+    """So many rows that a workgroup's share of them is all of the call: the largest sequence's workspace serves the shorter ones, too."""
+    sizes = [vs.cache_attend_workspace(1, hq, 1, n_q, n) for n in sorted({1 << i for i in range(21)} | {600, 2000, 2300, 5000, 12345, 131000})]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[-1] > 0
+
+
+def test_largest_calls(p):
+    """Sizes behind which a launch or a value would leave 32 bits are refused, whatever memory there is."""
+    L = binding._load()
+    many = ctypes.byref(cache(p, kv_heads=1, max_pages=4, pages=1 << 20, table=p))
+    attend = lambda batch, hq, n_q, scale=0.1: L.vs_cache_attend(p, many, batch, hq, n_q, None, 100, scale, p, None, p, 1 << 60, None)
+    assert attend(32, 4096, 128) == -2 and attend(1 << 12, 32, 128) == -2
+    assert attend(1, 1, 1, scale=3e38) == -1                # scale * log2(e) is past fp32
+    t = binding._Rotation(p, 128, 0, 1.0)
+    x = ctypes.byref(binding._Rows(p, 128, 128))
+    norm = lambda eps=1e-6, pos0=0, rows=4: L.vs_qk_norm_rope(x, x, None, 1, rows, 1, 1, p, p, eps, ctypes.byref(t), None, pos0, p, p, None, None)
+    assert norm(pos0=(1 << 31) - 3) == -2 and norm(pos0=1 << 62) == -2
+    assert norm(eps=1e-39) == -1 and norm(eps=1.5) == -1
+
+
 def test_plain_cache():
     """The plain form itself: its codes stand for the nearest numbers, a block's bytes hold every token once."""
     rng = np.random.default_rng(5)
