@@ -11,6 +11,7 @@
 // A head's row costs a norm and four products a plane: the weights are folded into the angles' sines and cosines.
 // Bound by the memory: every element is read and written once.  131072 positions of 32 / 8 heads 675 us (4.8 TB/s; a large copy reaches 5.1),
 // with one row's loads in flight, weights apart and all parts in one loop 860.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -213,7 +214,7 @@ extern "C" int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_
     if (batch <= 0 || rows <= 0 || q_heads <= 0 || kv_heads <= 0 || pos0 < 0) return VS_ERR_INVALID_ARG;
     if (!vs::aligned16(q_out) || !vs::aligned16(k_out) || !vs::aligned16(v_out) || !vs::aligned16(w_q) || !vs::aligned16(w_k) ||
         !vs::aligned4(lens)) return VS_ERR_INVALID_ARG;
-    if ((w_q || w_k) && (!(eps > 0.0f) || !isfinite(eps))) return VS_ERR_INVALID_ARG;
+    if ((w_q || w_k) && !(eps >= FLT_MIN && eps <= 1.0f)) return VS_ERR_INVALID_ARG;
     if (!rotation->freq || !vs::aligned16(rotation->freq) || !isfinite(rotation->magnitude)) return VS_ERR_INVALID_ARG;
     if (rotation->pairing != 0 && rotation->pairing != 1) return VS_ERR_INVALID_ARG;
     const vs_rows_t* in[3] = {q, k, v};
@@ -223,6 +224,7 @@ extern "C" int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_
         if (x->token_stride % 8 || x->head_stride % 8) return VS_ERR_INVALID_ARG;
     }
     if (rotation->rot_dim < 8 || rotation->rot_dim > VS_HEAD_DIM || rotation->rot_dim % 8) return VS_ERR_UNSUPPORTED;
+    if (pos0 > (1ll << 31) - rows) return VS_ERR_UNSUPPORTED;      // an angle's fraction of a turn keeps 2^-24
     if (rows > VS_MAX_SEQ || batch > 65535 || static_cast<int64_t>(batch) * rows > (1 << 26) || q_heads > 4096 || kv_heads > 4096) return VS_ERR_UNSUPPORTED;
 
     NormRopeParams p;
@@ -247,7 +249,7 @@ extern "C" int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_
     p.magnitude = rotation->magnitude;
     p.eps = eps;
     const unsigned blocks = (p.tokens + kPositions - 1) / kPositions;
-        // Short calls: the heads are shared out over about two workgroups per compute unit, whole batches of heads together; every
+    // Short calls: the heads are shared out over about two workgroups per compute unit, whole batches of heads together; every
     // workgroup evaluates the angles of its positions.  One workgroup over all heads / shared out: 16 x 1 position, 32 / 8 heads 33.6 / 4.2 us,
     // 4099 positions 92 / 22.7 (2048 workgroups 23.7, 8192 26.0), 131072 positions the same.
     unsigned groups = 0;
