@@ -6,7 +6,9 @@
 //   O^T = V^T P^T (channels x query rows): the lane that holds scores 4 c .. 4 c + 3 of a column holds the weights that the second
 //                 product wants from it, nothing moves between lanes.
 // A word of V codes is eight keys of one channel and each key has its own scale, so V's scales go to the weights instead: P times
-// the scale (a power of two: no rounding besides P's own to bf16), one set per 32 channels.
+// the scale (a power of two: no rounding besides P's own to bf16), one set per 32 channels.  As exponents of bf16 numbers that is a subtraction for two
+// weights, of words that the wavefront makes in LDS once a block (five tokens of four sequences of 20011 22.9 -> 20.3 us against words made by every
+// lane for itself, 16 rows of 131072 39 -> 36, 64 rows of 32768 30 -> 26).
 //   up to four query rows of a KV head (FOLD): the 16 columns are four rows x four channel groups; every column has its group's
 //     weights, and of each output tile the columns of its group count
 //   more: 16 rows a tile, four sets of weights
@@ -39,49 +41,80 @@ __device__ __forceinline__ float column_reduce(float x, F op) {
     return op(__builtin_bit_cast(float, q0), __builtin_bit_cast(float, q1));
 }
 
-template <bool FOLD>
 struct Block {
     uint4 k[4], v[4];
-    uint32_t ks;
-    uint4 vs[FOLD ? 1 : 4];
-    uint32_t any[FOLD ? 0 : 1];                            // four of V's scales, all of the block's over the wavefront
+    uint32_t ks, vs;                                       // four scales each, all of the block's over the wavefront
 };
 
 // lane's offsets into a block: beside a block's address, the same for the wavefront, they are all that a load needs
-template <bool FOLD>
 struct Offsets {
-    uint32_t k, v, ks, vs, any;
+    uint32_t k, v, ks, vs;
     __device__ __forceinline__ explicit Offsets(int lane) {
         const uint32_t c = lane >> 4, m = lane & 15;
         k = 64 * m + 16 * c;
         v = kVCodes + 16 * lane;
         ks = kKScales + 4 * lane;
-        vs = kVScales + 64 * c + (FOLD ? 16 * (m & 3) : 0);
-        any = kVScales + 4 * lane;
+        vs = kVScales + 4 * lane;
     }
 };
 
-template <bool FOLD>
-__device__ __forceinline__ void load_block(Block<FOLD>& x, const uint8_t* at, const Offsets<FOLD>& off) {
+__device__ __forceinline__ void load_block(Block& x, const uint8_t* at, const Offsets& off) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) x.k[t] = *reinterpret_cast<const uint4*>(at + off.k + 1024 * t);
 #pragma unroll
     for (int p = 0; p < 4; ++p) x.v[p] = *reinterpret_cast<const uint4*>(at + off.v + 1024 * p);
     x.ks = *reinterpret_cast<const uint32_t*>(at + off.ks);
-#pragma unroll
-    for (int g = 0; g < (FOLD ? 1 : 4); ++g) x.vs[g] = *reinterpret_cast<const uint4*>(at + off.vs + 16 * g);
-    if (!FOLD) x.any[0] = *reinterpret_cast<const uint32_t*>(at + off.any);
+    x.vs = *reinterpret_cast<const uint32_t*>(at + off.vs);
 }
 
-// A pair of bf16 weights times 2^(e - 127), e bytes 0, 1 or 2, 3 of a word of scales: the bytes are added to the exponents, both halves of the word at once,
-// and what falls below the smallest number becomes zero.  A weight of zero counts as 2^-127, like any other below fp32's normal numbers
-// nothing beside the row's largest, which is 2^-8 at least.  Not for the byte 255, nor for ones whose sum with a weight of 2^8 would carry into
-// the sign, nor for small ones, where weights that count would be lost.
-__device__ __forceinline__ uint32_t scaled_pair(uint32_t weights, uint32_t e, int high) {
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    const uint32_t exponents = __builtin_amdgcn_perm(e, e, high ? 0x030c020cu : 0x010c000cu) >> 1;
-    const u16x2 up = __builtin_bit_cast(u16x2, weights) + __builtin_bit_cast(u16x2, exponents);
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(up, u16x2{0x3f80, 0x3f80}));
+// V's scales meet the weights as what they take off a bf16 number's exponent: 2^(e - 127) = 2^kRaise 2^-(127 + kRaise - e), where the
+// first factor goes to V.  So a pair of weights takes one subtraction, and the words that are subtracted are the same for all rows: the
+// wavefront makes them once a block, in LDS (word 2 x + i: scales 2 i and 2 i + 1 of the x-th word of V's scales).
+// What falls below the smallest number becomes less than 2^-126: a key loses less than 2^-126 2^kRaise 6 of the sum.  Scales past 2^kRaise
+// and small ones, where that would count, take the way of weights multiplied in fp32.
+constexpr int kRaise = 16;
+constexpr uint32_t kScaleMost = 127 + kRaise, kScaleLeast = 56;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t less_pair(uint32_t a, uint32_t b) {      // a - b in both halves
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(u16x2, a) - __builtin_bit_cast(u16x2, b));
+}
+
+__device__ __forceinline__ uint2 scale_words(uint32_t e) {
+    constexpr uint32_t most = (kScaleMost << 7) * 0x10001u;
+    return make_uint2(less_pair(most, __builtin_amdgcn_perm(e, e, 0x010c000cu) >> 1), less_pair(most, __builtin_amdgcn_perm(e, e, 0x030c020cu) >> 1));
+}
+
+__device__ __forceinline__ uint32_t scaled_pair(uint32_t weights, uint32_t word) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, weights), __builtin_bit_cast(u16x2, word)));
+}
+
+// the same for any scales: the byte 255 is a NaN, by the lowest bit of the fraction
+__device__ __forceinline__ uint32_t scaled_pair_any(float a, float b, uint32_t word) {
+    const uint32_t e = less_pair((kScaleMost << 7) * 0x10001u, word);
+    return pack_bf16(a * __uint_as_float(e << 16 | 1u), b * __uint_as_float((e & 0xffff0000u) | 1u));
+}
+
+// Lane's word of V's scales with those of keys that no row sees (they have no weight, whatever the memory holds) replaced by an ordinary one;
+// `live`: keys of the block that hold a token.
+__device__ __forceinline__ uint32_t live_scales(uint32_t e, int lane, int live) {
+    const int n = live - 16 * (lane & 3) - 4 * (lane >> 4);
+    const uint32_t mine = n <= 0 ? 0u : n >= 4 ? ~0u : (1u << (8 * n)) - 1;
+    return (e & mine) | (0x7f7f7f7fu & ~mine);
+}
+
+// a byte of the word is above kScaleMost, or below kScaleLeast and not 0 (a group of zeros takes any weights)
+__device__ __forceinline__ bool odd_scales(uint32_t e) {
+    const uint32_t low = (e - kScaleLeast * 0x01010101u) & ~e & (((e & 0x7f7f7f7fu) + 0x7f7f7f7fu) | e);
+    return ((((kScaleMost * 0x01010101u - e) & e) | low) & 0x80808080u) != 0;
+}
+
+// all lanes' words of scales to the wavefront's 512 bytes of LDS
+__device__ __forceinline__ void put_scales(uint2* words, uint32_t e, int lane) {
+    words[lane] = scale_words(e);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // What a wavefront knows of its query rows (FOLD: four, else 16) and keeps of the keys so far.
@@ -110,11 +143,10 @@ struct Rows {
         for (int j = 0; j < 8; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    // 64 keys from position `key` on; edge: some row does not see all of them.  STRAIGHT: the second products of an ordinary block without
-    // branches between them, for more registers.
-    template <bool STRAIGHT>
-    __device__ __forceinline__ void take(const AttendParams& p, const Block<FOLD>& x, int lane, int key, bool edge) {
+    // 64 keys from position `key` on; edge: some row does not see all of them
+    __device__ __forceinline__ void take(const AttendParams& p, const Block& x, int lane, int key, bool edge, int len, uint2* words) {
         const int c = lane >> 4;
+        put_scales(words, x.vs, lane);
         f32x4 s[4];
         float scale[4];
         uint32_t word[4][4];
@@ -172,40 +204,43 @@ struct Rows {
             }
         sum = (part[0] + part[1]) + (part[2] + part[3]);
 
-        uint32_t pair[8];                                  // 16 rows: the weights as they are, keys 2 i and 2 i + 1 of the lane's 16
-        bool plain = true;
-        if (!FOLD) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) pair[i] = pack_bf16(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
-            // no scale byte is above 240 or below 40
-            const uint32_t e = x.any[0];
-            plain = !__any(((((0xf0f0f0f0u - e) & e) | ((e - 0x28282828u) & ~e)) & 0x80808080u) != 0);
+        uint32_t pair[8], scales = x.vs;                   // weights of keys 2 i and 2 i + 1 of the lane's 16
+        if (edge) {
+            scales = live_scales(scales, lane, len - key);
+            asm volatile("" ::: "memory");
         }
-        // kind 0: every row sees every key and no scale is out of the ordinary, 1: not so, 2: as it turns out
-        auto products = [&](auto kind) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pair[i] = pack_bf16(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
+        const bool plain = !__any(odd_scales(scales));
+        // ordinary: no scale is out of the ordinary
+        auto products = [&](auto ordinary) __attribute__((always_inline)) {
             bf16x8 w[2];
+            const uint4* const of = reinterpret_cast<const uint4*>(words) + 8 * c + (FOLD ? 2 * (lane & 3) : 0);
+            uint4 ahead[2] = {of[0], of[1]};               // words of V's scales, requested a step ahead
+            int base = key;
+            asm volatile("" : "+s"(base));                 // (positions of keys are not evaluated before)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 if (!FOLD || g == 0) {
-                    const uint32_t e[4] = {x.vs[FOLD ? 0 : g].x, x.vs[FOLD ? 0 : g].y, x.vs[FOLD ? 0 : g].z, x.vs[FOLD ? 0 : g].w};
-                    uint32_t y[8];
-                    if (!FOLD && (kind == 0 || (kind == 2 && plain))) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] = scaled_pair(pair[i], e[i >> 1], i & 1);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            y[i] = pack_bf16(s[i >> 1][2 * (i & 1)] * scale_of(e[i >> 1], 2 * (i & 1)),
-                                             s[i >> 1][2 * (i & 1) + 1] * scale_of(e[i >> 1], 2 * (i & 1) + 1));
+                    const uint32_t e[8] = {ahead[0].x, ahead[0].y, ahead[0].z, ahead[0].w, ahead[1].x, ahead[1].y, ahead[1].z, ahead[1].w};
+                    if (!FOLD) {
+                        if (g < 3) {
+                            ahead[0] = of[2 * g + 2];
+                            ahead[1] = of[2 * g + 3];
+                        }
+                        __builtin_amdgcn_sched_barrier(0xf);       // (reads stay in front)
                     }
-                    if (kind == 1 || (kind == 2 && edge)) {    // a key that the row does not see has whatever scale the memory holds
+                    uint32_t y[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int at = key + 16 * (i >> 1) + 4 * c + 2 * (i & 1);
+                    for (int i = 0; i < 8; ++i) {
+                        if (ordinary) {
+                            y[i] = scaled_pair(pair[i], e[i]);
+                        } else {                           // a key that the row does not see has whatever scale the memory holds
+                            y[i] = scaled_pair_any(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1], e[i]);
+                            const int at = base + 16 * (i >> 1) + 4 * c + 2 * (i & 1);
                             if (at > limit) y[i] = 0;
                             if (at + 1 > limit) y[i] &= 0xffffu;
                         }
-                        asm volatile("" ::: "memory");
                     }
 #pragma unroll
                     for (int u = 0; u < 2; ++u) w[u] = operand(make_uint4(y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]));
@@ -215,11 +250,12 @@ struct Rows {
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
-                        o[2 * g + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(dequantise8(v[2 * half + u], 1.0f)), w[u], o[2 * g + half], 0, 0, 0);
+                        o[2 * g + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(dequantise8(v[2 * half + u], ordinary ? static_cast<float>(1 << kRaise) : 1.0f)),
+                                                                                 w[u], o[2 * g + half], 0, 0, 0);
             }
         };
-        if (STRAIGHT && plain && !edge) products(std::integral_constant<int, 0>{});
-        else products(std::integral_constant<int, STRAIGHT ? 1 : 2>{});
+        if (plain) products(std::integral_constant<bool, true>{});
+        else products(std::integral_constant<bool, false>{});
     }
 
     // output tile j of those that count in this lane
@@ -247,6 +283,7 @@ __global__ __launch_bounds__(64 * kHeadWaves) void attend_head_kernel(AttendPara
     using R = Rows<FOLD>;
     __shared__ float4 sums[kHeadWaves][R::kKept][64];
     __shared__ float2 stat[kHeadWaves][16];
+    __shared__ __align__(16) uint2 words[kHeadWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int unit = blockIdx.x, b = unit / p.cache.kv_heads, h = unit - b * p.cache.kv_heads;
     const int len = cache_length_scalar(p.cache, b), last = blocks_of(len);
@@ -256,29 +293,29 @@ __global__ __launch_bounds__(64 * kHeadWaves) void attend_head_kernel(AttendPara
     // Two blocks in registers: the next one's loads are in flight while one is worked on, and its address is known before.  Loads and
     // work are unconditional (a branch around them would make the wait for the older loads a wait for all): past the end
     // the last block is fetched again, without a page the begin of the cache, and no row sees it.
-    const Offsets<FOLD> off(lane);
+    const Offsets off(lane);
     auto address = [&](int i, bool* there) __attribute__((always_inline)) {
         const uint8_t* x = cache_block(p.cache, b, h, min(i, last - 1));
         *there = i < last && x;
         return x ? x : p.cache.data;
     };
-    auto take = [&](const Block<FOLD>& x, int i, bool there) __attribute__((always_inline)) {
+    auto take = [&](const Block& x, int i, bool there) __attribute__((always_inline)) {
         const int key = there ? i * kBlock : kNowhere;
-        rows.template take<false>(p, x, lane, key, key + kBlock - 1 > len - p.n_q);
+        rows.take(p, x, lane, key, key + kBlock - 1 > len - p.n_q, len, words[wave]);
     };
     if (wave < last) {
         bool there0, there1, there2;
         const uint8_t *at0 = address(wave, &there0), *at1 = address(wave + kHeadWaves, &there1);
-        Block<FOLD> x0, x1;
-        load_block<FOLD>(x0, at0, off);
+        Block x0, x1;
+        load_block(x0, at0, off);
         for (int block = wave;;) {
             at0 = address(block + 2 * kHeadWaves, &there2);
-            load_block<FOLD>(x1, at1, off);
+            load_block(x1, at1, off);
             take(x0, block, there0);
             there0 = there2;
             if ((block += kHeadWaves) >= last) break;
             at1 = address(block + 2 * kHeadWaves, &there2);
-            load_block<FOLD>(x0, at0, off);
+            load_block(x0, at0, off);
             take(x1, block, there1);
             there1 = there2;
             if ((block += kHeadWaves) >= last) break;
@@ -318,10 +355,11 @@ __global__ __launch_bounds__(64 * kHeadWaves) void attend_head_kernel(AttendPara
 
 // Every wavefront by itself takes `chunk` consecutive blocks of the row of all blocks, from one head and sequence to the next.
 template <bool FOLD>
-__global__ __launch_bounds__(256, FOLD ? 2 : 1) void attend_row_kernel(AttendParams p) {
+__global__ __launch_bounds__(256, 2) void attend_row_kernel(AttendParams p) {
     using R = Rows<FOLD>;
     const int lane = threadIdx.x & 63;
-    const int share = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    __shared__ __align__(16) uint2 words[4][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = blockIdx.x * 4 + wave;
     Place at;
     int left;
     {
@@ -348,16 +386,16 @@ __global__ __launch_bounds__(256, FOLD ? 2 : 1) void attend_row_kernel(AttendPar
     };
     // A block's codes are requested kDepth - 1 blocks ahead, its page one more.  Loads and work are unconditional (a branch around them
     // would make the wait for the older loads a wait for all): without a page the begin of the cache is fetched and no row sees it.
-    const Offsets<FOLD> off(lane);
+    const Offsets off(lane);
     struct Held {
-        Block<FOLD> x;
+        Block x;
         int unit, block, len, key;
     };
     int remain = left, page;
     auto look_up = [&]() __attribute__((always_inline)) { page = cache_page(p.cache, at.b, at.page); };
     auto fetch = [&](Held& y) __attribute__((always_inline)) {
         const bool paged = cache_paged(p.cache, page);
-        load_block<FOLD>(y.x, p.cache.data + (paged ? cache_offset(p.cache, page, at.h, at.in_page) : 0), off);
+        load_block(y.x, p.cache.data + (paged ? cache_offset(p.cache, page, at.h, at.in_page) : 0), off);
         y.unit = at.b * p.cache.kv_heads + at.h;
         y.block = at.block;
         y.len = at.len;
@@ -373,15 +411,15 @@ __global__ __launch_bounds__(256, FOLD ? 2 : 1) void attend_row_kernel(AttendPar
         const float l = rows.total();
         if (rows.row >= p.rows) return;
         const int64_t r = static_cast<int64_t>(unit) * p.rows + rows.row, slot = static_cast<int64_t>(share + unit) * p.rows + rows.row;
+        if (whole) {
 #pragma unroll
-        for (int j = 0; j < R::kKept; ++j) {
-            const float4 y = rows.kept(j, lane);
-            if (whole) put_row(p, r, R::channel(j, lane), y, l);
-            else *reinterpret_cast<float4*>(p.part + slot * 128 + R::channel(j, lane)) = y;
-        }
-        if (R::speaks(lane)) {
-            if (whole) put_lse(p, r, rows.top, l);
-            else part_stat(p)[slot] = make_float2(rows.top, l);
+            for (int j = 0; j < R::kKept; ++j) put_row(p, r, R::channel(j, lane), rows.kept(j, lane), l);
+            if (R::speaks(lane)) put_lse(p, r, rows.top, l);
+        } else {
+            float4* const to = reinterpret_cast<float4*>(p.part + slot * 128 + R::channel(0, lane));
+#pragma unroll
+            for (int j = 0; j < R::kKept; ++j) to[(R::channel(j, 0) - R::channel(0, 0)) / 4] = rows.kept(j, lane);
+            if (R::speaks(lane)) part_stat(p)[slot] = make_float2(rows.top, l);
         }
     };
     int len_at = 0, upto = 0;
@@ -395,7 +433,7 @@ __global__ __launch_bounds__(256, FOLD ? 2 : 1) void attend_row_kernel(AttendPar
         rows.begin(p, lane, unit, y.len);
     };
     auto take = [&](const Held& y) __attribute__((always_inline)) {
-        rows.template take<!FOLD>(p, y.x, lane, y.key, y.key + kBlock - 1 > y.len - p.n_q);
+        rows.take(p, y.x, lane, y.key, y.key + kBlock - 1 > y.len - p.n_q, y.len, words[wave]);
         upto = y.block + 1;
     };
 
@@ -508,11 +546,11 @@ Plan plan(int64_t units, int rows, int64_t max_n) {
     x.shares = by_head ? 0 : 1024 / x.groups < 4 ? 4 : 1024 / x.groups / 4 * 4;
     x.least = static_cast<int>((blocks + kMaxParts - 3) / (kMaxParts - 2));
     // Many rows: every workgroup turns a block into bf16 once for 256 rows; one workgroup on every compute unit, twelve blocks for each at least (its
-    // start and its larger parts cost about as much as six).  16 rows a wavefront / 256 a workgroup, us: 32 / 8 heads, 32768 tokens, 16 new ones (64 rows)
-    // 32.7 / 37.0, 20 41.5 / 38.1, 32 54 / 41, 64 99 / 54, 100 156 / 85, 8 heads, 100 of 30000 48.5 / 41.0; four sequences of 5000, 32 new ones (10 blocks
-    // for each workgroup) 24.9 / 27.7, one head, 128 of 30000 (2) 16.1 / 18.7.
+    // start and its larger parts cost about as much as six).  16 rows a wavefront / 256 a workgroup, us: 32 / 8 heads, 32768 tokens, 32 new ones
+    // (128 rows) 41 / 42, 40 52 / 49, 48 59 / 52, 64 73 / 55, 100 112 / 86; 64 of 24000 56 / 51, of 16000 (8 blocks for each workgroup) 42 / 43, 100 of 16000
+    // 61 / 58, of 10000 (10) 44 / 47; 40 of 131072 171 / 146; four sequences of 8000, 50 new ones 44 / 45; 8 heads, 100 of 30000 37 / 42.
     const int tile_groups = (rows + vs::kTileRows - 1) / vs::kTileRows;
-    x.many = x.shares && rows > 72 && units * blocks * tile_groups >= 12 * 256;
+    x.many = x.shares && rows > 160 && units * blocks * tile_groups >= 12 * 256;
     if (x.many) {
         x.groups = tile_groups;
         x.shares = 256 / tile_groups < 4 ? 4 : 256 / tile_groups;     // (no fewer than above: shorter sequences need no larger workspace)

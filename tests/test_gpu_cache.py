@@ -208,8 +208,9 @@ def check(o, lse, q, k, v, lens, scale=128 ** -0.5, heads=None, dead=None):
             for head in range(h * hq // hk, (h + 1) * hq // hk):
                 ro, rl, size = plain.attend(q[b, head], kk, vv, limits, scale)
                 off = 2.0 ** -17 * scale * (np.abs(q[b, head]).sum(1) * (np.abs(kk).max() if n and len(kk) else 0.0))
-                # a weight below 2^-126 of the row's largest is below fp32's normal numbers and counts as zero: at most n such, times |v|
-                lost = 2.0 ** -126 * n * (np.abs(vv).max() if len(vv) else 0.0)
+                # A weight below 2^-126 of the row's largest is below fp32's normal numbers and counts as zero: at most n such, times |v|.
+                # A weight times V's scale and 2^-16 may be lost below 2^-126: times a code of at most 6 and 2^16 less than 2^-107 a key.
+                lost = n * (2.0 ** -126 * (np.abs(vv).max() if len(vv) else 0.0) + 2.0 ** -107)
                 bound = 2.0 ** -8 * np.abs(ro) + (2.0 ** -8 + 2 * off[:, None] + 2.0 ** -16) * size + lost
                 err = np.abs(o[b, head] - ro) - bound
                 assert err.max() <= 0, "sequence %d head %d row %d: %g past the bound" % (b, head, err.max(1).argmax(), err.max())
@@ -235,13 +236,15 @@ def test_attend_one_long_sequence(n_q, n, page):
 
 
 @pytest.mark.parametrize("n_q, lens, max_n, hq, hk", [(100, [13001], 13001, 32, 4), (128, [30001], 60000, 8, 2), (73, [3000, 0, 40, 5001, 73], 60000, 16, 16),
+                                                     (73, [3000, 0, 40, 5001, 73], 60000, 48, 16),
                                                      (128, [20000, 100, 64, 0], 20000, 33, 11)])
 def test_attend_many_rows(n_q, lens, max_n, hq, hk):
     """Chunks of a hundred rows and more over long contexts: row blocks that are not full, several sequences in a share, idle ones."""
     c, q, k, v, n = attend_case(200 + n_q + hq, hq, hk, n_q, lens, 192, max_n=max_n)
     rows = hq // hk * n_q
-    # the kernel for many rows: 256 rows a workgroup, its parts and one for each head
-    assert vs.cache_attend_workspace(len(lens), hq, hk, n_q, n) == (len(lens) * hk + 256 // -(-rows // 256)) * rows * 130 * 4
+    # the kernel for more than 160 rows: 256 rows a workgroup, its parts and one for each head
+    shares = 256 // -(-rows // 256) if rows > 160 else 1024 // -(-rows // 16) // 4 * 4
+    assert vs.cache_attend_workspace(len(lens), hq, hk, n_q, n) == (len(lens) * hk + shares) * rows * 130 * 4
     check(*call(c, q, lens, n), q, k, v, lens, heads=range(min(hk, 2)))
 
 
@@ -318,8 +321,8 @@ def test_attend_scores_whose_rounding_exceeds_a_unit(hq, hk, n_q, n):
         vv = plain.values(*plain.quantise(f64(v[0, h])))
         for r in range(n_q):
             at = n - 1 if r == n_q - 1 else peak
-            # weights of zero may count as 2^-126 (see check); a value of three bits keeps its bits beside that
-            assert (np.abs(f64(o[0, head, r]) - vv[at]) <= 2.0 ** -126 * n * np.abs(vv).max()).all(), (head, r)
+            # (what check's `lost` allows for the other weights)
+            assert (np.abs(f64(o[0, head, r]) - vv[at]) <= n * (2.0 ** -126 * np.abs(vv).max() + 2.0 ** -107)).all(), (head, r)
             want = f64(q[0, head, r]).sum() * float(k[0, h, at, 0]) * 128 ** -0.5
             assert abs(float(lse[0, head, r]) - want) <= 2.0 ** -16 * want, (head, r)
     check(o, lse, q, k, v, [n], heads=range(min(hk, 2)))     # (its bound for a large row allows anything)
@@ -379,6 +382,29 @@ def test_attend_extreme_scales():
         o, lse = call(c, q, lens, n)
         check(o, lse, q, k, v, lens)
         assert (o[2] == 0).all()
+
+
+@pytest.mark.parametrize("n_q", [1, 5])
+@pytest.mark.parametrize("n", [100, 9000])
+def test_attend_scales_of_all_sizes(n_q, n):
+    """Groups of V from 2^-120 to 2^100 beside each other, groups of zeros, in one block: weights whose exponents take a scale, and ones
+    that cannot."""
+    g = torch.Generator().manual_seed(n)
+    v = torch.randn(1, 2, n, 128, generator=g)
+    e = torch.randint(-120, 101, (1, 2, n, 4), generator=g)
+    e[0, 1] = torch.randint(-74, 17, (n, 4), generator=g)              # at the ends of the ordinary range, and
+    e[0, 1, :64] = torch.randint(-60, 10, (64, 4), generator=g)        # inside it
+    x = torch.exp2(e.float())
+    x[torch.rand(1, 2, n, 4, generator=g) < 0.1] = 0
+    v = (v * x.repeat_interleave(32, 3)).bfloat16().cuda()
+    c, q, k, _, _ = attend_case(95, 8, 2, n_q, [n], 64, v=v)[0:2] + (tokens(97, 1, 2, n), None, None)
+    check(*call(c, q, [n], n), q, k, v, [n])
+    padded = v.clone()
+    padded[..., 64:] = 0
+    c, q, _, _, _ = attend_case(95, 8, 2, n_q, [n], 64, v=padded)
+    o, lse = call(c, q, [n], n)
+    assert (o[..., 64:] == 0).all()
+    check(o, lse, q, k, padded, [n])
 
 
 def near(a, b, size):
