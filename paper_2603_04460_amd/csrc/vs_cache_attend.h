@@ -36,11 +36,9 @@ constexpr float kStale = 8.0f;                             // log2 units by whic
 constexpr float kLarge = 16777216.0f;                      // 2^24: from here on a score's rounding, times log2(e) and scale, is a unit and more
 constexpr int kMaxParts = 256;                             // shares of one sequence and KV head: the threads of the joining kernel
 
-// Scale byte i of a word as a number.  The lowest bit of the fraction makes the byte 255 a NaN instead of an infinity and is
-// far below the weights' rounding.
-__device__ __forceinline__ float scale_of(uint32_t w, int i) {
-    const uint32_t field = i == 0 ? w << 23 : i == 1 ? w << 15 : i == 2 ? w << 7 : w >> 1;
-    return __uint_as_float((field & 0x7f800000u) | 1u);
+// Scale byte i of a word for the conversions, which look at the exponent only: what is in the other bits does not matter.
+__device__ __forceinline__ float scale_field(uint32_t w, int i) {
+    return __uint_as_float(i == 0 ? w << 23 : i == 1 ? w << 15 : i == 2 ? w << 7 : w >> 1);
 }
 
 __device__ __forceinline__ bf16x8 operand(uint4 x) { return __builtin_bit_cast(bf16x8, x); }

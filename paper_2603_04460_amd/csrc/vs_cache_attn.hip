@@ -152,7 +152,7 @@ struct Rows {
         uint32_t word[4][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            scale[t] = __uint_as_float(((x.ks >> (8 * t)) & 0xffu) << 23);
+            scale[t] = scale_field(x.ks, t);
             word[t][0] = x.k[t].x;
             word[t][1] = x.k[t].y;
             word[t][2] = x.k[t].z;
@@ -547,7 +547,7 @@ Plan plan(int64_t units, int rows, int64_t max_n) {
     x.least = static_cast<int>((blocks + kMaxParts - 3) / (kMaxParts - 2));
     // Many rows: every workgroup turns a block into bf16 once for 256 rows; one workgroup on every compute unit, twelve blocks for each at least (its
     // start and its larger parts cost about as much as six).  16 rows a wavefront / 256 a workgroup, us: 32 / 8 heads, 32768 tokens, 32 new ones
-    // (128 rows) 41 / 42, 40 52 / 49, 48 59 / 52, 64 73 / 55, 100 112 / 86; 64 of 24000 56 / 51, of 16000 (8 blocks for each workgroup) 42 / 43, 100 of 16000
+    // (128 rows) 41 / 42, 40 52 / 49, 48 59 / 52, 64 73 / 55, 100 112 / 84; 64 of 24000 56 / 51, of 16000 (8 blocks for each workgroup) 42 / 43, 100 of 16000
     // 61 / 58, of 10000 (10) 44 / 47; 40 of 131072 171 / 146; four sequences of 8000, 50 new ones 44 / 45; 8 heads, 100 of 30000 37 / 42.
     const int tile_groups = (rows + vs::kTileRows - 1) / vs::kTileRows;
     x.many = x.shares && rows > 160 && units * blocks * tile_groups >= 12 * 256;

@@ -7,9 +7,9 @@
 // so that 16 lanes reading a chunk of 16 rows use all banks.
 // The codes of the block after next are on their way into registers while one block is worked on and the next one's are written to the other
 // buffer: one barrier a block.
-// 32 / 8 heads, 100 rows of 32768 tokens 85 us (54 Gflop: 630 TFLOP/s), 128 rows 88 (with 16 rows a wavefront and every wavefront turning its blocks into
-// bf16 for itself 156 and 191).  A block takes about 5500 clocks, of which the two products take 1100 each (the matrix unit is busy throughout), the
-// softmax 800 to 1000 and the turning into bf16 1800 to 2300.  The two wavefronts of a SIMD in opposite orders (one turns while the other multiplies) 94,
+// 32 / 8 heads, 32768 tokens, 100 new ones (400 rows) 84 us (54 Gflop: 640 TFLOP/s), 64 55 (with 16 rows a wavefront and every wavefront turning its
+// blocks into bf16 for itself 112 and 73).  A block takes about 5500 clocks, of which the two products take 1100 each (the matrix unit is busy throughout), the
+// softmax 800 to 1000 and the turning into bf16 1700 to 2200.  The two wavefronts of a SIMD in opposite orders (one turns while the other multiplies) 94,
 // 64 rows a wavefront, four wavefronts 114: not taken.
 #include "vs_cache_attend.h"
 
@@ -52,11 +52,14 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
 
     // a thread's piece of a block: 16 channels of a key, and 16 tokens of a channel of V with their scales
     const int key = threadIdx.x >> 3, chunk = 2 * (threadIdx.x & 7);
-    const int pc = threadIdx.x >> 5, c = pc & 3, channel = 32 * (pc >> 2) + 16 * (threadIdx.x & 1) + ((threadIdx.x >> 1) & 15);
-    const uint32_t k_scale = kKScales + 4 * (16 * (chunk >> 2) + (key & 15)) + (key >> 4), v_scale = kVScales + 16 * (4 * c + (pc >> 2));
+    // (so that 32 lanes, writing 8 bytes each, use all banks: 16 channels and both c of a 16-byte chunk)
+    const int group = threadIdx.x >> 7, c = ((threadIdx.x >> 6) & 1) + 2 * ((threadIdx.x >> 4) & 1);
+    const int channel = 32 * group + 16 * ((threadIdx.x >> 5) & 1) + (threadIdx.x & 15);
+    const uint32_t k_scale = kKScales + 4 * (16 * (chunk >> 2) + (key & 15)) + (key >> 4), v_scale = kVScales + 16 * (4 * c + group);
+    const uint32_t v_code = v_word(channel, c, 0);
     auto load = [&](Raw& x, const uint8_t* from) __attribute__((always_inline)) {
         x.k = *reinterpret_cast<const uint2*>(from + 8 * threadIdx.x);
-        x.v = *reinterpret_cast<const uint2*>(from + (kVCodes + 8 * threadIdx.x));
+        x.v = *reinterpret_cast<const uint2*>(from + v_code);
         x.ke = from[k_scale];
         x.ve = *reinterpret_cast<const uint4*>(from + v_scale);
     };
@@ -71,35 +74,34 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
         }
         uint8_t* const out = tile[to][1] + 128 * channel;
         const uint32_t e[4] = {x.ve.x, x.ve.y, x.ve.z, x.ve.w};
-        float y[16];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {                      // tokens 16 t + 4 c + 0 .. 3
+        uint32_t y[8];                                     // tokens 16 t + 4 c + 2 i, + 1 at 2 t + i: a word converted with the scale of either
+        static_for<8>([&](auto k) __attribute__((always_inline)) {
+            constexpr int t = k / 2, i = k % 2, two = 2 * (t & 1) + i;
             const uint32_t w = t < 2 ? x.v.x : x.v.y;
-            const f32x2 a = t & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
-            const f32x2 d = t & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
-            y[4 * t] = a[0] * scale_of(e[t], 0);
-            y[4 * t + 1] = a[1] * scale_of(e[t], 1);
-            y[4 * t + 2] = d[0] * scale_of(e[t], 2);
-            y[4 * t + 3] = d[1] * scale_of(e[t], 3);
-        }
+            const uint32_t a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale_field(e[t], 2 * i), two));
+            const uint32_t d = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale_field(e[t], 2 * i + 1), two));
+            y[k] = __builtin_amdgcn_perm(d, a, 0x07060100u);
+        });
         uint32_t nan = 0;                                  // some byte of the four words is 255
 #pragma unroll
         for (int t = 0; t < 4; ++t) nan |= (0xfefefefeu - e[t]) & e[t];
         if (live < kBlock || __any((nan & 0x80808080u) != 0)) {
             bool bad = false;
 #pragma unroll
-            for (int t = 0; t < 16; ++t) {
-                const bool there = 16 * (t >> 2) + 4 * c + (t & 3) < live;
-                bad |= there && y[t] != y[t];
-                y[t] = there && y[t] == y[t] ? y[t] : 0.0f;
-            }
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t half = j ? 0xffff0000u : 0xffffu;
+                    const bool there = 16 * (k >> 1) + 4 * c + 2 * (k & 1) + j < live, finite = ((y[k] & half) >> 16 * j & 0x7f80u) != 0x7f80u;
+                    bad |= there && !finite;
+                    if (!there || !finite) y[k] &= ~half;
+                }
             if (bad) tainted[to] = step;
             asm volatile("" ::: "memory");                 // (a branch, not selects for every block)
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-            *reinterpret_cast<uint2*>(out + 16 * ((2 * t + (c & 1)) ^ ((channel >> 1) & 7)) + 8 * (c >> 1)) =
-                make_uint2(pack_bf16(y[4 * t], y[4 * t + 1]), pack_bf16(y[4 * t + 2], y[4 * t + 3]));
+            *reinterpret_cast<uint2*>(out + 16 * ((2 * t + (c & 1)) ^ ((channel >> 1) & 7)) + 8 * (c >> 1)) = make_uint2(y[2 * t], y[2 * t + 1]);
     };
 
     // the block behind the one at x; the last one of the share stays
