@@ -5,7 +5,9 @@
  * cumulative-threshold budget with TopK, and causal vertical-slash sparse attention with the
  * per-query-tile index merge done inside the attention kernel, plus a dense causal attention
  * kernel on the same layout and the vertical-slash aggregation of the dense attention map (the
- * indexer's distillation target and the Attention Recall metric).
+ * indexer's distillation target and the Attention Recall metric).  "Around the prefill" has what a serving
+ * program needs beside it: norm and rotation of a projection's rows, a paged 4-bit cache of keys and values,
+ * and the attention of single tokens and short chunks over that cache.
  *
  * Conventions shared by every call
  *   - Every tensor pointer is a DEVICE pointer owned by the caller, contiguous, 16-byte

@@ -17,7 +17,7 @@
 //   attend_head_kernel  short sequences: eight wavefronts share a head's keys and add up in LDS
 //   attend_row_kernel   all blocks of all heads and sequences in a row, divided evenly among the wavefronts of the GPU whatever the sequences'
 //                       lengths (which only the GPU knows); attend_join_kernel adds the parts up
-// Bound by the memory for few rows: 136 bytes a key and KV head.  32 / 8 heads, one token of 131072 34 us (142 MB; a plain read of as much
+// Bound by the memory for few rows: 136 bytes a key and KV head.  32 / 8 heads, one token of 131072 33 us (142 MB; a plain read of as much
 // 24), of which the loop over the blocks 23, its slowest wavefront 26, the start 2 and the second kernel 5.
 #include "vs_cache_attend.h"
 
