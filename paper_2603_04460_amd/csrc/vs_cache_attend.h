@@ -15,7 +15,6 @@ struct AttendParams {
     float* part;                   // [items][rows][128] sums, then [items][rows] (maximum, sum of weights)
     int batch, n_q, rows;          // sequences; new tokens; query rows of a KV head (group * n_q)
     int shares;                    // workers (workgroups or wavefronts) that divide the blocks among them; 0: one for each head
-    int least;                     // blocks of a worker at least
     int items;                     // room in part: shares + sequences x KV heads
     float c, inverse_c;            // scale * log2(e), 1 / c
 };
@@ -34,7 +33,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kStale = 8.0f;                             // log2 units by which a score may exceed the running maximum
 constexpr float kLarge = 16777216.0f;                      // 2^24: from here on a score's rounding, times log2(e) and scale, is a unit and more
-constexpr int kMaxParts = 256;                             // shares of one sequence and KV head: the threads of the joining kernel
 
 // Scale byte i of a word for the conversions, which look at the exponent only: what is in the other bits does not matter.
 __device__ __forceinline__ float scale_field(uint32_t w, int i) {
@@ -77,7 +75,7 @@ __device__ __forceinline__ Lengths look(const AttendParams& p, int lane) {
     x.total = __builtin_amdgcn_readlane(wave_scan(blocks_of(x.first)), 63);
     for (int at = 64; at < p.batch; at += 64) x.total += __builtin_amdgcn_readlane(wave_scan(blocks_of(length_at(p, at + lane))), 63);
     const int all = x.total * p.cache.kv_heads;            // below 2^31: at most 65535 pairs of at most 16384 blocks
-    x.chunk = max((all + p.shares - 1) / p.shares, p.least);
+    x.chunk = max((all + p.shares - 1) / p.shares, 1);
     return x;
 }
 

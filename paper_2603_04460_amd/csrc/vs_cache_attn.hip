@@ -456,16 +456,17 @@ __global__ __launch_bounds__(256, 2) void attend_row_kernel(AttendParams p) {
 }
 
 // The parts of a row added up.  A workgroup has SLICE channels of a row: SLICE / 4 lanes hold them, the other lanes are that many groups,
-// which take the parts in turn; their first loads go out together with the statistics, which every thread reads of one part.
+// which take the parts in turn, four at a time, each with a running maximum of its own; they meet inside the wavefronts, then once in LDS.
+// 8 heads of 131072 tokens (128 parts of each) 4 us, the second kernel of a call; one head of 131072 (1024 parts) 13.5 with the first.
 template <int SLICE>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
     constexpr int kLanes = SLICE / 4, kGroups = 256 / kLanes, kAhead = 4;
-    __shared__ float weight[kMaxParts];
-    __shared__ float4 sums[kGroups][kLanes];
-    __shared__ float2 wave_stat[4];
+    static_assert(kLanes == 8 || kLanes == 32);
+    __shared__ float4 sums[4][kLanes];
+    __shared__ float2 stat[4];
     const int unit = blockIdx.x / p.rows, row = blockIdx.x - unit * p.rows;
     const int64_t r = blockIdx.x;
-    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, b = unit / p.cache.kv_heads;
+    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, wave = threadIdx.x >> 6, b = unit / p.cache.kv_heads;
     const int channel = blockIdx.y * SLICE + 4 * lane;
     const Lengths lens = look(p, threadIdx.x & 63);
     const Place at = find(p, lens, threadIdx.x & 63, 0, b, unit - b * p.cache.kv_heads);
@@ -475,49 +476,72 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
     if (parts == 1) return;                                // written by the wavefront that has all of the keys
     const int64_t slot = static_cast<int64_t>(from_share + unit) * p.rows + row;
     const float4* from = reinterpret_cast<const float4*>(p.part + slot * 128 + channel);
-    const int64_t step = static_cast<int64_t>(p.rows) * 32;
-    float4 z[kAhead];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-        z[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (group + kGroups * k < parts) z[k] = from[(group + kGroups * k) * step];
-    }
-    float2 mine = make_float2(-FLT_MAX, 0.0f);
-    if (static_cast<int>(threadIdx.x) < parts) mine = part_stat(p)[slot + static_cast<int64_t>(threadIdx.x) * p.rows];
-    const float m_wave = wave_max(mine.x);
-    if ((threadIdx.x & 63) == 0) wave_stat[threadIdx.x >> 6].x = m_wave;
-    __syncthreads();
-    const float m = fmaxf(fmaxf(wave_stat[0].x, wave_stat[1].x), fmaxf(wave_stat[2].x, wave_stat[3].x));
-    const float f = __builtin_amdgcn_exp2f(mine.x - m);
-    weight[threadIdx.x] = f;
-    const float l_wave = wave_sum(f * mine.y);
-    if ((threadIdx.x & 63) == 0) wave_stat[threadIdx.x >> 6].y = l_wave;
-    __syncthreads();
-    const float l = (wave_stat[0].y + wave_stat[1].y) + (wave_stat[2].y + wave_stat[3].y);
+    const float2* from_stat = part_stat(p) + slot;
+    float m = -FLT_MAX, l = 0.0f;
     float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    auto add = [&](const float4& x, float g) __attribute__((always_inline)) {
-        y.x = fmaf(x.x, g, y.x);
-        y.y = fmaf(x.y, g, y.y);
-        y.z = fmaf(x.z, g, y.z);
-        y.w = fmaf(x.w, g, y.w);
-    };
+    for (int s = group; s < parts; s += kAhead * kGroups) {
+        float4 z[kAhead];
+        float2 x[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-        if (group + kGroups * k < parts) add(z[k], weight[group + kGroups * k]);
-    for (int s = group + kGroups * kAhead; s < parts; s += kGroups) add(from[s * step], weight[s]);
-    sums[group][lane] = y;
-    for (int half = kGroups / 2; half > 0; half /= 2) {
-        __syncthreads();
-        if (group < half) {
-            const float4 x = sums[group + half][lane];
-            y.x += x.x;
-            y.y += x.y;
-            y.z += x.z;
-            y.w += x.w;
-            sums[group][lane] = y;
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t i = min(s + kGroups * k, parts - 1);
+            z[k] = from[i * p.rows * 32];
+            x[k] = from_stat[i * p.rows];
+        }
+        float most = m;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (s + kGroups * k >= parts) {                // the last part again: no weight
+                x[k] = make_float2(-FLT_MAX, 0.0f);
+                z[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+            most = fmaxf(most, x[k].x);
+        }
+        const float f = __builtin_amdgcn_exp2f(m - most);
+        m = most;
+        l *= f;
+        y = make_float4(y.x * f, y.y * f, y.z * f, y.w * f);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const float g = __builtin_amdgcn_exp2f(x[k].x - m);
+            l = fmaf(x[k].y, g, l);
+            y.x = fmaf(z[k].x, g, y.x);
+            y.y = fmaf(z[k].y, g, y.y);
+            y.z = fmaf(z[k].z, g, y.z);
+            y.w = fmaf(z[k].w, g, y.w);
         }
     }
+    // over the wavefront's groups: lanes that differ in bit 5, and bits 3 and 4
+    auto across = [&](float v, auto op) __attribute__((always_inline)) {
+        if (kLanes == 8) {
+            v = op(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true)));   // row_ror 8
+            return column_reduce(v, op);
+        }
+        const auto w = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+        const unsigned w0 = w[0], w1 = w[1];
+        return op(__builtin_bit_cast(float, w0), __builtin_bit_cast(float, w1));
+    };
+    const auto plus = [](float u, float v) { return u + v; };
+    const float most = across(m, [](float u, float v) { return fmaxf(u, v); }), f = __builtin_amdgcn_exp2f(m - most);
+    l = across(l * f, plus);
+    y = make_float4(across(y.x * f, plus), across(y.y * f, plus), across(y.z * f, plus), across(y.w * f, plus));
+    if ((threadIdx.x & 63) < kLanes) sums[wave][lane] = y;
+    if ((threadIdx.x & 63) == 0) stat[wave] = make_float2(most, l);
+    __syncthreads();
     if (group) return;
+    m = fmaxf(fmaxf(stat[0].x, stat[1].x), fmaxf(stat[2].x, stat[3].x));
+    l = 0.0f;
+    y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float g = __builtin_amdgcn_exp2f(stat[k].x - m);
+        const float4 z = sums[k][lane];
+        l = fmaf(stat[k].y, g, l);
+        y.x = fmaf(z.x, g, y.x);
+        y.y = fmaf(z.y, g, y.y);
+        y.z = fmaf(z.z, g, y.z);
+        y.w = fmaf(z.w, g, y.w);
+    }
     put_row(p, r, channel, y, l);
     if (channel == 0) put_lse(p, r, m, l);
 }
@@ -526,7 +550,7 @@ struct Plan {
     bool fold;
     bool many;                     // rows: the kernel of vs_cache_tile.hip
     int groups;                    // workgroups over the rows of a sequence and KV head
-    int shares, least;             // see AttendParams
+    int shares;                    // see AttendParams
     int64_t items;
 };
 
@@ -544,7 +568,6 @@ Plan plan(int64_t units, int rows, int64_t max_n) {
     // parts.  512 / 1024 / 1536 / 2048 wavefronts, us: 32 / 8 heads, one sequence of 32768 tokens 16.4 / 14.0 / 16.6 / 16.5, 131072 41 / 34 /
     // 37 / 36, 64 of 8000 59 / 45 / 47 / 44, four new tokens of 131072 54 / 38 / 43 / 41.
     x.shares = by_head ? 0 : 1024 / x.groups < 4 ? 4 : 1024 / x.groups / 4 * 4;
-    x.least = static_cast<int>((blocks + kMaxParts - 3) / (kMaxParts - 2));
     // Many rows: every workgroup turns a block into bf16 once for 256 rows; one workgroup on every compute unit, twelve blocks for each at least (its
     // start and its larger parts cost about as much as six).  16 rows a wavefront / 256 a workgroup, us: 32 / 8 heads, 32768 tokens, 32 new ones
     // (128 rows) 41 / 42, 40 52 / 49, 48 59 / 52, 64 73 / 55, 100 112 / 84; 64 of 24000 56 / 51, of 16000 (8 blocks for each workgroup) 42 / 43, 100 of 16000
@@ -594,7 +617,6 @@ extern "C" int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch
     p.batch = batch;
     p.n_q = n_q;
     p.shares = x.shares;
-    p.least = x.least;
     p.items = static_cast<int>(x.items);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (!x.shares) {

@@ -248,6 +248,13 @@ def test_attend_many_rows(n_q, lens, max_n, hq, hk):
     check(*call(c, q, lens, n), q, k, v, lens, heads=range(min(hk, 2)))
 
 
+@pytest.mark.parametrize("hq, hk, n_q, n", [(1, 1, 1, 90000), (4, 1, 1, 70001), (8, 1, 2, 66000), (2, 2, 1, 131072)])
+def test_attend_hundreds_of_parts(hq, hk, n_q, n):
+    """One or two KV heads: every wavefront of the GPU has a block or two, hundreds of parts of a row are added up."""
+    c, q, k, v, max_n = attend_case(250 + hq + n_q, hq, hk, n_q, [n], 256)
+    check(*call(c, q, None, max_n), q, k, v, [n])
+
+
 def test_attend_many_rows_missing_pages_and_values_that_are_not_finite():
     n, n_q, hq, hk = 50000, 100, 8, 4
     at = [n - 30, 77]
