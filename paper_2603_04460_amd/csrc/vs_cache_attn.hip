@@ -560,10 +560,14 @@ Plan plan(int64_t units, int rows, int64_t max_n) {
     const int per = x.fold ? kRows<true> : kRows<false>;
     x.groups = (rows + per - 1) / per;
     const int64_t blocks = (max_n + kBlock - 1) / kBlock;
-    // Short sequences: one workgroup for each head, two rounds of its eight wavefronts at most (four where there are many heads), and no second
-    // kernel, which costs 3 to 4 us.  One workgroup a head / blocks in a row, us: 32 / 8 heads, one sequence of 500 tokens 5.5 / 7.9,
-    // 1000 7.0 / 7.9, 2000 9.9 / 8.0, 16 sequences of 1000 7.1 / 9.2, 2000 10.5 / 11.8, 4000 16.9 / 15.4, 64 of 2000 18.7 / 20.8.
-    const bool by_head = blocks <= 2 * kHeadWaves || (blocks <= 4 * kHeadWaves && units * x.groups >= 128);
+    // Short sequences: one workgroup for each head and tile of rows, two rounds of its eight wavefronts at most (more where there are many workgroups), and
+    // no second kernel, which costs 3 to 4 us.  One workgroup a head / blocks in a row, us: 32 / 8 heads, one sequence of 500 tokens 5.5 / 7.4, 1000
+    // 6.9 / 7.5, 1500 8.3 / 7.6, 2000 9.7 / 7.7, 16 sequences of 1000 7.2 / 9.0, 2000 10.1 / 10.8, 4000 16.2 / 14.1, 64 of 2000 18.3 / 18.8, 3000 21.2 / 20.7.
+    // 16 rows: one sequence of 2000, 5 new tokens (16 workgroups) 10.3 / 9.4, 25 (56) 10.4 / 11.6, of 3000, 25 13.2 / 12.7, 50 (104) 13.5 / 16.7, of 4000, 100 (200)
+    // 17.6 / 26.5, of 8000 29.9 / 37.8; 16 of 2000, 5 10.9 / 15.4, of 4000 17.4 / 20.0, of 8000 29.1 / 26.2; 64 of 8000, 5 89 / 75.
+    const int64_t workgroups = units * x.groups;
+    const bool by_head = blocks <= 2 * kHeadWaves || (blocks <= 4 * kHeadWaves && workgroups >= (x.fold ? 128 : 48)) ||
+                         (!x.fold && blocks <= 8 * kHeadWaves && workgroups >= 192);
     // Otherwise a wavefront for every SIMD: with two blocks in registers each that is enough to keep the memory busy, and more of them only make more
     // parts.  512 / 1024 / 1536 / 2048 wavefronts, us: 32 / 8 heads, one sequence of 32768 tokens 16.4 / 14.0 / 16.6 / 16.5, 131072 41 / 34 /
     // 37 / 36, 64 of 8000 59 / 45 / 47 / 44, four new tokens of 131072 54 / 38 / 43 / 41.
