@@ -394,8 +394,8 @@ int vs_cache_read(const vs_cache_t* cache, int batch, int64_t rows, const int32_
  *   q, o  [batch, q_heads, n_q, 128] bf16 (not overlapping);  lse [batch, q_heads, n_q] fp32 out or NULL
  * A row without a key (negative position, idle slot, missing pages only) gives zeros and lse = -inf.  Longer chunks: vs_cache_read, then
  * vs_sparse_prefill_chunk or vs_dense_prefill_chunk.
- * Arithmetic: K and V are exact in bf16; bf16 MFMA, fp32 accumulation and softmax, P rounded to bf16.  The same call always gives
- * the same bits.  A score has to lie within fp32's range, and so do sums of V times weights of up to 2^8 (they do for |V| < 2^96).
+ * Arithmetic: K and V are exact in bf16; bf16 MFMA, fp32 accumulation and softmax, P as two bf16 terms (2^-15 of a weight; the output's own
+ * rounding is 2^-8).  The same call always gives the same bits.  A score has to lie within fp32's range, and so do sums of V times weights of up to 2^8 (they do for |V| < 2^96).
  * At most 2^24 - 1 rows in a call (batch * q_heads * n_q).  Workspace: vs_cache_attend_workspace; the answer for max_n is enough for every smaller max_n of the same call.
  */
 #define VS_CACHE_MAX_NEW 128

@@ -41,6 +41,16 @@ __device__ __forceinline__ float scale_field(uint32_t w, int i) {
 
 __device__ __forceinline__ bf16x8 operand(uint4 x) { return __builtin_bit_cast(bf16x8, x); }
 
+// Two weights as two bf16 terms each, 15 significant bits: the first cut off (so that the second is not negative), the second rounded.
+struct TwoTerms {
+    uint32_t high, low;
+};
+
+__device__ __forceinline__ TwoTerms two_terms(float a, float b) {
+    const uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
+    return {__builtin_amdgcn_perm(v, u, 0x07060302u), pack_bf16(a - __uint_as_float(u & 0xffff0000u), b - __uint_as_float(v & 0xffff0000u))};
+}
+
 // position of the first key of a block without a page: no row sees it
 constexpr int kNowhere = 1 << 30;
 

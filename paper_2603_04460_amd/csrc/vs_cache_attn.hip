@@ -5,8 +5,11 @@
 //   S^T = K Q^T   (keys x query rows, 16 x 16 x 32 matrix instructions, K's scales inside the conversion)
 //   O^T = V^T P^T (channels x query rows): the lane that holds scores 4 c .. 4 c + 3 of a column holds the weights that the second
 //                 product wants from it, nothing moves between lanes.
-// A word of V codes is eight keys of one channel and each key has its own scale, so V's scales go to the weights instead: P times
-// the scale (a power of two: no rounding besides P's own to bf16), one set per 32 channels.  As exponents of bf16 numbers that is a subtraction for two
+// P goes into the second product as two bf16 terms: rounded to one it would be as far off as the output's own rounding (error against 64 bits 0.0023
+// relative, in two terms 0.0016, the same as the output's rounding alone; one token of 131072 33.4 us with one term, 34.1 with two, five tokens of four
+// sequences of 20011 20.0 and 21.9).
+// A word of V codes is eight keys of one channel and each key has its own scale, so V's scales go to the weights instead: P's terms times
+// the scale (a power of two: no rounding), one set per 32 channels.  As exponents of bf16 numbers that is a subtraction for two
 // weights, of words that the wavefront makes in LDS once a block (five tokens of four sequences of 20011 22.9 -> 20.3 us against words made by every
 // lane for itself, 16 rows of 131072 39 -> 36, 64 rows of 32768 30 -> 26).
 //   up to four query rows of a KV head (FOLD): the 16 columns are four rows x four channel groups; every column has its group's
@@ -90,9 +93,9 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t weights, uint32_t word)
 }
 
 // the same for any scales: the byte 255 is a NaN, by the lowest bit of the fraction
-__device__ __forceinline__ uint32_t scaled_pair_any(float a, float b, uint32_t word) {
+__device__ __forceinline__ TwoTerms scaled_pair_any(float a, float b, uint32_t word) {
     const uint32_t e = less_pair((kScaleMost << 7) * 0x10001u, word);
-    return pack_bf16(a * __uint_as_float(e << 16 | 1u), b * __uint_as_float((e & 0xffff0000u) | 1u));
+    return two_terms(a * __uint_as_float(e << 16 | 1u), b * __uint_as_float((e & 0xffff0000u) | 1u));
 }
 
 // Lane's word of V's scales with those of keys that no row sees (they have no weight, whatever the memory holds) replaced by an ordinary one;
@@ -204,17 +207,18 @@ struct Rows {
             }
         sum = (part[0] + part[1]) + (part[2] + part[3]);
 
-        uint32_t pair[8], scales = x.vs;                   // weights of keys 2 i and 2 i + 1 of the lane's 16
+        TwoTerms pair[8];                                  // weights of keys 2 i and 2 i + 1 of the lane's 16
+        uint32_t scales = x.vs;
         if (edge) {
             scales = live_scales(scales, lane, len - key);
             asm volatile("" ::: "memory");
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pair[i] = pack_bf16(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
+        for (int i = 0; i < 8; ++i) pair[i] = two_terms(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
         const bool plain = !__any(odd_scales(scales));
         // ordinary: no scale is out of the ordinary
         auto products = [&](auto ordinary) __attribute__((always_inline)) {
-            bf16x8 w[2];
+            bf16x8 high[2], low[2];
             const uint4* const of = reinterpret_cast<const uint4*>(words) + 8 * c + (FOLD ? 2 * (lane & 3) : 0);
             uint4 ahead[2] = {of[0], of[1]};               // words of V's scales, requested a step ahead
             int base = key;
@@ -230,28 +234,38 @@ struct Rows {
                         }
                         __builtin_amdgcn_sched_barrier(0xf);       // (reads stay in front)
                     }
-                    uint32_t y[8];
+                    TwoTerms y[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         if (ordinary) {
-                            y[i] = scaled_pair(pair[i], e[i]);
+                            y[i] = {scaled_pair(pair[i].high, e[i]), scaled_pair(pair[i].low, e[i])};
                         } else {                           // a key that the row does not see has whatever scale the memory holds
                             y[i] = scaled_pair_any(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1], e[i]);
                             const int at = base + 16 * (i >> 1) + 4 * c + 2 * (i & 1);
-                            if (at > limit) y[i] = 0;
-                            if (at + 1 > limit) y[i] &= 0xffffu;
+                            const uint32_t seen = at > limit ? 0u : at + 1 > limit ? 0xffffu : ~0u;
+                            y[i] = {y[i].high & seen, y[i].low & seen};
                         }
                     }
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) w[u] = operand(make_uint4(y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]));
+                    for (int u = 0; u < 2; ++u) {
+                        high[u] = operand(make_uint4(y[4 * u].high, y[4 * u + 1].high, y[4 * u + 2].high, y[4 * u + 3].high));
+                        low[u] = operand(make_uint4(y[4 * u].low, y[4 * u + 1].low, y[4 * u + 2].low, y[4 * u + 3].low));
+                    }
                 }
                 const uint32_t v[4] = {x.v[g].x, x.v[g].y, x.v[g].z, x.v[g].w};
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
+                {
+                    bf16x8 values[2];
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        values[half] = operand(dequantise8(v[2 * half + u], ordinary ? static_cast<float>(1 << kRaise) : 1.0f));
+                        o[2 * g + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values[half], high[u], o[2 * g + half], 0, 0, 0);
+                    }
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
-                        o[2 * g + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(dequantise8(v[2 * half + u], ordinary ? static_cast<float>(1 << kRaise) : 1.0f)),
-                                                                                 w[u], o[2 * g + half], 0, 0, 0);
+                        o[2 * g + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values[half], low[u], o[2 * g + half], 0, 0, 0);
+                }
             }
         };
         if (plain) products(std::integral_constant<bool, true>{});

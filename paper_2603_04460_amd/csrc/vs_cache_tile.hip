@@ -7,6 +7,7 @@
 // so that 16 lanes reading a chunk of 16 rows use all banks.
 // The codes of the block after next are on their way into registers while one block is worked on and the next one's are written to the other
 // buffer: one barrier a block.
+// P goes into the second product as two bf16 terms, which read the same operand of V (see vs_cache_attn.hip): 84 us with one term, 97 with two.
 // 32 / 8 heads, 32768 tokens, 100 new ones (400 rows) 84 us (54 Gflop: 640 TFLOP/s), 64 55 (with 16 rows a wavefront and every wavefront turning its
 // blocks into bf16 for itself 112 and 73).  A block takes about 5500 clocks, of which the two products take 1100 each (the matrix unit is busy throughout), the
 // softmax 800 to 1000 and the turning into bf16 1700 to 2200.  The two wavefronts of a SIMD in opposite orders (one turns while the other multiplies) 94,
@@ -180,14 +181,14 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
         }
     };
 
-    // The operands' LDS reads run six ahead of the products that take them.
-    auto ahead_of_products = [&](auto id) __attribute__((always_inline)) {
+    // The operands' LDS reads run six ahead of the products that take them, `each` products an operand.
+    auto ahead_of_products = [&](auto id, auto each) __attribute__((always_inline)) {
         __builtin_amdgcn_sched_group_barrier(0x100, 6, id);                // LDS reads
         static_for<10>([&](auto) __attribute__((always_inline)) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, id);            // a matrix instruction
+            __builtin_amdgcn_sched_group_barrier(0x008, each, id);         // matrix instructions
             __builtin_amdgcn_sched_group_barrier(0x100, 1, id);
         });
-        __builtin_amdgcn_sched_group_barrier(0x008, 6, id);
+        __builtin_amdgcn_sched_group_barrier(0x008, 6 * each, id);
     };
     auto take = [&](int buffer, const Tag& y, int step) __attribute__((always_inline)) {
         const bool edge = y.key + kBlock - 1 > y.len - p.n_q;
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
                 const bf16x8 a = operand(*reinterpret_cast<const uint4*>(tile[buffer][0] + 256 * (32 * t + col) + 16 * ((2 * j + half) ^ (col & 15))));
                 s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[j], s[t], 0, 0, 0);
             }
-        ahead_of_products(std::integral_constant<int, 0>{});
+        ahead_of_products(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
         if (edge) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -238,18 +239,19 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
             }
         }
         float part[4] = {sum, 0.0f, 0.0f, 0.0f};
-        bf16x8 w[4];
+        bf16x8 high[4], low[4];                            // the weights in two terms
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            uint32_t word[4];
+            TwoTerms y[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float a = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][8 * (k & 1) + 2 * i], p.c, -less));
                 const float b = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][8 * (k & 1) + 2 * i + 1], p.c, -less));
                 part[k] += a + b;
-                word[i] = pack_bf16(a, b);
+                y[i] = two_terms(a, b);
             }
-            w[k] = operand(make_uint4(word[0], word[1], word[2], word[3]));
+            high[k] = operand(make_uint4(y[0].high, y[1].high, y[2].high, y[3].high));
+            low[k] = operand(make_uint4(y[0].low, y[1].low, y[2].low, y[3].low));
         }
         sum = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
@@ -257,9 +259,10 @@ __global__ __launch_bounds__(64 * vs::kTileWaves, 2) void attend_tile_kernel(Att
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const bf16x8 a = operand(*reinterpret_cast<const uint4*>(tile[buffer][1] + 128 * (32 * j + col) + 16 * ((2 * k + half) ^ ((col >> 1) & 7))));
-                o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[k], o[j], 0, 0, 0);
+                o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, high[k], o[j], 0, 0, 0);
+                o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, low[k], o[j], 0, 0, 0);
             }
-        ahead_of_products(std::integral_constant<int, 1>{});
+        ahead_of_products(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});
         if (tainted[buffer] == step) {
             const int live = live_of(y);
             for (int g = 0; g < 4; ++g)
