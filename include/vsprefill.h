@@ -365,6 +365,9 @@ typedef struct {
     int max_pages;
 } vs_cache_t;
 
+/* Bytes of `data`; 0 for sizes that name no cache, 2^64 less a page (more than any memory) where the product passes 64 bits.  The calls
+ * take pages < 2^31, kv_heads <= 4096, page_size <= VS_MAX_SEQ, batch * kv_heads <= 65535 and caches of less than 2^63 bytes; others are
+ * VS_ERR_UNSUPPORTED. */
 size_t vs_cache_bytes(int64_t pages, int kv_heads, int page_size);
 
 /*

@@ -166,6 +166,9 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheParams p, uin
 // workgroups along the tokens: blocks that `rows` tokens can touch wherever they begin
 unsigned blocks_of(int64_t rows) { return static_cast<unsigned>((rows + kBlock - 2) / kBlock + 1); }
 
+// at most 2^12 heads of 2^14 blocks: below 2^40
+int64_t page_bytes(int kv_heads, int page_size) { return static_cast<int64_t>(kv_heads) * (page_size / kBlock) * kBlockBytes; }
+
 }  // namespace
 
 namespace vs {
@@ -175,6 +178,8 @@ int cache_params(const vs_cache_t* cache, int batch, const int32_t* lens, int64_
     if (batch <= 0 || max_n <= 0 || cache->pages <= 0 || cache->kv_heads <= 0 || cache->page_size <= 0 || cache->max_pages <= 0) return VS_ERR_INVALID_ARG;
     if (cache->page_size % kBlock || cache->page_size > VS_MAX_SEQ || max_n > VS_MAX_SEQ || cache->kv_heads > 4096 || batch > 65535 ||
         static_cast<int64_t>(batch) * cache->kv_heads > 65535 || cache->pages > INT32_MAX) return VS_ERR_UNSUPPORTED;
+    int64_t bytes;                                         // offsets into the cache have to fit in 64 bits
+    if (__builtin_mul_overflow(cache->pages, page_bytes(cache->kv_heads, cache->page_size), &bytes)) return VS_ERR_UNSUPPORTED;
     if (max_n > static_cast<int64_t>(cache->max_pages) * cache->page_size) return VS_ERR_INVALID_ARG;
     if (!cache->table && static_cast<int64_t>(batch) * cache->max_pages > cache->pages) return VS_ERR_INVALID_ARG;
     p->data = static_cast<uint8_t*>(cache->data);
@@ -193,7 +198,9 @@ int cache_params(const vs_cache_t* cache, int batch, const int32_t* lens, int64_
 
 extern "C" size_t vs_cache_bytes(int64_t pages, int kv_heads, int page_size) {
     if (pages <= 0 || kv_heads <= 0 || page_size <= 0 || page_size % kBlock || pages > INT32_MAX || kv_heads > 4096 || page_size > VS_MAX_SEQ) return 0;
-    return static_cast<size_t>(pages) * kv_heads * (page_size / kBlock) * kBlockBytes;
+    size_t bytes;
+    const size_t page = static_cast<size_t>(page_bytes(kv_heads, page_size));
+    return __builtin_mul_overflow(static_cast<size_t>(pages), page, &bytes) ? 0 - page : bytes;
 }
 
 extern "C" int vs_cache_write(const vs_cache_t* cache, const void* k, const void* v, int batch, int64_t rows, const int32_t* lens,
