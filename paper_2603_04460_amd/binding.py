@@ -428,19 +428,28 @@ def rope_frequencies(theta_base, rot_dim=128, scaling=0, factor=1.0, low=1.0, hi
 
 
 class Rope:
-    """Rotation of the first 2 * len(freq) elements of every head.  freq: float64 on the GPU (rope_frequencies(...).cuda())."""
+    """Rotation of the first 2 * len(freq) elements of every head.  freq: float64 on the GPU (rope_frequencies(...).cuda()).
+    freq, pairing and magnitude may be set; calls already captured into a graph keep what they were captured with."""
 
     def __init__(self, freq, pairing=0, magnitude=1.0):
+        self._set(freq, int(pairing), float(magnitude))
+
+    def _set(self, freq, pairing, magnitude):
         import torch
-        self.freq = _dev(freq, torch.float64, "freq")
+        _dev(freq, torch.float64, "freq")
         assert freq.dim() == 1
-        self.pairing, self.magnitude = int(pairing), float(magnitude)
-        self._c = _Rotation(freq.data_ptr(), 2 * freq.numel(), self.pairing, self.magnitude)
-        self._ref, self._device = ctypes.byref(self._c), freq.get_device()
+        self._freq, self._device = freq, freq.get_device()
+        self._c = _Rotation(freq.data_ptr(), 2 * freq.numel(), pairing, magnitude)
+        self._ref = ctypes.byref(self._c)
+        self._pairing, self._magnitude = pairing, magnitude
+
+    freq = property(lambda self: self._freq, lambda self, x: self._set(x, self._pairing, self._magnitude))
+    pairing = property(lambda self: self._pairing, lambda self, x: self._set(self._freq, int(x), self._magnitude))
+    magnitude = property(lambda self: self._magnitude, lambda self, x: self._set(self._freq, self._pairing, float(x)))
 
     def _on(self, at):
         if self._device != at:
-            raise ValueError("freq is on %s, the current device is cuda:%d" % (self.freq.device, at))
+            raise ValueError("freq is on %s, the current device is cuda:%d" % (self._freq.device, at))
 
     def c_struct(self):
         return self._c
@@ -500,23 +509,34 @@ def cache_bytes(pages, kv_heads, page_size):
 
 class Cache:
     """The paged 4-bit cache of a layer: data [pages, kv_heads, page_size / 64, 8704] uint8 and the page table [batch, max_pages]
-    int32, or max_pages alone: sequence b then has the pages b * max_pages .. (b + 1) * max_pages - 1."""
+    int32, or max_pages alone: sequence b then has the pages b * max_pages .. (b + 1) * max_pages - 1.
+    data and table (or max_pages without a table) may be set, as a cache grows; the other sizes follow.  The tensors themselves are not to be
+    resized in place, and calls already captured into a graph keep what they were captured with."""
 
     def __init__(self, data, table=None, max_pages=None):
+        self._set(data, table, max_pages)
+
+    def _set(self, data, table, max_pages):
         import torch
         _dev(data, torch.uint8, "data")
         assert data.dim() == 4 and data.shape[3] == CACHE_BLOCK_BYTES and (table is None) != (max_pages is None)
         if table is not None:
             _dev(table, torch.int32, "table")
             assert table.dim() == 2
+            if table.get_device() != data.get_device():
+                raise ValueError("data is on %s, table on %s" % (data.device, table.device))
             max_pages = table.shape[1]
-        self.data, self.table, self.max_pages = data, table, int(max_pages)
-        self.pages, self.kv_heads, self.page_size = data.shape[0], data.shape[1], data.shape[2] * CACHE_BLOCK
-        self._c = _Cache(data.data_ptr(), self.pages, self.kv_heads, self.page_size, None if table is None else table.data_ptr(),
-                         self.max_pages)
-        self._ref, self._device = ctypes.byref(self._c), data.get_device()
-        if table is not None and table.get_device() != self._device:
-            raise ValueError("data is on %s, table on %s" % (data.device, table.device))
+        c = _Cache(data.data_ptr(), data.shape[0], data.shape[1], data.shape[2] * CACHE_BLOCK, None if table is None else table.data_ptr(),
+                   int(max_pages))
+        self._data, self._table, self._c, self._ref, self._device = data, table, c, ctypes.byref(c), data.get_device()
+        self._kv_heads, self._batches = data.shape[1], None if table is None else table.shape[0]
+
+    data = property(lambda self: self._data, lambda self, x: self._set(x, self._table, self._c.max_pages if self._table is None else None))
+    table = property(lambda self: self._table, lambda self, x: self._set(self._data, x, None))
+    max_pages = property(lambda self: self._c.max_pages, lambda self, x: self._set(self._data, self._table, x))
+    pages = property(lambda self: self._c.pages)
+    kv_heads = property(lambda self: self._kv_heads)
+    page_size = property(lambda self: self._c.page_size)
 
     def c_struct(self):
         return self._c
@@ -526,8 +546,8 @@ class Cache:
         batch, h, rows, d = shape if len(shape) == 4 else (1,) + tuple(shape)
         assert d == 128 and (heads is None or h == heads)
         if self._device != at:
-            raise ValueError("the cache is on %s, the current device is cuda:%d" % (self.data.device, at))
-        assert self.table is None or self.table.shape[0] == batch
+            raise ValueError("the cache is on %s, the current device is cuda:%d" % (self._data.device, at))
+        assert self._batches is None or self._batches == batch
         if lens is not None:
             assert _on(at, lens, int32, "lens").numel() == batch
         return batch, h, rows
@@ -538,7 +558,7 @@ def cache_write(cache, k, v, max_n, lens=None, stream=None):
     that then hold lens [batch] int32 tokens each (None: max_n)."""
     import torch
     at, bf16 = torch.cuda.current_device(), torch.bfloat16
-    batch, _, rows = cache._batch(at, k, bf16, cache.kv_heads, lens, torch.int32, "k")
+    batch, _, rows = cache._batch(at, k, bf16, cache._kv_heads, lens, torch.int32, "k")
     assert _on(at, v, bf16, "v").shape == k.shape
     _check((_lib or _load()).vs_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), batch, rows, _ptr(lens), max_n, _stream(stream, at)),
            "vs_cache_write")
@@ -549,7 +569,7 @@ def cache_read(cache, k, v, max_n, lens=None, stream=None):
     """The last tokens of each sequence as the cache holds them, into k, v [batch, kv_heads, rows, 128] bf16 (one may be None)."""
     import torch
     at, bf16 = torch.cuda.current_device(), torch.bfloat16
-    batch, _, rows = cache._batch(at, v if k is None else k, bf16, cache.kv_heads, lens, torch.int32, "v" if k is None else "k")
+    batch, _, rows = cache._batch(at, v if k is None else k, bf16, cache._kv_heads, lens, torch.int32, "v" if k is None else "k")
     if k is not None and v is not None:
         assert _on(at, v, bf16, "v").shape == k.shape
     _check((_lib or _load()).vs_cache_read(cache._ref, batch, rows, _ptr(lens), max_n, _ptr(k), _ptr(v), _stream(stream, at)), "vs_cache_read")
