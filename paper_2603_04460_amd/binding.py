@@ -451,9 +451,6 @@ class Rope:
         if self._device != at:
             raise ValueError("freq is on %s, the current device is cuda:%d" % (self._freq.device, at))
 
-    def c_struct(self):
-        return self._c
-
 
 def _rows(at, x, dtype, shape, what):
     """Address and strides (a vs_rows_t) of a [tokens, heads, 128] tensor with any strides of tokens and heads."""
@@ -537,9 +534,6 @@ class Cache:
     pages = property(lambda self: self._c.pages)
     kv_heads = property(lambda self: self._kv_heads)
     page_size = property(lambda self: self._c.page_size)
-
-    def c_struct(self):
-        return self._c
 
     def _batch(self, at, x, bf16, heads, lens, int32, what):
         shape = _on(at, x, bf16, what).shape
