@@ -137,6 +137,8 @@ def _stream(stream, at=None):
         import torch
         # the handle of torch.cuda.current_stream() without the object around it, which costs more than a launch
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if at is None else at)
+    if at is not None and stream.device.index != at:
+        raise ValueError("stream is on %s, the current device is cuda:%d" % (stream.device, at))
     return stream.cuda_stream
 
 

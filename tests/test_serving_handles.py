@@ -69,3 +69,17 @@ def test_a_rotation_that_is_replaced():
         with pytest.raises(error):
             r.freq = bad
         assert r.freq is kept and same()
+
+
+class Stream:
+    cuda_stream = 77
+
+    def __init__(self, index):
+        self.device = torch.device("cuda", index)
+
+
+def test_streams_of_another_device():
+    """The tensors of a call are on the current device, and so has its stream to be."""
+    assert binding._stream(Stream(0), 0) == 77 and binding._stream(Stream(3), 3) == 77
+    with pytest.raises(ValueError):
+        binding._stream(Stream(1), 0)
