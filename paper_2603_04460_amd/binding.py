@@ -585,8 +585,8 @@ def cache_attend(q, cache, o, max_n, lens=None, lse=None, ws=None, scale=None, s
     assert _on(at, o, bf16, "o").shape == q.shape
     if lse is not None:
         assert _on(at, lse, torch.float32, "lse").numel() == batch * q_heads * n_q
-    if ws is not None and ws.get_device() != at:
-        raise ValueError("ws is on %s, the current device is cuda:%d" % (ws.device, at))
+    if ws is not None:
+        _on(at, ws, ws.dtype, "ws")
     _check((_lib or _load()).vs_cache_attend(q.data_ptr(), cache._ref, batch, q_heads, n_q, _ptr(lens), max_n, 128 ** -0.5 if scale is None else scale,
                                              o.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream, at)),
            "vs_cache_attend")

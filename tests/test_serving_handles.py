@@ -83,3 +83,13 @@ def test_streams_of_another_device():
     assert binding._stream(Stream(0), 0) == 77 and binding._stream(Stream(3), 3) == 77
     with pytest.raises(ValueError):
         binding._stream(Stream(1), 0)
+
+
+def test_workspaces_that_hold_less_than_they_say(monkeypatch):
+    """A workspace is a contiguous tensor of the current device: nbytes of an expanded one counts memory that it does not have."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)           # where host tensors say that they are
+    c = vs.Cache(pages(4), max_pages=4)
+    q = torch.zeros(1, 4, 1, 128, dtype=torch.bfloat16)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 20)[::2]):
+        with pytest.raises(TypeError):
+            vs.cache_attend(q, c, torch.zeros_like(q), 300, ws=ws)
