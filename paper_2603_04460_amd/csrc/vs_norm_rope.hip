@@ -31,7 +31,7 @@ struct Part {                                  // q, k or v
     const float* w;                            // null: no norm
     int64_t token, head;                       // strides of x in elements
     int heads;
-    int groups;                                // workgroups that share the heads
+    int groups, per;                           // workgroups that share the heads, heads of each
     int plain;                                 // copied as it is
 };
 
@@ -120,8 +120,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormRopeParams p) {
     // the two pieces of four elements
     const int at0 = turned && PAIRED_HALVES ? 4 * l : 8 * l;
     const int at1 = turned && PAIRED_HALVES ? p.rot_dim / 2 + 4 * l : 8 * l + 4;
-    const int per = (part.heads + part.groups - 1) / part.groups;
-    const int h0 = group * per, h1 = min(group * per + per, part.heads);
+    const int h0 = group * part.per, h1 = min(h0 + part.per, part.heads);
     const uint16_t* x = part.x + t * part.token;
     uint16_t* out = part.out + (static_cast<int64_t>(b) * part.heads * p.rows + r) * 128;
     const int64_t out_head = static_cast<int64_t>(p.rows) * 128;
@@ -251,12 +250,15 @@ extern "C" int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_
     const unsigned blocks = (p.tokens + kPositions - 1) / kPositions;
     // Short calls: the heads are shared out over about two workgroups per compute unit, whole batches of heads together; every
     // workgroup evaluates the angles of its positions.  One workgroup over all heads / shared out: 16 x 1 position, 32 / 8 heads 33.6 / 4.2 us,
-    // 4099 positions 92 / 22.7 (2048 workgroups 23.7, 8192 26.0), 131072 positions the same.
+    // 4099 positions 92 / 22.7 (2048 workgroups 23.7, 8192 26.0), 131072 positions the same; shares of whole batches / of ceil(heads / workgroups) heads:
+    // 1000 positions 8.3 / 9.0, 2000 11.6 / 12.4, 33 / 11 heads x 1000 8.8 / 9.4, 16 sequences x 1 4.0 / 4.2, 700, 1500, 4099 and 32768 positions the same.
     unsigned groups = 0;
     for (Part& x : p.part) {
-        const int most = (x.heads + kBatch - 1) / kBatch;
-        x.groups = static_cast<int>((512ll * x.heads / (q_heads + 2 * kv_heads) + blocks - 1) / blocks);
-        x.groups = x.groups < 1 ? (x.heads > 0) : x.groups > most ? most : x.groups;
+        const int batches = (x.heads + kBatch - 1) / kBatch;
+        int64_t share = (512ll * x.heads / (q_heads + 2 * kv_heads) + blocks - 1) / blocks;
+        share = share < 1 ? 1 : share > batches ? batches : share;
+        x.per = batches ? static_cast<int>((batches + share - 1) / share) * kBatch : kBatch;
+        x.groups = (x.heads + x.per - 1) / x.per;
         groups += x.groups;
     }
     const dim3 grid(blocks, groups);
