@@ -340,7 +340,8 @@ int vs_rope_frequencies(double theta_base, int rot_dim, int scaling, double fact
  *   q_out [batch, q_heads, rows, 128], k_out, v_out [batch, kv_heads, rows, 128] bf16.  An output may be its own input where both
  *               have the same layout; otherwise they must not overlap.
  *   eps         FLT_MIN .. 1 (ignored without w_q and w_k);  pos0 + rows at most 2^31
- * Arithmetic: angles reduced in fp64, sine, cosine, norm and rotation in fp32, one rounding to bf16.
+ * Arithmetic: angles reduced in fp64, sine, cosine, norm and rotation in fp32, one rounding to bf16: before it within 2^-19 of magnitude
+ * (|a| + |b|) where |position * freq| < 2^31 (freq <= 1 at every position; larger angles lose 3 * 2^-53 of themselves more).
  */
 int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_rows_t* v, int batch, int64_t rows, int q_heads, int kv_heads,
                     const float* w_q, const float* w_k, float eps, const vs_rotation_t* rotation, const int32_t* lens, int64_t pos0,

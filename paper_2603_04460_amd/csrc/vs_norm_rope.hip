@@ -6,8 +6,10 @@
 //
 // 16 lanes hold a row, eight elements each, as two 8-byte pieces: lanes below rot_dim / 8 have whole planes 4 l .. 4 l + 3 (with half
 // pairing the pieces are rot_dim / 2 apart), the others plain elements, so that a rotation needs no lane's neighbour.  The angle
-// is reduced to a fraction of a turn in fp64 (positions reach 2^20), its sine and cosine are fp32: within 2^-23 of the
-// rotated pair's size, 2^14 times finer than a bf16 step.  They serve all heads of a position that a thread walks over.
+// is reduced to a fraction of a turn in fp64, its sine and cosine are fp32.  Before its rounding an element is within 2^-19 of |a| + |b|, the rotated pair, for
+// |position * freq| up to 2^31: 3 * 2^-53 of the angle from the reduction (2^-20.4 there, nothing at 2^20), 2 pi 2^-26 where the fraction
+// becomes fp32, 2^-23 of sine and cosine, fewer than 13 roundings of 2^-24 in norm, weights, magnitude and products; 2^11 times finer than
+// the rounding to bf16.  The angles serve all heads of a position that a thread walks over.
 // A head's row costs a norm and four products a plane: the weights are folded into the angles' sines and cosines.
 // Bound by the memory: every element is read and written once.  131072 positions of 32 / 8 heads 675 us (4.8 TB/s; a large copy reaches 5.1),
 // with one row's loads in flight, weights apart and all parts in one loop 860.
@@ -223,7 +225,7 @@ extern "C" int vs_qk_norm_rope(const vs_rows_t* q, const vs_rows_t* k, const vs_
         if (x->token_stride % 8 || x->head_stride % 8) return VS_ERR_INVALID_ARG;
     }
     if (rotation->rot_dim < 8 || rotation->rot_dim > VS_HEAD_DIM || rotation->rot_dim % 8) return VS_ERR_UNSUPPORTED;
-    if (pos0 > (1ll << 31) - rows) return VS_ERR_UNSUPPORTED;      // an angle's fraction of a turn keeps 2^-24
+    if (pos0 > (1ll << 31) - rows) return VS_ERR_UNSUPPORTED;      // (with freq <= 1 the angle's reduction keeps 2^-20)
     if (rows > VS_MAX_SEQ || batch > 65535 || static_cast<int64_t>(batch) * rows > (1 << 26) || q_heads > 4096 || kv_heads > 4096) return VS_ERR_UNSUPPORTED;
 
     NormRopeParams p;
