@@ -560,6 +560,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
     if (channel == 0) put_lse(p, r, m, l);
 }
 
+constexpr int kSliced = 512;                               // fewer rows than this: the joining kernel has four workgroups a row
+
 struct Plan {
     bool fold;
     bool many;                     // rows: the kernel of vs_cache_tile.hip
@@ -568,33 +570,52 @@ struct Plan {
     int64_t items;
 };
 
-Plan plan(int64_t units, int rows, int64_t max_n) {
+// The form with the least time by these estimates (us), each a line in the number of blocks that the bound of the lengths allows: a start, the blocks of one worker,
+// and `join`, the second kernel, the parts and the scans over the lengths.  Sequences of a batch differ in length and are counted as 2/5 of the bound (the
+// batches below: spread evenly in their logarithm from a sixteenth of it to all of it).
+//   head   a workgroup for each head and tile of rows, eight wavefronts to its blocks, one workgroup on a compute unit at a time, no second kernel
+//   row    all blocks in a row, divided among the wavefronts of the GPU
+//   tile   all blocks in a row, turned into bf16 once for 256 rows
+// The estimates' starts grow in this order, so that with more blocks the form goes from head to row to tile and never back, and so does the workspace.
+// Measured, head / row, 32 / 8 heads (sequences x new tokens x longest): 1 x 1 x 1000 7.5 / 7.6, 1500 9.2 / 7.8, 4 x 1 x 1000 7.4 / 7.9, 1500 9.2 / 8.2, 8 x 1 x 1500 9.2 / 9.2,
+// 2000 10.8 / 9.3, 12 x 1 x 1500 9.2 / 10.2, 2000 11.0 / 10.4, 16 x 1 x 1500 9.6 / 10.8, 2000 11.4 / 11.2, 4000 18.5 / 14.8, 32 x 1 x 2000 12.9 / 14.8, 3000 16.4 / 16.0, 4000 19.8 / 17.2,
+// 64 x 1 x 2000 20.1 / 19.6, 3000 23.2 / 22.1, 4 heads on one, 64 x 1 x 1500 9.1 / 9.1, 200 10.3 / 15.3, 300 14.7 / 18.0; 1 x 5 x 1000 7.9 / 8.8, 1500 9.7 / 9.2, 2000 11.5 / 9.7, 4 x 5 x 1500 9.7 / 9.7, 2000 11.6 / 10.8, 16 x 5 x 4000 20.1 / 20.9, 6000 27.1 / 23.3,
+// 64 x 5 x 2000 33 / 38, 4000 59 / 61, 8000 99 / 82; 1 x 25 x 2000 11.8 / 12.2, 3000 15.5 / 13.4, 1 x 50 x 3000 15.7 / 17.7, 4000 19.4 / 19.6, 6000 26.7 / 24.1, 1 x 75 x 8000 34 / 36,
+// 1 x 100 x 4000 20 / 29, 8000 34 / 42, 12000 48 / 59; 4 x 25 x 4000 19.5 / 20.5, 6000 27 / 21, 16 x 16 x 4000 36 / 36, 8000 53 / 44, 4 x 50 x 2000 22 / 24, 4000 37 / 31.
+// Row / tile: 1 x 24 (96 rows of a KV head) x 32768 41 / 42, 131072 130 / 128, 1 x 32 (128) x 24000 39 / 39, 32768 48 / 44, 131072 164 / 132, 1 x 40 (160) x 16000 35 / 39,
+// 24000 48 / 48, 32768 60 / 55, 131072 211 / 172, 1 x 48 x 16000 41 / 41, 24000 55 / 51, 1 x 64 x 10000 35 / 40, 16000 49 / 46, 32768 88 / 63, 1 x 100 x 16000 73 / 64, 32768 136 / 98;
+// 4 x 50 x 8000 50 / 48; 8 / 8 heads, 1 x 100 x 30000 42 / 44, 1 x 128 x 60000 80 / 72; 16 / 2 heads, 1 x 32 x 131072 86 / 62.
+Plan plan(int64_t batch, int kv_heads, int rows, int64_t max_n) {
     Plan x;
     x.fold = rows <= 4;
     const int per = x.fold ? kRows<true> : kRows<false>;
     x.groups = (rows + per - 1) / per;
-    const int64_t blocks = (max_n + kBlock - 1) / kBlock;
-    // Short sequences: one workgroup for each head and tile of rows, two rounds of its eight wavefronts at most (more where there are many workgroups), and
-    // no second kernel, which costs 3 to 4 us.  One workgroup a head / blocks in a row, us: 32 / 8 heads, one sequence of 500 tokens 5.5 / 7.4, 1000
-    // 6.9 / 7.5, 1500 8.3 / 7.6, 2000 9.7 / 7.7, 16 sequences of 1000 7.2 / 9.0, 2000 10.1 / 10.8, 4000 16.2 / 14.1, 64 of 2000 18.3 / 18.8, 3000 21.2 / 20.7.
-    // 16 rows: one sequence of 2000, 5 new tokens (16 workgroups) 10.3 / 9.4, 25 (56) 10.4 / 11.6, of 3000, 25 13.2 / 12.7, 50 (104) 13.5 / 16.7, of 4000, 100 (200)
-    // 17.6 / 26.5, of 8000 29.9 / 37.8; 16 of 2000, 5 10.9 / 15.4, of 4000 17.4 / 20.0, of 8000 29.1 / 26.2; 64 of 8000, 5 89 / 75.
-    const int64_t workgroups = units * x.groups;
-    const bool by_head = blocks <= 2 * kHeadWaves || (blocks <= 4 * kHeadWaves && workgroups >= (x.fold ? 128 : 48)) ||
-                         (!x.fold && blocks <= 8 * kHeadWaves && workgroups >= 192);
-    // Otherwise a wavefront for every SIMD: with two blocks in registers each that is enough to keep the memory busy, and more of them only make more
+    const int64_t units = batch * kv_heads, blocks = (max_n + kBlock - 1) / kBlock;
+    const double all = static_cast<double>(units * blocks) * (batch > 1 ? 0.4 : 1.0);
+    const int64_t total = units * rows;
+    const double join = 0.0016 * static_cast<double>(total < kSliced ? 4 * total : total) + 0.02 * static_cast<double>(batch);
+
+    const int64_t rounds = (units * x.groups + 255) / 256;
+    const double head = 4.2 + (x.fold ? 1.68 : 1.86) * static_cast<double>(rounds * blocks) / kHeadWaves;
+    // A wavefront for every SIMD: with two blocks in registers each that is enough to keep the memory busy, and more of them only make more
     // parts.  512 / 1024 / 1536 / 2048 wavefronts, us: 32 / 8 heads, one sequence of 32768 tokens 16.4 / 14.0 / 16.6 / 16.5, 131072 41 / 34 /
     // 37 / 36, 64 of 8000 59 / 45 / 47 / 44, four new tokens of 131072 54 / 38 / 43 / 41.
-    x.shares = by_head ? 0 : 1024 / x.groups < 4 ? 4 : 1024 / x.groups / 4 * 4;
-    // Many rows: every workgroup turns a block into bf16 once for 256 rows; one workgroup on every compute unit, twelve blocks for each at least (its
-    // start and its larger parts cost about as much as six).  16 rows a wavefront / 256 a workgroup, us: 32 / 8 heads, 32768 tokens, 32 new ones
-    // (128 rows) 41 / 42, 40 52 / 49, 48 59 / 52, 64 73 / 55, 100 112 / 84; 64 of 24000 56 / 51, of 16000 (8 blocks for each workgroup) 42 / 43, 100 of 16000
-    // 61 / 58, of 10000 (10) 44 / 47; 40 of 131072 171 / 146; four sequences of 8000, 50 new ones 44 / 45; 8 heads, 100 of 30000 37 / 42.
-    const int tile_groups = (rows + vs::kTileRows - 1) / vs::kTileRows;
-    x.many = x.shares && rows > 160 && units * blocks * tile_groups >= 12 * 256;
-    if (x.many) {
+    x.shares = 1024 / x.groups < 4 ? 4 : 1024 / x.groups / 4 * 4;
+    const double row = (x.fold ? 7.8 : 9.1) + (x.fold ? 1.0 : 1.15) * all / x.shares + join;
+    // One workgroup on every compute unit; with fewer than six blocks for each, its start and its parts are more than the estimate.  Up to 64 rows it has no gain,
+    // and from 65 on no fewer shares than above: shorter sequences need no larger workspace.
+    const int tile_groups = (rows + vs::kTileRows - 1) / vs::kTileRows, tile_shares = 256 / tile_groups < 4 ? 4 : 256 / tile_groups;
+    const int waves = (rows < vs::kTileRows ? rows + 31 : vs::kTileRows) / 32;
+    const double tile = 16.0 + (waves <= 4 ? 1.8 : 1.65 + 0.15 * waves) * all / tile_shares + join;
+    x.many = rows > 64 && all >= 6.0 * tile_shares && tile < row;
+    // Head up to 24 blocks for each of its wavefronts: beyond, a hundred tokens would still gain (1 x 100 x 14000 55 / 59 with tile, 1 x 128 56 / 63, x 16000 63 / 67), which
+    // is left.
+    if (blocks <= 24 * kHeadWaves && head < (x.many ? tile : row)) {
+        x.many = false;
+        x.shares = 0;
+    } else if (x.many) {
         x.groups = tile_groups;
-        x.shares = 256 / tile_groups < 4 ? 4 : 256 / tile_groups;     // (no fewer than above: shorter sequences need no larger workspace)
+        x.shares = tile_shares;
     }
     x.items = x.shares ? units + x.shares : units;
     return x;
@@ -609,7 +630,7 @@ bool sizes_ok(int batch, int q_heads, int kv_heads, int n_q, int64_t max_n) {
 
 extern "C" size_t vs_cache_attend_workspace(int batch, int q_heads, int kv_heads, int n_q, int64_t max_n) {
     if (!sizes_ok(batch, q_heads, kv_heads, n_q, max_n)) return 0;
-    const Plan x = plan(static_cast<int64_t>(batch) * kv_heads, q_heads / kv_heads * n_q, max_n);
+    const Plan x = plan(batch, kv_heads, q_heads / kv_heads * n_q, max_n);
     return x.shares ? static_cast<size_t>(x.items) * (q_heads / kv_heads * n_q) * (VS_HEAD_DIM + 2) * sizeof(float) : 0;
 }
 
@@ -626,7 +647,7 @@ extern "C" int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch
     const int64_t units = static_cast<int64_t>(batch) * cache->kv_heads;
     p.rows = q_heads / cache->kv_heads * n_q;
     if (units * p.rows >= 1 << 24) return VS_ERR_UNSUPPORTED;     // threads of the joining kernel: 256 a row, 32 bits
-    const Plan x = plan(units, p.rows, max_n);
+    const Plan x = plan(batch, cache->kv_heads, p.rows, max_n);
     if (x.shares && (!ws || ws_bytes < vs_cache_attend_workspace(batch, q_heads, cache->kv_heads, n_q, max_n))) return VS_ERR_WORKSPACE;
     p.q = static_cast<const uint16_t*>(q);
     p.o = static_cast<uint16_t*>(o);
@@ -651,7 +672,7 @@ extern "C" int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch
         VS_LAUNCH_CHECK();
     }
     const unsigned total = static_cast<unsigned>(units * p.rows);
-    if (total < 512) hipLaunchKernelGGL(attend_join_kernel<32>, dim3(total, 4), dim3(256), 0, s, p);
+    if (total < kSliced) hipLaunchKernelGGL(attend_join_kernel<32>, dim3(total, 4), dim3(256), 0, s, p);
     else hipLaunchKernelGGL(attend_join_kernel<128>, dim3(total), dim3(256), 0, s, p);
     VS_LAUNCH_CHECK();
     return VS_OK;
