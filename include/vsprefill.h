@@ -340,6 +340,7 @@ int vs_rope_frequencies(double theta_base, int rot_dim, int scaling, double fact
  *   q_out [batch, q_heads, rows, 128], k_out, v_out [batch, kv_heads, rows, 128] bf16.  An output may be its own input where both
  *               have the same layout; otherwise they must not overlap.
  *   eps         FLT_MIN .. 1 (ignored without w_q and w_k);  pos0 + rows at most 2^31
+ *   rows        at most 2^20, batch at most 65535, batch * rows at most 2^26, heads at most 4096 (VS_ERR_UNSUPPORTED beyond)
  * Arithmetic: angles reduced in fp64, sine, cosine, norm and rotation in fp32, one rounding to bf16: before it within 2^-19 of magnitude
  * (|a| + |b|) where |position * freq| < 2^31 (freq <= 1 at every position; larger angles lose 3 * 2^-53 of themselves more).
  */
@@ -376,7 +377,7 @@ size_t vs_cache_bytes(int64_t pages, int kv_heads, int page_size);
  *   lens   [batch] int32 (device), values outside [0, max_n] count as the nearer end; NULL: every sequence holds max_n tokens
  *   max_n  bound of lens that the host knows, at most max_pages * page_size
  * Entries of the table that name no page (outside [0, pages)) are legal: their tokens are not written, not read and not attended to.
- * Sequences may share pages that are only read; no page may be written for two sequences in one call.
+ * Sequences may share pages that are only read; no page may be written for two sequences in one call, nor for two parts of one.
  *
  * Writes the last `rows` tokens of each sequence; rows of negative position are skipped and all other tokens keep what they hold.
  *   k, v  [batch, kv_heads, rows, 128] bf16 (k carries RoPE)
@@ -399,8 +400,10 @@ int vs_cache_read(const vs_cache_t* cache, int batch, int64_t rows, const int32_
  * A row without a key (negative position, idle slot, missing pages only) gives zeros and lse = -inf.  Longer chunks: vs_cache_read, then
  * vs_sparse_prefill_chunk or vs_dense_prefill_chunk.
  * Arithmetic: K and V are exact in bf16; bf16 MFMA, fp32 accumulation and softmax, P as two bf16 terms (2^-15 of a weight; the output's own
- * rounding is 2^-8).  The same call always gives the same bits.  A score has to lie within fp32's range, and so do sums of V times weights of up to 2^8 (they do for |V| < 2^96).
- * At most 2^24 - 1 rows in a call (batch * q_heads * n_q).  Workspace: vs_cache_attend_workspace; the answer for max_n is enough for every smaller max_n of the same call.
+ * rounding is 2^-8).  The same call always gives the same bits.  A key whose weight is below 2^-126 of the row's largest counts as zero, and one whose weight
+ * times V is far below the others' may lose up to 2^-107 (in the units of V).
+ * A score has to lie within fp32's range, and so do sums of V times weights of up to 2^8 (they do for |V| < 2^96).
+ * At most 4096 query heads and 2^24 - 1 rows in a call (batch * q_heads * n_q).  Workspace: vs_cache_attend_workspace; the answer for max_n is enough for every smaller max_n of the same call.
  */
 #define VS_CACHE_MAX_NEW 128
 size_t vs_cache_attend_workspace(int batch, int q_heads, int kv_heads, int n_q, int64_t max_n);

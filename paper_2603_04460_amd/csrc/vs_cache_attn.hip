@@ -10,8 +10,8 @@
 // sequences of 20011 20.0 and 21.9).
 // A word of V codes is eight keys of one channel and each key has its own scale, so V's scales go to the weights instead: P's terms times
 // the scale (a power of two: no rounding), one set per 32 channels.  As exponents of bf16 numbers that is a subtraction for two
-// weights, of words that the wavefront makes in LDS once a block (five tokens of four sequences of 20011 22.9 -> 20.3 us against words made by every
-// lane for itself, 16 rows of 131072 39 -> 36, 64 rows of 32768 30 -> 26).
+// weights, of words that the wavefront makes in LDS once a block (with weights of one term, five tokens of four sequences of 20011 22.9 -> 20.3 us against
+// words made by every lane for itself, 16 rows of 131072 39 -> 36, 64 rows of 32768 30 -> 26).
 //   up to four query rows of a KV head (FOLD): the 16 columns are four rows x four channel groups; every column has its group's
 //     weights, and of each output tile the columns of its group count
 //   more: 16 rows a tile, four sets of weights
@@ -20,8 +20,8 @@
 //   attend_head_kernel  short sequences: eight wavefronts share a head's keys and add up in LDS
 //   attend_row_kernel   all blocks of all heads and sequences in a row, divided evenly among the wavefronts of the GPU whatever the sequences'
 //                       lengths (which only the GPU knows); attend_join_kernel adds the parts up
-// Bound by the memory for few rows: 136 bytes a key and KV head.  32 / 8 heads, one token of 131072 33 us (142 MB; a plain read of as much
-// 24), of which the loop over the blocks 23, its slowest wavefront 26, the start 2 and the second kernel 5.
+// Bound by the memory for few rows: 136 bytes a key and KV head.  32 / 8 heads, one token of 131072 34 us (142 MB; a plain read of as much
+// 24): 28 to 29.7 of them the first kernel, with a start of 2, then the second kernel and the gap in front of it.
 #include "vs_cache_attend.h"
 
 namespace {
@@ -598,7 +598,7 @@ Plan plan(int64_t batch, int kv_heads, int rows, int64_t max_n) {
     const int64_t rounds = (units * x.groups + 255) / 256;
     const double head = 4.2 + (x.fold ? 1.68 : 1.86) * static_cast<double>(rounds * blocks) / kHeadWaves;
     // A wavefront for every SIMD: with two blocks in registers each that is enough to keep the memory busy, and more of them only make more
-    // parts.  512 / 1024 / 1536 / 2048 wavefronts, us: 32 / 8 heads, one sequence of 32768 tokens 16.4 / 14.0 / 16.6 / 16.5, 131072 41 / 34 /
+    // parts.  512 / 1024 / 1536 / 2048 wavefronts (weights of one term), us: 32 / 8 heads, one sequence of 32768 tokens 16.4 / 14.0 / 16.6 / 16.5, 131072 41 / 34 /
     // 37 / 36, 64 of 8000 59 / 45 / 47 / 44, four new tokens of 131072 54 / 38 / 43 / 41.
     x.shares = 1024 / x.groups < 4 ? 4 : 1024 / x.groups / 4 * 4;
     const double row = (x.fold ? 7.8 : 9.1) + (x.fold ? 1.0 : 1.15) * all / x.shares + join;

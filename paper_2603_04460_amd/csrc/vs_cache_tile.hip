@@ -8,10 +8,11 @@
 // The codes of the block after next are on their way into registers while one block is worked on and the next one's are written to the other
 // buffer: one barrier a block.
 // P goes into the second product as two bf16 terms, which read the same operand of V (see vs_cache_attn.hip): 84 us with one term, 97 with two.
-// 32 / 8 heads, 32768 tokens, 100 new ones (400 rows) 84 us (54 Gflop: 640 TFLOP/s), 64 55 (with 16 rows a wavefront and every wavefront turning its
-// blocks into bf16 for itself 112 and 73).  A block takes about 5500 clocks, of which the two products take 1100 each (the matrix unit is busy throughout), the
-// softmax 800 to 1000 and the turning into bf16 1700 to 2200.  The two wavefronts of a SIMD in opposite orders (one turns while the other multiplies) 94,
-// 64 rows a wavefront, four wavefronts 114: not taken.
+// 32 / 8 heads, 32768 tokens, 100 new ones (400 rows) 97 us (54 Gflop, 81 with the second terms: 830 TFLOP/s), 64 62 (with 16 rows a wavefront and every
+// wavefront turning its blocks into bf16 for itself 135 and 87).  A block takes about 6400 clocks: 5500 with one term (the two products 1100 each, the
+// softmax 800 to 1000, the turning into bf16 1700 to 2200), 900 more for the second terms; the matrix unit is busy for 40 % of the kernel.  With one term: the two wavefronts of a SIMD in opposite orders (one turns
+// while the other multiplies) 94 against 91, 64 rows a wavefront, four wavefronts 114; with two: the second terms of four channels' tiles behind their first 98, each 16 keys' weights
+// evaluated in front of their products 100, the reads of V's operands left to the compiler 102: not taken.
 #include "vs_cache_attend.h"
 
 namespace {
