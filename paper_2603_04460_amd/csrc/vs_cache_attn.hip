@@ -582,6 +582,9 @@ struct Plan {
 // 64 x 1 x 2000 20.1 / 19.6, 3000 23.2 / 22.1, 4 heads on one, 64 x 1 x 1500 9.1 / 9.1, 200 10.3 / 15.3, 300 14.7 / 18.0; 1 x 5 x 1000 7.9 / 8.8, 1500 9.7 / 9.2, 2000 11.5 / 9.7, 4 x 5 x 1500 9.7 / 9.7, 2000 11.6 / 10.8, 16 x 5 x 4000 20.1 / 20.9, 6000 27.1 / 23.3,
 // 64 x 5 x 2000 33 / 38, 4000 59 / 61, 8000 99 / 82; 1 x 25 x 2000 11.8 / 12.2, 3000 15.5 / 13.4, 1 x 50 x 3000 15.7 / 17.7, 4000 19.4 / 19.6, 6000 26.7 / 24.1, 1 x 75 x 8000 34 / 36,
 // 1 x 100 x 4000 20 / 29, 8000 34 / 42, 12000 48 / 59; 4 x 25 x 4000 19.5 / 20.5, 6000 27 / 21, 16 x 16 x 4000 36 / 36, 8000 53 / 44, 4 x 50 x 2000 22 / 24, 4000 37 / 31.
+// Batches whose sequences are all as long as the bound (only the GPU knows): 8 x 1 x 2000 11.6 / 12.2, 16 x 1 x 2000 12.2 / 14.0, 4000 19.1 / 19.7, 6000 29 / 26, 32 x 1 x 4000 31 / 36, 64 x 1 x 4000 58 / 63,
+// 16 x 5 x 4000 22 / 31, 5000 26 / 36, 6000 32 / 42, 64 x 5 x 4000 106 / 95, 4 x 25 x 4000 20 / 30, 6000 27 / 38, 4 x 50 x 4000 38 / 50: up to 45 % for the estimate's 2/5; counted full, the
+// batches above would lose as much (32 x 1 x 8000 33 / 21, 16 x 5 x 12000 48 / 34).
 // Row / tile: 1 x 24 (96 rows of a KV head) x 32768 41 / 42, 131072 130 / 128, 1 x 32 (128) x 24000 39 / 39, 32768 48 / 44, 131072 164 / 132, 1 x 40 (160) x 16000 35 / 39,
 // 24000 48 / 48, 32768 60 / 55, 131072 211 / 172, 1 x 48 x 16000 41 / 41, 24000 55 / 51, 1 x 64 x 10000 35 / 40, 16000 49 / 46, 32768 88 / 63, 1 x 100 x 16000 73 / 64, 32768 136 / 98;
 // 4 x 50 x 8000 50 / 48; 8 / 8 heads, 1 x 100 x 30000 42 / 44, 1 x 128 x 60000 80 / 72; 16 / 2 heads, 1 x 32 x 131072 86 / 62.
@@ -593,7 +596,7 @@ Plan plan(int64_t batch, int kv_heads, int rows, int64_t max_n) {
     const int64_t units = batch * kv_heads, blocks = (max_n + kBlock - 1) / kBlock;
     const double all = static_cast<double>(units * blocks) * (batch > 1 ? 0.4 : 1.0);
     const int64_t total = units * rows;
-    const double join = 0.0016 * static_cast<double>(total < kSliced ? 4 * total : total) + 0.02 * static_cast<double>(batch);
+    const double join = 0.0016 * static_cast<double>(total < kSliced ? 4 * total : total) + 1.3 * static_cast<double>((batch - 1) / 64);
 
     const int64_t rounds = (units * x.groups + 255) / 256;
     const double head = 4.2 + (x.fold ? 1.68 : 1.86) * static_cast<double>(rounds * blocks) / kHeadWaves;
@@ -601,7 +604,7 @@ Plan plan(int64_t batch, int kv_heads, int rows, int64_t max_n) {
     // parts.  512 / 1024 / 1536 / 2048 wavefronts (weights of one term), us: 32 / 8 heads, one sequence of 32768 tokens 16.4 / 14.0 / 16.6 / 16.5, 131072 41 / 34 /
     // 37 / 36, 64 of 8000 59 / 45 / 47 / 44, four new tokens of 131072 54 / 38 / 43 / 41.
     x.shares = 1024 / x.groups < 4 ? 4 : 1024 / x.groups / 4 * 4;
-    const double row = (x.fold ? 7.8 : 9.1) + (x.fold ? 1.0 : 1.15) * all / x.shares + join;
+    const double row = (x.fold ? 7.8 + 0.006 * static_cast<double>(units) : 9.1) + (x.fold ? 1.0 : 1.15) * all / x.shares + join;
     // One workgroup on every compute unit; with fewer than six blocks for each, its start and its parts are more than the estimate.  Up to 64 rows it has no gain,
     // and from 65 on no fewer shares than above: shorter sequences need no larger workspace.
     const int tile_groups = (rows + vs::kTileRows - 1) / vs::kTileRows, tile_shares = 256 / tile_groups < 4 ? 4 : 256 / tile_groups;

@@ -42,9 +42,9 @@ def form(batch, hq, hk, n_q, n):
 
 
 @pytest.mark.parametrize("batch, hq, hk, n_q, n, want", [
-    # timed in each form; the faster by a tenth and more
+    # timed in each form; the faster by a tenth and more (16 sequences of 2000: where they are equally long)
     (1, 32, 8, 1, 500, "head"), (1, 32, 8, 1, 1500, "row"), (12, 32, 8, 1, 1500, "head"), (32, 32, 8, 1, 2000, "head"), (64, 32, 8, 1, 4000, "row"),
-    (300, 4, 1, 1, 1500, "head"), (48, 4, 1, 1, 2000, "row"), (1, 32, 8, 5, 1000, "head"), (1, 32, 8, 5, 2000, "row"), (16, 32, 8, 5, 2000, "head"),
+    (300, 4, 1, 1, 1500, "head"), (16, 32, 8, 1, 2000, "head"), (48, 4, 1, 1, 2000, "row"), (1, 32, 8, 5, 1000, "head"), (1, 32, 8, 5, 2000, "row"), (16, 32, 8, 5, 2000, "head"),
     (16, 32, 8, 5, 8000, "row"), (64, 32, 8, 5, 2000, "head"), (64, 32, 8, 5, 8000, "row"), (1, 32, 8, 50, 3000, "head"), (1, 32, 8, 50, 6000, "row"),
     (1, 32, 8, 100, 8000, "head"), (1, 32, 8, 100, 10000, "head"), (1, 32, 8, 100, 16000, "tile"), (1, 32, 8, 64, 10000, "row"), (1, 32, 8, 64, 24000, "tile"),
     (1, 32, 8, 40, 16000, "row"), (1, 32, 8, 40, 131072, "tile"), (1, 32, 8, 32, 131072, "tile"), (1, 32, 8, 16, 131072, "row"), (4, 32, 8, 25, 6000, "row"),
