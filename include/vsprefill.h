@@ -297,7 +297,7 @@ int vs_sparse_prefill_counters(const void* ws, size_t ws_bytes, void* stream, in
 /*
  * ---- Around the prefill: from a layer's projection to the calls above, and single tokens after the prompt ----
  *
- * One convention holds for the four calls below: `lens` [batch] int32 (device) is the number of tokens that each sequence
+ * One convention holds for the calls below: `lens` [batch] int32 (device) is the number of tokens that each sequence
  * holds, the new ones among them, and a call's `rows` (or n_q) rows of a sequence are its LAST tokens: row r is position
  * lens[b] - rows + r.  One array serves a whole decoding step; a slot with lens 0 is idle; a batch of prompts of different
  * lengths is padded in front (rows of negative position have no token).  `lens` and page tables may begin at any element of an
@@ -373,7 +373,7 @@ typedef struct {
 size_t vs_cache_bytes(int64_t pages, int kv_heads, int page_size);
 
 /*
- * Shared by the three calls on a cache:
+ * Shared by the calls on a cache:
  *   lens   [batch] int32 (device), values outside [0, max_n] count as the nearer end; NULL: every sequence holds max_n tokens
  *   max_n  bound of lens that the host knows, at most max_pages * page_size
  * Entries of the table that name no page (outside [0, pages)) are legal: their tokens are not written, not read and not attended to.
@@ -397,8 +397,8 @@ int vs_cache_read(const vs_cache_t* cache, int batch, int64_t rows, const int32_
  * Attention of the last n_q tokens (1 .. VS_CACHE_MAX_NEW) of each sequence over the cache, which already holds them:
  *     o[b, h, r] = sum_j softmax_j(scale * q[b, h, r] . K_j) V_j  over  j <= lens[b] - n_q + r.
  *   q, o  [batch, q_heads, n_q, 128] bf16 (not overlapping);  lse [batch, q_heads, n_q] fp32 out or NULL
- * A row without a key (negative position, idle slot, missing pages only) gives zeros and lse = -inf.  Longer chunks: vs_cache_read, then
- * vs_sparse_prefill_chunk or vs_dense_prefill_chunk.
+ * A row without a key (negative position, idle slot, missing pages only) gives zeros and lse = -inf.  Longer chunks: vs_cache_prefill, or vs_cache_read and then
+ * vs_sparse_prefill_chunk.
  * Arithmetic: K and V are exact in bf16; bf16 MFMA, fp32 accumulation and softmax, P as two bf16 terms (2^-15 of a weight; the output's own
  * rounding is 2^-8).  The same call always gives the same bits.  A key whose weight is below 2^-126 of the row's largest counts as zero, and one whose weight
  * times V is far below the others' may lose up to 2^-107 (in the units of V).
@@ -410,6 +410,62 @@ size_t vs_cache_attend_workspace(int batch, int q_heads, int kv_heads, int n_q, 
 
 int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch, int q_heads, int n_q, const int32_t* lens, int64_t max_n,
                     float scale, void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The same attention for any number of new tokens (1 .. VS_MAX_SEQ), a chunk of a prompt for instance; sequences of a batch may differ in length, prompts shorter
+ * than n_q are padded in front.  Layouts, masks, rows without a key and missing pages as for vs_cache_attend, which takes calls of up to
+ * VS_CACHE_MAX_NEW rows.
+ * Arithmetic of more rows: K is exact in bf16, V in fp16 in units of the largest scale so far of its 32 channels (what is below 2^-27 of that, and groups that are not
+ * finite, goes through fp32), P in fp16 (11 significant bits), fp32 accumulation and softmax.  The same call always gives the same bits.
+ * A key whose weight is below 2^-31 of the row's largest counts as zero in the output, V below 2^-126 of the largest of its 32 channels, too.  Scores have to lie
+ * within fp32's range, and V within 2^96.  At most 4096 query heads.  Workspace: vs_cache_prefill_workspace; the answer for max_n is enough for every smaller max_n of the same call.
+ */
+size_t vs_cache_prefill_workspace(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n);
+
+int vs_cache_prefill(const void* q, const vs_cache_t* cache, int batch, int q_heads, int64_t n_q, const int32_t* lens, int64_t max_n,
+                     float scale, void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The weight that each held token gets from the last n_q tokens' queries (1 .. VS_MAX_SEQ), added to what it had:
+ *     weights[b, g, j] = decay * old[b, g, j] + sum over the query heads h of KV head g and the rows r that see j, j <= lens[b] - n_q + r, of
+ *                        exp(scale * q[b, h, r] . K_j - lse[b, h, r])
+ * for j < lens[b]; entries behind stay as they are.  The last `fresh` tokens have no weight yet: what `old` holds for them is not read
+ * (fresh = n_q in a decoding step or a chunk, whose own tokens are the new ones; max_n or old = NULL to begin anew).
+ *   q       [batch, q_heads, n_q, 128] bf16;  lse [batch, q_heads, n_q] fp32, as vs_cache_attend or vs_cache_prefill left it for the same rows
+ *   old     [batch, kv_heads, stride] fp32 or NULL (zeros); may be `weights`, must not overlap it otherwise
+ *   decay   0 .. 1; with 0 `old` is not read
+ *   weights [batch, kv_heads, stride] fp32 out, stride >= max_n
+ * A row without a key (lse = -inf) adds nothing.  A token of a missing page gets nothing and keeps decay * old.  scale * log2(e) has to be a normal fp32 number.
+ * Arithmetic: K is exact in bf16; bf16 MFMA, fp32 exponentials and sums in a fixed order: the same call always gives the same bits.
+ * At most 4096 query heads and 2^30 - 1 rows of a KV head (q_heads / kv_heads * n_q).  Workspace: vs_cache_weigh_workspace; the answer for max_n is enough for every smaller max_n of the same call.
+ */
+size_t vs_cache_weigh_workspace(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n);
+
+int vs_cache_weigh(const void* q, const float* lse, const vs_cache_t* cache, int batch, int q_heads, int64_t n_q, const int32_t* lens,
+                   int64_t max_n, float scale, const float* old, float decay, int64_t fresh, float* weights, int64_t stride, void* ws,
+                   size_t ws_bytes, void* stream);
+
+/*
+ * Eviction: of each sequence and KV head `keep` tokens stay, in their order, as the tokens 0 .. of the same cache or of another one.  The first n_sink
+ * and the last n_recent stay in any case, then those with the largest weights, of equal ones the first (NaN is below every number, the two zeros are
+ * equal).  Tokens of missing pages do not stay: min(keep, tokens that are there) tokens of every head remain, all of them where that is no more than keep.
+ * Codes and scales are moved as they are.  Positions are baked into K: tokens that come later are rotated by their own position (lens of
+ * vs_qk_norm_rope: tokens seen), not by their place in the cache (lens of the calls on the cache: tokens held).
+ *   weights      [batch, kv_heads, stride] fp32, stride >= max_n, e.g. vs_cache_weigh's
+ *   keep         1 .. VS_MAX_SEQ, at most to->max_pages * page_size;  n_sink + n_recent <= keep
+ *   to           where the tokens go (kv_heads as in `cache`, any page size); NULL: the same cache.  Its pages that take tokens must belong to one sequence only,
+ *                and where `to` is another cache in the same memory not to `cache`'s sequences.  Tokens whose page is missing in `to` are lost; what
+ *                `to` holds behind the last token stays.
+ *   weights_out  [batch, kv_heads, stride_out] fp32 out: weights of the tokens that stay, stride_out >= keep; NULL, or `weights` with the same stride
+ *   kept         [batch, kv_heads, keep] int32 out or NULL: their numbers, ascending, -1 behind them
+ *   lens_out     [batch] int32 out: tokens that each sequence then holds; may be `lens`
+ * Workspace: vs_cache_evict_workspace.
+ */
+size_t vs_cache_evict_workspace(int batch, int kv_heads, int64_t max_n, int64_t keep);
+
+int vs_cache_evict(const vs_cache_t* cache, const float* weights, int64_t stride, int batch, const int32_t* lens, int64_t max_n, int64_t keep,
+                   int64_t n_sink, int64_t n_recent, const vs_cache_t* to, float* weights_out, int64_t stride_out, int32_t* kept,
+                   int32_t* lens_out, void* ws, size_t ws_bytes, void* stream);
 
 const char* vs_strerror(int status);
 int vs_last_hip_error(void);

@@ -17,7 +17,8 @@ EXPORTS = [
     "vs_sparse_prefill_tiles", "vs_sparse_prefill_counters", "vs_aggregate_workspace", "vs_aggregate",
     "vs_index_train_workspace", "vs_index_train_step",
     "vs_rope_frequencies", "vs_qk_norm_rope", "vs_cache_bytes", "vs_cache_write", "vs_cache_read", "vs_cache_attend_workspace",
-    "vs_cache_attend",
+    "vs_cache_attend", "vs_cache_prefill_workspace", "vs_cache_prefill", "vs_cache_weigh_workspace", "vs_cache_weigh", "vs_cache_evict_workspace",
+    "vs_cache_evict",
     "vs_strerror", "vs_last_hip_error", "vs_version",
 ]
 
@@ -108,6 +109,15 @@ def _load():
     L.vs_cache_attend_workspace.argtypes = [i32, i32, i32, i32, i64]
     L.vs_cache_attend_workspace.restype = sz
     L.vs_cache_attend.argtypes = [vp, vp, i32, i32, i32, vp, i64, f32, vp, vp, vp, sz, vp]
+    L.vs_cache_prefill_workspace.argtypes = [i32, i32, i32, i64, i64]
+    L.vs_cache_prefill_workspace.restype = sz
+    L.vs_cache_prefill.argtypes = [vp, vp, i32, i32, i64, vp, i64, f32, vp, vp, vp, sz, vp]
+    L.vs_cache_weigh_workspace.argtypes = [i32, i32, i32, i64, i64]
+    L.vs_cache_weigh_workspace.restype = sz
+    L.vs_cache_weigh.argtypes = [vp, vp, vp, i32, i32, i64, vp, i64, f32, vp, f32, i64, vp, i64, vp, sz, vp]
+    L.vs_cache_evict_workspace.argtypes = [i32, i32, i64, i64]
+    L.vs_cache_evict_workspace.restype = sz
+    L.vs_cache_evict.argtypes = [vp, vp, i64, i32, vp, i64, i64, i64, i64, vp, vp, i64, vp, vp, vp, sz, vp]
     L.vs_strerror.argtypes = [i32]
     L.vs_strerror.restype = ctypes.c_char_p
     L.vs_last_hip_error.restype = i32
@@ -591,3 +601,81 @@ def cache_attend(q, cache, o, max_n, lens=None, lse=None, ws=None, scale=None, s
                                              o.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream, at)),
            "vs_cache_attend")
     return o
+
+
+def cache_prefill_workspace(batch, q_heads, kv_heads, n_q, max_n):
+    return _load().vs_cache_prefill_workspace(batch, q_heads, kv_heads, n_q, max_n)
+
+
+def cache_prefill(q, cache, o, max_n, lens=None, lse=None, ws=None, scale=None, stream=None):
+    """cache_attend for any number of new tokens: a chunk of a prompt, or of several of different lengths."""
+    import torch
+    at, bf16 = torch.cuda.current_device(), torch.bfloat16
+    batch, q_heads, n_q = cache._batch(at, q, bf16, None, lens, torch.int32, "q")
+    assert _on(at, o, bf16, "o").shape == q.shape
+    if lse is not None:
+        assert _on(at, lse, torch.float32, "lse").numel() == batch * q_heads * n_q
+    if ws is not None:
+        _on(at, ws, ws.dtype, "ws")
+    _check((_lib or _load()).vs_cache_prefill(q.data_ptr(), cache._ref, batch, q_heads, n_q, _ptr(lens), max_n, 128 ** -0.5 if scale is None else scale,
+                                              o.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream, at)),
+           "vs_cache_prefill")
+    return o
+
+
+def cache_weigh_workspace(batch, q_heads, kv_heads, n_q, max_n):
+    return _load().vs_cache_weigh_workspace(batch, q_heads, kv_heads, n_q, max_n)
+
+
+def cache_weigh(q, lse, cache, weights, max_n, lens=None, old=None, decay=1.0, fresh=None, ws=None, scale=None, stream=None):
+    """weights [batch, kv_heads, >= max_n] fp32 = decay * old + what every held token gets from the queries q [batch, q_heads, n_q, 128] of
+    the last n_q tokens (or all without the batch dimension), lse [batch, q_heads, n_q] fp32 as cache_attend or cache_prefill left it.  old: as weights,
+    the same tensor or None (zeros); the last fresh tokens (None: n_q) have no weight in it yet."""
+    import torch
+    at, bf16, fp32 = torch.cuda.current_device(), torch.bfloat16, torch.float32
+    batch, q_heads, n_q = cache._batch(at, q, bf16, None, lens, torch.int32, "q")
+    assert _on(at, lse, fp32, "lse").numel() == batch * q_heads * n_q
+    stride = _on(at, weights, fp32, "weights").shape[-1]
+    assert weights.numel() == batch * cache._kv_heads * stride
+    if old is not None:
+        assert _on(at, old, fp32, "old").shape == weights.shape
+    if ws is not None:
+        _on(at, ws, ws.dtype, "ws")
+    _check((_lib or _load()).vs_cache_weigh(q.data_ptr(), lse.data_ptr(), cache._ref, batch, q_heads, n_q, _ptr(lens), max_n,
+                                            128 ** -0.5 if scale is None else scale, _ptr(old), decay, n_q if fresh is None else fresh,
+                                            weights.data_ptr(), stride, _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream, at)),
+           "vs_cache_weigh")
+    return weights
+
+
+def cache_evict_workspace(batch, kv_heads, max_n, keep):
+    return _load().vs_cache_evict_workspace(batch, kv_heads, max_n, keep)
+
+
+def cache_evict(cache, weights, max_n, keep, lens_out, lens=None, n_sink=0, n_recent=0, to=None, weights_out=None, kept=None, ws=None, stream=None):
+    """The keep tokens of each sequence and KV head with the largest weights [batch, kv_heads, >= max_n] fp32 (the first n_sink and the last n_recent
+    in any case), in their order, to the front of the cache `to` (None: the same one); lens_out [batch] int32 (may be lens): what each sequence
+    then holds, weights_out [batch, kv_heads, >= keep] (may be weights) and kept [batch, kv_heads, keep] int32: weights and numbers of what stays."""
+    import torch
+    at, int32, fp32 = torch.cuda.current_device(), torch.int32, torch.float32
+    batch, stride = _on(at, lens_out, int32, "lens_out").numel(), _on(at, weights, fp32, "weights").shape[-1]
+    for x, what in ((cache, "cache"), (to, "to")):
+        if x is not None:
+            if x._device != at:
+                raise ValueError("%s is on %s, the current device is cuda:%d" % (what, x._data.device, at))
+            assert x._batches is None or x._batches == batch
+    units = batch * cache._kv_heads
+    assert weights.numel() == units * stride
+    if lens is not None:
+        assert _on(at, lens, int32, "lens").numel() == batch
+    if weights_out is not None:
+        assert _on(at, weights_out, fp32, "weights_out").numel() == units * weights_out.shape[-1]
+    if kept is not None:
+        assert _on(at, kept, int32, "kept").numel() == units * keep
+    if ws is not None:
+        _on(at, ws, ws.dtype, "ws")
+    _check((_lib or _load()).vs_cache_evict(cache._ref, weights.data_ptr(), stride, batch, _ptr(lens), max_n, keep, n_sink, n_recent,
+                                            None if to is None else to._ref, _ptr(weights_out), 0 if weights_out is None else weights_out.shape[-1],
+                                            _ptr(kept), lens_out.data_ptr(), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream, at)),
+           "vs_cache_evict")
+    return lens_out

@@ -25,6 +25,8 @@ EXTRA_FLAGS = {
     # score and output accumulators in the registers that the conversions and the softmax use
     "vs_cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "vs_cache_tile.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "vs_cache_prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "vs_cache_weigh.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

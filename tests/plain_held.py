@@ -1,0 +1,134 @@
+"""Plain 64-bit forms of the calls on tokens that the cache holds (attention of a chunk, weights, eviction), and inputs for them."""
+import numpy as np
+import torch
+
+import paper_2603_04460_amd as vs
+
+EPS = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}     # half a step
+
+
+def ints(*x):
+    return torch.tensor(x, dtype=torch.int32).cuda()
+
+
+def normal(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed))
+
+
+def kv(seed, batch, hk, n):
+    """Keys with two large channels, values; sizes that differ from token to token."""
+    k, v = normal(seed, batch, hk, n, 128), normal(seed + 1, batch, hk, n, 128)
+    k[..., 5] *= 6.0
+    k[..., 77] *= 4.0
+    v *= torch.exp2(torch.randint(-2, 3, (batch, hk, n, 1), generator=torch.Generator().manual_seed(seed + 2)).float())
+    return k.bfloat16().cuda(), v.bfloat16().cuda()
+
+
+def filled(seed, k, v, page, spare=2, n=None):
+    """A cache of mixed-up pages, full of whatever was there before, that holds k, v [batch, hk, n, 128] from position 0 on."""
+    batch, hk, have, _ = k.shape
+    pages = -(-max(have, n or 0) // page)
+    order = np.random.default_rng(seed).permutation(batch * pages + spare)[:batch * pages]
+    table = torch.from_numpy(order.reshape(batch, pages).astype(np.int32)).cuda()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    data = torch.randint(0, 256, (batch * pages + spare, hk, page // 64, vs.CACHE_BLOCK_BYTES), generator=g, dtype=torch.uint8, device="cuda")
+    cache = vs.Cache(data, table)
+    vs.cache_write(cache, k, v, have)
+    return cache
+
+
+def held(cache, n, batch):
+    """What the cache holds, [batch, hk, n, 128] in 64 bits; zeros where there is no page."""
+    k = torch.zeros(batch, cache.kv_heads, n, 128, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    vs.cache_read(cache, k, v, n)
+    return k.double().cpu(), v.double().cpu()
+
+
+def present(cache, b, n):
+    """Which of the first n tokens of sequence b have a page."""
+    if cache.table is None:
+        return np.ones(n, dtype=bool)
+    page = cache.table[b].cpu().numpy()[np.arange(n) // cache.page_size]
+    return (page >= 0) & (page < cache.pages)
+
+
+def scores(q, k, n, there, scale):
+    """One head: q [rows, 128], k [n, 128] -> scores [rows, n], -inf where the row does not see the key, and the largest sum of |terms|."""
+    rows = q.shape[0]
+    x = q @ k.T * scale
+    seen = (torch.arange(n) <= torch.arange(n - rows, n).unsqueeze(1)) & torch.from_numpy(there)
+    size = (q.abs() @ torch.nan_to_num(k.abs(), 0, 0, 0).T * scale).max().item() if n else 0.0
+    return torch.where(seen, x, -torch.inf), seen, size
+
+
+def attention(q, cache, lens, max_n, scale=128 ** -0.5):
+    """o, lse, and how far they may be off, all float64: one rounding of the output, one of each weight (fp16), scores off by the fp32 sum of 128 products
+    and the exponential (2^-17 of the sum of |terms|), the running maximum's rounding; weights below 2^-31 of the largest count as zero."""
+    batch, hq, rows, _ = q.shape
+    hk = cache.kv_heads
+    k, v = held(cache, max_n, batch)
+    q = q.double().cpu()
+    o, lse = torch.zeros(batch, hq, rows, 128, dtype=torch.float64), torch.full((batch, hq, rows), -torch.inf, dtype=torch.float64)
+    tol_o, tol_lse = torch.zeros_like(o), torch.zeros_like(lse)
+    for b, n in enumerate(lens):
+        there = present(cache, b, n)
+        for h in range(hq if n else 0):
+            g = h // (hq // hk)
+            x, seen, size = scores(q[b, h], k[b, g, :n], n, there, scale)
+            some = seen.any(1)
+            top = torch.where(some, x.nan_to_num(0, 0, -1e300).max(1).values, 0.0)
+            p = torch.where(seen, torch.exp(x - top.unsqueeze(1)), 0.0)
+            total = p.sum(1)
+            w = v[b, g, :n]
+            bad = ~torch.isfinite(w)
+            y = p @ torch.where(bad, 0.0, w)
+            mass = p @ torch.where(bad, 0.0, w).abs()
+            poisoned = (seen.double() @ bad.double()) > 0
+            off = 2.0 ** -17 * size + 2.0 ** -20
+            at = (b, h, some)
+            t = total[some].unsqueeze(1)
+            o[at] = torch.where(poisoned, torch.nan, y / total.unsqueeze(1))[some]
+            lse[at] = (top + total.log())[some]
+            tol_o[at] = ((1 + 2.0 ** -7) * (2.0 ** -8 * (y[some] / t).abs() + (2.0 ** -11 + 2 * off) * mass[some] / t)
+                         + n * 2.0 ** -31 * torch.where(bad, 0.0, w).abs().max(0).values / t)
+            tol_lse[at] = off + 2.0 ** -22 * lse[at].abs()
+    return o, lse, tol_o, tol_lse
+
+
+def weights(q, lse, cache, lens, max_n, old, decay, fresh, scale=128 ** -0.5):
+    """weights and how far they may be off: the exponents by 2^-17 of the sum of |terms| and 2^-22 of lse, the fp32 sums."""
+    batch, hq, rows, _ = q.shape
+    hk = cache.kv_heads
+    k, _ = held(cache, max_n, batch)
+    q, lse = q.double().cpu(), lse.double().cpu()
+    out = torch.zeros(batch, hk, max_n, dtype=torch.float64)
+    tol = torch.zeros_like(out)
+    for b, n in enumerate(lens):
+        there = present(cache, b, n)
+        for g in range(hk if n else 0):
+            if old is not None and decay:
+                out[b, g, :max(0, n - fresh)] = old[b, g, :max(0, n - fresh)].double().cpu() * decay
+            for h in range(g * (hq // hk), (g + 1) * (hq // hk)):
+                x, seen, size = scores(q[b, h], k[b, g, :n], n, there, scale)
+                l = lse[b, h].unsqueeze(1)
+                p = torch.where(seen & (l != -torch.inf), torch.exp(x - l), 0.0)
+                out[b, g, :n] += p.sum(0)
+                tol[b, g, :n] += (p * (2.0 ** -17 * size + 2.0 ** -20 + 2.0 ** -22 * torch.where(torch.isfinite(l), l.abs(), 0.0))).sum(0)
+            tol[b, g, :n] += (hq // hk * rows + 2) * 2.0 ** -24 * out[b, g, :n].abs() + 2.0 ** -126 * hq * rows
+    return out, tol
+
+
+def order(w):
+    """A weight's place: NaN below all, one zero."""
+    return -np.inf if np.isnan(w) else w + 0.0
+
+
+def stays(weights, there, keep, n_sink, n_recent):
+    """Numbers of the tokens that stay, ascending, in plain Python."""
+    n = len(weights)
+    tokens = [j for j in range(n) if there[j]]
+    always = [j for j in tokens if j < n_sink or j >= n - n_recent]
+    # NaN below -inf: a second place in the order
+    others = sorted((j for j in tokens if n_sink <= j < n - n_recent), key=lambda j: (np.isnan(weights[j]), -order(weights[j]), j))
+    return sorted(always + others[:max(0, min(keep, len(tokens)) - len(always))])[:keep]
