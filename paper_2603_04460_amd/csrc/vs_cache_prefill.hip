@@ -20,12 +20,17 @@ typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kUnitRows = 256;
-constexpr int kTileBytes = kBlock * 256;                   // K or V of a block in 16 bits
 constexpr float kGrown = 8.0f;                             // log2 units by which a score may exceed the running maximum
 constexpr float kLift = 7.0f;                              // weights are held times 2^7
+constexpr float kGrownSum = 32768.0f;                      // 2^(8 + 7): no weight of a lane is larger if their sum is not
+constexpr float kSafe = 1024.0f;                           // scores (log2 units) up to which a product and a difference in one rounding are good enough
+constexpr int kShares = 256;                               // a workgroup for every compute unit
+constexpr int kStart = 3;                                  // steps that a unit's start and end count for
+constexpr int kSteps = 4;                                  // of a workgroup, if there are so few
 constexpr int kTop = 13;                                   // fp16 exponent of a code with E = R: 6 * 2^13 < 65504
 constexpr int kSpan = 27;                                  // E from R - 27 (2^-14 in fp16) to R
 
@@ -34,10 +39,110 @@ struct PrefillParams {
     const uint16_t* q;
     uint16_t* o;
     float* lse;
-    int q_heads, n_q, group, hc, tok;      // tok: tokens of a unit, 256 / hc
-    int tiles;                             // units of a head chunk
+    float* part;                           // [2 shares][256 rows][128] sums, then [2 shares][256] (maximum, sum of weights)
+    int batch, q_heads, n_q, group, hc;
+    int tok, tok_blocks;                   // tokens of a unit, 256 / hc, and that in blocks
+    int tiles;                             // units of a sequence's head chunk
+    int heads;                             // head chunks of a sequence: kv_heads * group / hc
+    int shares;
     float c;                               // scale * log2(e)
 };
+
+// ---- the work of a call in a row: steps by sequence, head chunk, unit, block, which the workgroups divide evenly ----
+// A unit of sequence b has kStart steps in front (its start and end cost as much) and one for each block up to its last row's position.
+struct Sequence {
+    int len, base, first;                  // base: position of row 0;  first: blocks up to row 0, may be negative
+    __device__ __forceinline__ Sequence(const PrefillParams& p, int b, bool scalar) {
+        len = b < p.batch ? (scalar ? cache_length_scalar(p.cache, b) : cache_length(p.cache, b)) : 0;
+        base = len - p.n_q;
+        first = (base + kBlock - 1) >> 6;
+    }
+    __device__ __forceinline__ int blocks(const PrefillParams& p, int tile) const {
+        return max(tile + 1 < p.tiles ? first + (tile + 1) * p.tok_blocks : (len + kBlock - 1) >> 6, 0);
+    }
+    // steps of the units in front of `tile` (tile < tiles: none of them is the last one)
+    __device__ __forceinline__ int64_t before(const PrefillParams& p, int tile) const {
+        const int64_t z = min(max(-first, 0) / p.tok_blocks, tile), t = tile;      // units that end in front of position 0
+        return kStart * t + (t - z) * first + p.tok_blocks * ((t * (t + 1) - z * (z + 1)) >> 1);
+    }
+    __device__ __forceinline__ int64_t steps(const PrefillParams& p) const { return before(p, p.tiles - 1) + kStart + blocks(p, p.tiles - 1); }
+};
+
+__device__ __forceinline__ int64_t scan64(int64_t x, int lane) {
+    for (int d = 1; d < 64; d *= 2) {
+        const int64_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
+    return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+struct Place {
+    int b, head, tile, step, blocks;       // head: of the sequence's head chunks;  step: of the unit, which has kStart + blocks
+    int len, base;
+    __device__ __forceinline__ void next(const PrefillParams& p) {                 // the unit behind this one
+        step = 0;
+        if (++tile == p.tiles) {
+            tile = 0;
+            if (++head == p.heads) {
+                head = 0;
+                ++b;
+            }
+        }
+        enter(p);
+    }
+    __device__ __forceinline__ void enter(const PrefillParams& p) {
+        const Sequence s(p, b, true);
+        len = s.len;
+        base = s.base;
+        blocks = s.blocks(p, tile);
+    }
+};
+
+// Steps of a share, and where share `share` begins (false: behind the end).
+__device__ __forceinline__ bool find(const PrefillParams& p, int share, int lane, int64_t* per, int64_t* total, Place* at) {
+    int64_t all = 0;
+    for (int b = 0; b < p.batch; b += 64) {
+        const int64_t mine = b + lane < p.batch ? Sequence(p, b + lane, false).steps(p) : 0;
+        all += uniform64(__shfl(scan64(mine, lane), 63));
+    }
+    all *= p.heads;
+    *total = all;
+    *per = (all + p.shares - 1) / p.shares;
+    int64_t x = *per * share;
+    if (x >= all) return false;
+    for (int b = 0;; b += 64) {
+        const int64_t mine = b + lane < p.batch ? Sequence(p, b + lane, false).steps(p) * p.heads : 0;
+        const int64_t upto = scan64(mine, lane);
+        const int l = __popcll(__ballot(upto <= x));
+        if (l < 64) {
+            at->b = b + l;
+            x -= uniform64(__shfl(upto - mine, l));
+            break;
+        }
+        x -= uniform64(__shfl(upto, 63));
+    }
+    const Sequence s(p, at->b, true);
+    const int64_t each = s.steps(p);
+    at->head = static_cast<int>(x / each);
+    x -= at->head * each;
+    int low = 0, high = p.tiles - 1;
+    while (low < high) {
+        const int mid = (low + high + 1) >> 1;
+        if (s.before(p, mid) <= x) low = mid;
+        else high = mid - 1;
+    }
+    at->tile = low;
+    at->step = static_cast<int>(x - s.before(p, low));
+    at->enter(p);
+    return true;
+}
+
+__device__ __forceinline__ float2* part_stat(const PrefillParams& p) { return reinterpret_cast<float2*>(p.part + static_cast<int64_t>(2 * p.shares) * kUnitRows * 128); }
 
 __device__ __forceinline__ float half_max(float x) {
     auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -46,259 +151,633 @@ __device__ __forceinline__ float half_max(float x) {
 }
 
 // wavefront maximum of whole numbers >= 0
-__device__ __forceinline__ int wave_max_int(int x) { return static_cast<int>(wave_max(static_cast<float>(x))); }
+__device__ __forceinline__ int wave_max_int(int x) { return __builtin_amdgcn_readfirstlane(static_cast<int>(wave_max(static_cast<float>(x)))); }
 
-struct Raw {
-    uint4 k, v, ve;
-    uint32_t ke;
-};
+// f(integral_constant<int, FROM>), .., f(integral_constant<int, TO - 1>)
+template <int FROM, int TO, class F>
+__device__ __forceinline__ void unroll(F f) {
+    static_for<TO - FROM>([&](auto i) __attribute__((always_inline)) { f(std::integral_constant<int, FROM + decltype(i)::value>{}); });
+}
 
-struct Tiles {
-    uint8_t k[2][kTileBytes];
-    uint8_t v[2][kTileBytes];
+// K in LDS: chunk (eight channels) after chunk, 64 rows of 16 bytes each; a chunk's pad spreads the four chunks that four lanes write over the banks.
+// V: word (eight tokens) after word, 128 channels of 16 bytes each.  Every read is 512 bytes in a row for a half of the wavefront.
+constexpr int kChunkBytes = 64 * 16 + 16, kKBytes = 16 * kChunkBytes, kWordBytes = 128 * 16, kVBytes = 8 * kWordBytes;
+
+struct Lds {
+    uint8_t k[2][kKBytes];
+    uint8_t v[2][kVBytes];
     int unit_of[2][4];                     // R of the buffer's block
-    int event[2];                          // block whose R or V needs more than the products
+    int event[2];                          // last step (its number in the workgroup's life) that had a new R
+    int any_far;                           // last step with values out of the products' range
+    uint32_t far[VS_MAX_SEQ / kBlock / 32];                // a bit for every stage that has some
 };
 
 __device__ __forceinline__ int row_of_key(int key) { return (key & 0x27) | ((key >> 1) & 8) | ((key << 1) & 16); }
 
-__global__ __launch_bounds__(kThreads, 1) void prefill_kernel(PrefillParams p) {
+// Rows in front of their sequence.
+__device__ __forceinline__ void no_keys(const PrefillParams& p, const Place& at, int tid) {
+    const int g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc);
+    for (int i = tid; i < kUnitRows * 16; i += kThreads) {
+        const int w = i >> 9, row = at.tile * p.tok + 32 * (w / p.hc) + ((i >> 4) & 31);
+        if (row >= p.n_q) continue;
+        const int64_t r = static_cast<int64_t>(at.b * p.q_heads + g * p.group + hchunk * p.hc + w % p.hc) * p.n_q + row;
+        reinterpret_cast<uint4*>(p.o + r * 128)[i & 15] = make_uint4(0, 0, 0, 0);
+        if (p.lse && (i & 15) == 0) p.lse[r] = -INFINITY;
+    }
+}
+
+// Softmax, products and the turning into 16 bits in one instruction stream, written out in issue order (one wavefront a SIMD hides nothing): the two row
+// blocks run half a stage apart, as in vs_dense_kernel.
+//   slot X(i): matrix: scores of block 0 for stage i, P V of block 0 for stage i - 1;  vector: softmax of block 1, stage i - 1, and V of stage i to LDS
+//   slot Y(i): matrix: scores of block 1 for stage i, P V of block 1 for stage i - 1;  vector: softmax of block 0, stage i, and K of stage i + 2 to LDS
+// One barrier a stage, at the start of Y(i): it publishes V of stage i and K of stage i + 1, whose buffers' last readers are in front of it.
+__global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParams p) {
     extern __shared__ __align__(16) unsigned char smem[];
-    Tiles& lds = *reinterpret_cast<Tiles*>(smem);
+    Lds& lds = *reinterpret_cast<Lds*>(smem);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
-    const int chunks = p.group / p.hc;
-    const int tile = blockIdx.x % p.tiles, hchunk = blockIdx.x / p.tiles;
-    const int b = blockIdx.y / p.cache.kv_heads, g = blockIdx.y - b * p.cache.kv_heads;
-    const int len = cache_length_scalar(p.cache, b), base = len - p.n_q;   // position of row 0
-    (void)chunks;
-
-    int head[2], row0[2], limit[2];
-    bf16x8 q[2][8];
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-        const int w = 2 * wave + rb;
-        head[rb] = b * p.q_heads + g * p.group + hchunk * p.hc + w % p.hc;
-        row0[rb] = tile * p.tok + 32 * (w / p.hc);
-        const int row = min(row0[rb] + col, p.n_q - 1);
-        limit[rb] = max(base + row, 0);
-        const uint16_t* const from = p.q + (static_cast<int64_t>(head[rb]) * p.n_q + row) * 128 + 8 * half;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[rb][j] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(from + 16 * j));
-    }
-    const int last = base + min((tile + 1) * p.tok, p.n_q) - 1;            // position of the unit's last row
-    const int blocks = max(last, 0) / kBlock + 1;
-
-    f32x16 o[2][4];
-    float top[2], sum[2];
-    int unit_now[4] = {0, 0, 0, 0};                                        // R that the sums of each group are in
-    int unit_mine = 0;                                                     // R of this wavefront's channels
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-        top[rb] = -INFINITY;
-        sum[rb] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[rb][j][e] = 0.0f;
-    }
-
-    const int key = tid >> 2, quarter = tid & 3, key_row = row_of_key(key);
-    const uint32_t k_scale = kKScales + 4 * (16 * quarter + (key & 15)) + (key >> 4);
-    const int c = lane >> 4, m = lane & 15;
-    const uint32_t v_code = kVCodes + 1024 * wave + 16 * lane, v_scale = kVScales + 16 * (4 * c + wave);
-
-    auto block_at = [&](int block) __attribute__((always_inline)) { return len > 0 ? cache_block(p.cache, b, g, block) : nullptr; };
-    auto load = [&](Raw& x, const uint8_t* from) __attribute__((always_inline)) {
-        x.k = *reinterpret_cast<const uint4*>(from + 16 * tid);
-        x.v = *reinterpret_cast<const uint4*>(from + v_code);
-        x.ve = *reinterpret_cast<const uint4*>(from + v_scale);
-        x.ke = from[k_scale];
-    };
-    auto put_k = [&](const Raw& x, int buffer) __attribute__((always_inline)) {
-        const float scale = __uint_as_float(x.ke << 23);
-        const uint32_t w[4] = {x.k.x, x.k.y, x.k.z, x.k.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint4*>(lds.k[buffer] + 256 * key_row + 16 * ((4 * quarter + i) ^ (key_row & 15))) = dequantise8(w[i], scale);
-    };
-    // block: its number, live: tokens of it that the sequence has
-    auto put_v = [&](const Raw& x, int buffer, int block, int live) __attribute__((always_inline)) {
-        const uint32_t e[4] = {x.ve.x, x.ve.y, x.ve.z, x.ve.w};
-        ushort2_t scale[8], most = {0, 0};
-        const uint16_t lowest = static_cast<uint16_t>(unit_mine - kSpan), bias = static_cast<uint16_t>((unit_mine - kSpan - 1) << 10);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {                      // tokens 16 (i / 2) + 4 c + 2 (i % 2) and the next
-            const ushort2_t pair = __builtin_bit_cast(ushort2_t, __builtin_amdgcn_perm(0u, e[i >> 1], i & 1 ? 0x0c030c02u : 0x0c010c00u));
-            most = __builtin_elementwise_max(most, pair - lowest);
-            scale[i] = pair * static_cast<uint16_t>(1024) - bias;
-        }
-        if (__any(most[0] > kSpan || most[1] > kSpan)) {   // not all of E in [R - 27, R]
-            int largest = 0;
-            auto there = [&](int i, int j) { return 16 * (i >> 1) + 4 * c + 2 * (i & 1) + j < live; };
-            auto byte = [&](int i, int j) { return static_cast<int>((e[i >> 1] >> (8 * (2 * (i & 1) + j))) & 255); };
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (there(i, j) && byte(i, j) < 255) largest = max(largest, byte(i, j));
-            largest = __builtin_amdgcn_readfirstlane(wave_max_int(largest));
-            bool event = largest > unit_mine;
-            if (largest > unit_mine) unit_mine = min(largest + 2, 254);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int x = byte(i, j) - unit_mine + kSpan + 1;
-                    const bool fits = there(i, j) && byte(i, j) < 255 && x > 0;
-                    scale[i][j] = fits ? static_cast<uint16_t>(x << 10) : 0;
-                    event |= there(i, j) && byte(i, j) > 0 && !fits;
-                }
-            if (__any(event)) lds.event[buffer] = block;
-        }
-        lds.unit_of[buffer][wave] = unit_mine;
-        const uint32_t w[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {                      // word 2 b + u
-            const int u = i & 1, channel = 32 * wave + 16 * (i >> 1) + m;
-            half2_t y[4];
-            y[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], 1.0f, 0) * __builtin_bit_cast(half2_t, scale[4 * u]);
-            y[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], 1.0f, 1) * __builtin_bit_cast(half2_t, scale[4 * u + 1]);
-            y[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], 1.0f, 2) * __builtin_bit_cast(half2_t, scale[4 * u + 2]);
-            y[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[i], 1.0f, 3) * __builtin_bit_cast(half2_t, scale[4 * u + 3]);
-            *reinterpret_cast<uint4*>(lds.v[buffer] + 128 * channel + 16 * ((4 * u + c) ^ ((channel >> 1) & 7))) =
-                make_uint4(__builtin_bit_cast(uint32_t, y[0]), __builtin_bit_cast(uint32_t, y[1]), __builtin_bit_cast(uint32_t, y[2]),
-                           __builtin_bit_cast(uint32_t, y[3]));
-        }
-    };
-
+    const int share = blockIdx.x;
+    int64_t per, total;
+    Place at;
+    if (!find(p, share, lane, &per, &total, &at)) return;
+    const int64_t mine = min(per, total - per * share);
     if (tid < 2) lds.event[tid] = -1;
-    __syncthreads();
-    for (int block = 0; block < blocks; ++block) {
-        const uint8_t* const from = block_at(block);
-        Raw raw;
-        load(raw, from ? from : p.cache.data);
-        put_k(raw, 0);
-        put_v(raw, 0, block, from ? min(len - block * kBlock, kBlock) : 0);
-        __syncthreads();
-        const bool event = lds.event[0] == block;
-        if (event) {
+    if (tid == 0) lds.any_far = -1;
+    for (int w = tid; w < VS_MAX_SEQ / kBlock / 32; w += kThreads) lds.far[w] = 0;
+
+    // a thread's piece of a block: 32 channels of a key, and of V the words of eight tokens 4 c .. of two channels of the wavefront's 32
+    const int key = tid >> 2, quarter = tid & 3, c = lane >> 4, m = lane & 15;
+    const uint32_t k_scale = kKScales + 4 * (16 * quarter + (key & 15)) + (key >> 4);
+    const uint32_t v_code = kVCodes + 1024 * wave + 16 * lane, v_scale = kVScales + 16 * (4 * c + wave);
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)smem));
+    const uint32_t k_to = lds0 + 4 * quarter * kChunkBytes + 16 * row_of_key(key);
+    const uint32_t v_to = lds0 + 2 * kKBytes + c * kWordBytes + 16 * (32 * wave + m);
+    const uint32_t k_from = lds0 + half * kChunkBytes + 16 * col;
+    const uint32_t v_from = lds0 + 2 * kKBytes + half * kWordBytes + 16 * col;
+    typedef __attribute__((address_space(3))) u32x4* lds_u4;
+
+    bf16x8 qf[2][8], kf[2][8];
+    half8_t vf[4][4], pb[2][2][2];
+    f32x16 sc[2][2], oacc[2][4];
+    float m_run[2], l_run[2];
+    uint4 raw_k, raw_v, raw_e;             // codes of K, codes of V and their scales on their way to LDS
+    uint32_t raw_s;                        // K's scale
+    int steps_done = 0;                    // numbers the steps for lds.event
+    int64_t left = mine;
+
+    for (; left > 0; at.next(p)) {
+        const int end = at.step + static_cast<int>(min(left, static_cast<int64_t>(kStart + at.blocks - at.step)));
+        left -= end - at.step;
+        const int b = at.b, g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc), len = at.len;
+        const int first_block = max(at.step - kStart, 0), nst = max(end - kStart, 0) - first_block;
+        if (nst == 0) {                                                    // the start alone, or (rows without a position) no more than that
+            if (at.blocks == 0 && end == kStart) no_keys(p, at, tid);
+            continue;
+        }
+        // ---- the unit's rows ----
+        int head[2], row0[2], limit[2], sure = INT32_MAX;                  // limit: last key that the lane's row sees;  sure: that every row of the wavefront sees
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) {
+            const int w = 2 * wave + rb;
+            head[rb] = b * p.q_heads + g * p.group + hchunk * p.hc + w % p.hc;
+            row0[rb] = at.tile * p.tok + 32 * (w / p.hc);
+            const int row = min(row0[rb] + col, p.n_q - 1);                // (rows behind the last one are not stored)
+            limit[rb] = max(at.base + row, 0);                             // (nor are rows in front of their sequence)
+            sure = min(sure, max(at.base + min(row0[rb], p.n_q - 1), 0));
+            const uint16_t* const from = p.q + (static_cast<int64_t>(head[rb]) * p.n_q + row) * 128 + 8 * half;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) qf[rb][j] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(from + 16 * j));
+            m_run[rb] = -INFINITY;
+            l_run[rb] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) oacc[rb][j][e] = 0.0f;
+        }
+        int unit_now[4] = {0, 0, 0, 0};                                    // R that the sums of each group are in
+        int unit_mine = 0;                                                 // R of this wavefront's channels
+        bool ready = false;                                                // stages without a mask need no search for a maximum
+
+        // ---- blocks: addresses a stage and more ahead ----
+        int page = first_block / p.cache.page_blocks, in_page = first_block - page * p.cache.page_blocks, ahead = 0;
+        int entry = cache_page(p.cache, b, page);
+        uint32_t there = 0;                                                // bit i: stage `now` + i has a page
+        auto next_block = [&]() __attribute__((always_inline)) -> const uint8_t* {
+            const bool paged = len > 0 && cache_paged(p.cache, entry);
+            const uint8_t* const from = p.cache.data + (paged ? cache_offset(p.cache, entry, g, in_page) : 0);
+            there = there >> 1 | (paged ? 8u : 0u);
+            if (++ahead < nst) {                                           // (behind the last stage: that one again)
+                if (++in_page == p.cache.page_blocks) {
+                    in_page = 0;
+                    entry = cache_page(p.cache, b, ++page);
+                }
+            }
+            return from;
+        };
+        auto load_k = [&](const uint8_t* from) __attribute__((always_inline)) {
+            raw_k = *reinterpret_cast<const uint4*>(from + 16 * tid);
+            raw_s = from[k_scale];
+        };
+        auto load_v = [&](const uint8_t* from) __attribute__((always_inline)) {
+            raw_v = *reinterpret_cast<const uint4*>(from + v_code);
+            raw_e = *reinterpret_cast<const uint4*>(from + v_scale);
+        };
+        auto live_of = [&](int st) __attribute__((always_inline)) { return min(len - (first_block + st) * kBlock, kBlock); };
+        const uint8_t* at_v;                                               // block that V is asked for next
+        const uint8_t* at_k;
+
+        // chunk i of this thread's four of K of stage st
+        auto put_k = [&](int st, int i) __attribute__((always_inline)) {
+            const uint32_t w = i == 0 ? raw_k.x : i == 1 ? raw_k.y : i == 2 ? raw_k.z : raw_k.w;
+            *(lds_u4)(k_to + (st & 1) * kKBytes + i * kChunkBytes) = __builtin_bit_cast(u32x4, dequantise8(w, __uint_as_float(raw_s << 23)));
+        };
+        ushort2_t scale[8], most;
+        auto put_v_scale = [&](int i) __attribute__((always_inline)) {     // tokens 16 (i / 2) + 4 c + 2 (i % 2) and the next
+            const uint32_t e = i < 2 ? raw_e.x : i < 4 ? raw_e.y : i < 6 ? raw_e.z : raw_e.w;
+            const ushort2_t pair = __builtin_bit_cast(ushort2_t, __builtin_amdgcn_perm(0u, e, i & 1 ? 0x0c030c02u : 0x0c010c00u));
+            const ushort2_t over = pair - static_cast<uint16_t>(unit_mine - kSpan);
+            most = i == 0 ? over : __builtin_elementwise_max(most, over);
+            scale[i] = pair * static_cast<uint16_t>(1024) - static_cast<uint16_t>((unit_mine - kSpan - 1) << 10);
+        };
+        auto check_v = [&](int st, bool paged) __attribute__((always_inline)) {
+            if (__builtin_expect(__ballot(most[0] > kSpan || most[1] > kSpan) != 0, 0)) {   // not all of E in [R - 27, R]
+                const int live = paged ? live_of(st) : 0;
+                const uint32_t e[4] = {raw_e.x, raw_e.y, raw_e.z, raw_e.w};
+                int largest = 0;
+                auto in = [&](int i, int j) { return 16 * (i >> 1) + 4 * c + 2 * (i & 1) + j < live; };
+                auto byte = [&](int i, int j) { return static_cast<int>((e[i >> 1] >> (8 * (2 * (i & 1) + j))) & 255); };
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (in(i, j) && byte(i, j) < 255) largest = max(largest, byte(i, j));
+                largest = wave_max_int(largest);
+                if (largest > unit_mine) {
+                    unit_mine = min(largest + 2, 254);
+                    lds.event[st & 1] = steps_done + st;
+                }
+                bool far = false;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int x = byte(i, j) - unit_mine + kSpan + 1;
+                        const bool fits = in(i, j) && byte(i, j) < 255 && x > 0;
+                        scale[i][j] = fits ? static_cast<uint16_t>(x << 10) : 0;
+                        far |= in(i, j) && byte(i, j) > 0 && !fits;
+                    }
+                if (__any(far)) {
+                    lds.any_far = steps_done;
+                    if (lane == 0) atomicOr(&lds.far[st >> 5], 1u << (st & 31));
+                }
+            }
+            lds.unit_of[st & 1][wave] = unit_mine;
+        };
+        uint32_t word[4];
+        auto put_v = [&](int st, int piece) __attribute__((always_inline)) {   // word 2 b + u (piece / 4), tokens 2 k, 2 k + 1 of its eight
+            const int i = piece >> 2, k = piece & 3, u = i & 1;
+            const uint32_t w = i == 0 ? raw_v.x : i == 1 ? raw_v.y : i == 2 ? raw_v.z : raw_v.w;
+            const half2_t s = __builtin_bit_cast(half2_t, scale[4 * u + k]);
+            half2_t y;
+            if (k == 0) y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0);
+            if (k == 1) y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1);
+            if (k == 2) y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2);
+            if (k == 3) y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3);
+            word[k] = __builtin_bit_cast(uint32_t, y * s);
+            if (k == 3) *(lds_u4)(v_to + (st & 1) * kVBytes + 4 * u * kWordBytes + 256 * (i >> 1)) = u32x4{word[0], word[1], word[2], word[3]};
+        };
+
+        auto read_k = [&](int st, int i) __attribute__((always_inline)) {  // fragment i % 8 of tile i / 8
+            const u32x4 x = *(lds_u4)(k_from + (st & 1) * kKBytes + 512 * (i >> 3) + 2 * kChunkBytes * (i & 7));
+            kf[i >> 3][i & 7] = __builtin_bit_cast(bf16x8, x);
+        };
+        auto read_v = [&](int st, int i) __attribute__((always_inline)) {  // tokens 16 (i / 4) .., channels 32 (i % 4) ..
+            const u32x4 x = *(lds_u4)(v_from + (st & 1) * kVBytes + 2 * kWordBytes * (i >> 2) + 512 * (i & 3));
+            vf[i >> 2][i & 3] = __builtin_bit_cast(half8_t, x);
+        };
+
+        // What the products of stage st's V do not have: a new unit for the sums (in front of them), values out of their range (behind them).
+        auto new_units = [&](int st) __attribute__((always_inline)) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int unit = __builtin_amdgcn_readfirstlane(lds.unit_of[0][j]);
+                const int unit = __builtin_amdgcn_readfirstlane(lds.unit_of[st & 1][j]);
                 if (unit == unit_now[j]) continue;
 #pragma unroll
                 for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[rb][j][e] = __builtin_ldexpf(o[rb][j][e], unit_now[j] - unit);
+                    for (int e = 0; e < 16; ++e) oacc[rb][j][e] = __builtin_ldexpf(oacc[rb][j][e], unit_now[j] - unit);
                 unit_now[j] = unit;
             }
-        }
+        };
+#define VS_FENCE() __builtin_amdgcn_sched_barrier(0)
+        // MR: the row block whose matrix products are issued; VR = 1 - MR: the one whose softmax runs.  sq: stage whose scores are computed (HAS_Q);
+        // sq - 1: stage whose P V is accumulated (HAS_P); sv: stage whose scores go through the softmax (HAS_S).
+        auto slot = [&](auto mr_tag, auto has_q, auto has_p, auto has_s, bool search, int sq, int sv) __attribute__((always_inline)) {
+            constexpr int MR = decltype(mr_tag)::value, VR = 1 - MR;
+            constexpr bool HAS_Q = decltype(has_q)::value, HAS_P = decltype(has_p)::value, HAS_S = decltype(has_s)::value;
+            auto qmfma = [&](int kk, int u) __attribute__((always_inline)) {
+                if (kk == 0) {
+                    f32x16 zero;
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-            f32x16 s[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[t][e] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(lds.k[0] + 256 * (32 * t + col) + 16 * ((2 * j + half) ^ (col & 15))));
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[rb][j], s[t], 0, 0, 0);
+                    for (int e = 0; e < 16; ++e) zero[e] = 0.0f;
+                    sc[MR][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][0], qf[MR][0], zero, 0, 0, 0);
+                } else {
+                    sc[MR][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][kk], qf[MR][kk], sc[MR][u], 0, 0, 0);
                 }
-            // key of element e of tile t: 32 t + 16 (e / 4 % 2) + 8 (e / 8) + 4 half + e % 4
-            float most = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int j = block * kBlock + 32 * t + 16 * ((e >> 2) & 1) + 8 * (e >> 3) + 4 * half + (e & 3);
-                    if (j > limit[rb] || !from) s[t][e] = -INFINITY;
-                    most = fmaxf(most, s[t][e]);
+            };
+            auto pmfma = [&](int i) __attribute__((always_inline)) {       // tokens 16 (i / 4) .., channels 32 (i % 4) ..
+                oacc[MR][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[i >> 2][i & 3], pb[MR][i >> 3][(i >> 2) & 1], oacc[MR][i & 3], 0, 0, 0);
+            };
+            if constexpr (MR == 1) {
+                if constexpr (HAS_Q) {
+                    at_v = at_k;
+                    at_k = next_block();                                   // block of stage sq + 3 (of sq + 2: at_v)
                 }
-            const float m_new = fmaxf(top[rb], half_max(most));
-            if (__any((m_new - top[rb]) * p.c > kGrown)) {
-                const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((top[rb] - m_new) * p.c);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[rb][j] *= alpha;
-                sum[rb] *= alpha;
-                top[rb] = m_new;
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                VS_FENCE();
             }
-            const float at = top[rb] == -INFINITY ? 0.0f : top[rb];
-            half8_t weight[2][2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(s[t][e] - at, p.c, kLift)), y = __builtin_amdgcn_exp2f(fmaf(s[t][e + 1] - at, p.c, kLift));
-                    sum[rb] += x + y;
-                    const f32x2 two = {x, y};
-                    const half2_t z = __builtin_convertvector(two, half2_t);
-                    weight[t][e >> 3][e & 7] = z[0];
-                    weight[t][e >> 3][(e & 7) + 1] = z[1];
+            if constexpr (MR == 0 && HAS_P) {
+                if (__builtin_expect(__builtin_amdgcn_readfirstlane(lds.event[(sq - 1) & 1]) == steps_done + sq - 1, 0)) new_units(sq - 1);
+                VS_FENCE();
+            }
+            // Softmax elements as a three-deep pipeline: step k scales element k, takes the exponential of element k - 1 and adds element k - 2 to the row
+            // sum (packing a finished pair): no instruction uses the result of its predecessor.
+            float mc = 0.0f, lsum = 0.0f;
+            float tq[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            int estep = 0;
+            auto pack_pair = [&](int u, int e, float x0, float x1) __attribute__((always_inline)) {       // weights of elements e - 1 and e
+                const f32x2 two = {x0, x1};
+                uint32_t packed = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, half2_t));
+                asm volatile("" : "+v"(packed));
+                const half2_t r = __builtin_bit_cast(half2_t, packed);
+                pb[VR][u][e >> 3][(e & 7) - 1] = r[0];
+                pb[VR][u][e >> 3][e & 7] = r[1];
+            };
+            auto expstep = [&]() __attribute__((always_inline)) {
+                if constexpr (HAS_S) {
+                    const int k = estep;
+                    if (k < 32) {
+                        float t = fmaf(sc[VR][k >> 4][k & 15], p.c, -mc);
+                        asm volatile("" : "+v"(t));
+                        tq[k & 3] = t;
+                    }
+                    if (k >= 1 && k <= 32) {
+                        float x = tq[(k - 1) & 3];
+                        x = __builtin_amdgcn_exp2f(x);
+                        asm volatile("" : "+v"(x));
+                        tq[(k - 1) & 3] = x;
+                    }
+                    if (k >= 2 && k <= 33) {
+                        const int idx = k - 2, u = idx >> 4, e = idx & 15;
+                        lsum += tq[idx & 3];
+                        asm volatile("" : "+v"(lsum));
+                        if (e & 1) pack_pair(u, e, tq[(idx - 1) & 3], tq[idx & 3]);
+                    }
+                    ++estep;
                 }
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const half8_t a = __builtin_bit_cast(half8_t, *reinterpret_cast<const uint4*>(lds.v[0] + 128 * (32 * j + col) + 16 * ((2 * k + half) ^ ((col >> 1) & 7))));
-                    o[rb][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, weight[k >> 1][k & 1], o[rb][j], 0, 0, 0);
+            };
+            auto expsteps_upto = [&](int target) __attribute__((always_inline)) {
+                while (estep < target) expstep();
+            };
+            auto exp_share = [&](int j) __attribute__((always_inline)) {   // behind matrix instruction j
+                expsteps_upto(min(34, ((j + 1) * 34 + 30) / 31));
+            };
+            // what goes to LDS, behind matrix instruction j
+            auto turn = [&](auto index) __attribute__((always_inline)) {
+                constexpr int j = decltype(index)::value;
+                if constexpr (HAS_Q && MR == 0) {
+                    if constexpr (j < 8) put_v_scale(j);
+                    if constexpr (j == 9) check_v(sq, there & 2);          // (`there` is at the stage in front)
+                    if constexpr (j >= 10 && j < 26) put_v(sq, j - 10);
+                    if constexpr (j == 27) load_v(at_v);
                 }
-            if (event && from) {                           // what the tile of V has not
-                const int live = min(len - block * kBlock, kBlock);
+                if constexpr (HAS_Q && MR == 1) {
+                    if constexpr (j >= 2 && j < 18 && (j - 2) % 4 == 0) put_k(sq + 2, (j - 2) / 4);
+                    if constexpr (j == 18) load_k(at_k);
+                }
+            };
+            auto rescale = [&](float mx) __attribute__((always_inline)) -> bool {
+                const float m_new = fmaxf(m_run[VR], half_max(mx));
+                if (!__ballot((m_new - m_run[VR]) * p.c > kGrown)) return false;
+                const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m_run[VR] - m_new) * p.c);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    for (int token = 0; token < live; ++token) {
-                        const int E = __builtin_amdgcn_readfirstlane(from[kVScales + 16 * (4 * ((token >> 2) & 3) + j) + 4 * (token >> 4) + (token & 3)]);
-                        if (E == 0 || (E < 255 && E >= unit_now[j] - kSpan)) continue;
-                        const int at_row = row_of_key(token), element = 4 * ((at_row >> 3) & 3) + (at_row & 3);
-                        float w = 0.0f;
 #pragma unroll
-                        for (int t = 0; t < 2; ++t)
+                    for (int e = 0; e < 16; ++e) oacc[VR][j][e] *= alpha;
+                l_run[VR] *= alpha;
+                m_run[VR] = m_new;
+                return true;
+            };
+            auto look_again = [&]() __attribute__((always_inline)) {
+                if (__builtin_expect(__ballot(lsum > kGrownSum) != 0ull, 0)) {
+                    float mx[2];
 #pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (32 * t + e == (token & 32) + element) w = static_cast<float>(weight[t][e >> 3][e & 7]);
-                        w = __shfl(w, col + 32 * ((at_row >> 2) & 1));
-                        const bool seen = block * kBlock + token <= limit[rb];
+                    for (int u = 0; u < 2; ++u) {
+                        mx[u] = sc[VR][u][0];
+#pragma unroll
+                        for (int e = 1; e < 16; ++e) mx[u] = fmaxf(mx[u], sc[VR][u][e]);
+                    }
+                    if (rescale(fmaxf(mx[0], mx[1]))) {
+                        lsum = 0.0f;
+#pragma unroll
+                        for (int idx = 0; idx < 32; idx += 2) {
+                            const int u = idx >> 4, e = idx & 15;
+                            const float x0 = __builtin_amdgcn_exp2f(fmaf(sc[VR][u][e] - m_run[VR], p.c, kLift));
+                            const float x1 = __builtin_amdgcn_exp2f(fmaf(sc[VR][u][e + 1] - m_run[VR], p.c, kLift));
+                            lsum += x0;
+                            lsum += x1;
+                            pack_pair(u, e + 1, x0, x1);
+                        }
+                        if (__ballot(fabsf(m_run[VR]) * p.c > kSafe)) ready = false;
+                    }
+                }
+            };
+            if constexpr (HAS_S) {
+                if (search) {
+                    // key of element e of tile u: 32 u + 16 (e / 4 % 2) + 8 (e / 8) + 4 half + e % 4
+                    const int last = there & 1u ? limit[VR] - (first_block + sv) * kBlock - 4 * half : -1;
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const int channel = 32 * j + 8 * (e >> 2) + 4 * half + (e & 3);
-                            const uint32_t word = *reinterpret_cast<const uint32_t*>(from + v_word(channel, (token >> 2) & 3, token >> 5));
-                            const uint32_t code = word >> (4 * ((token & 3) + ((token >> 4) & 1) * 4)) & 15u;
-                            const uint32_t size = code & 7u;           // 0 .5 1 1.5 2 3 4 6
-                            float v = size < 2 ? 0.5f * static_cast<float>(size) : __builtin_ldexpf(size & 1 ? 1.5f : 1.0f, static_cast<int>(size >> 1) - 1);
-                            if (code & 8u) v = -v;
-                            if (E == 255) v = __uint_as_float(0x7fc00000u);
-                            else v = __builtin_ldexpf(v, E - unit_now[j] + kTop);
-                            if (seen) o[rb][j][e] = fmaf(w, v, o[rb][j][e]);
+                            if (32 * u + 16 * ((e >> 2) & 1) + 8 * (e >> 3) + (e & 3) > last) sc[VR][u][e] = -INFINITY;
+                            mx[e & 3] = fmaxf(mx[e & 3], sc[VR][u][e]);
                         }
+                    rescale(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+                    const float at_least = m_run[VR] == -INFINITY ? 0.0f : m_run[VR];
+                    mc = fmaf(at_least, p.c, -kLift);
+                    if (__ballot(fabsf(at_least) * p.c > kSafe)) {         // (the row's largest weight is to be 1)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) sc[VR][u][e] -= at_least;
+                        mc = -kLift;
                     }
+                } else {
+                    mc = fmaf(m_run[VR], p.c, -kLift);
+                }
+                VS_FENCE();
+            }
+            unroll<0, 6>([&](auto index) __attribute__((always_inline)) {
+                constexpr int j = decltype(index)::value;
+                if constexpr (HAS_Q) qmfma(j >> 1, j & 1);
+                VS_FENCE();
+                if constexpr (MR == 0 && HAS_P) read_v(sq - 1, j);
+                turn(index);
+                if constexpr (HAS_S) exp_share(j);
+                VS_FENCE();
+            });
+            unroll<6, 16>([&](auto index) __attribute__((always_inline)) {
+                constexpr int j = decltype(index)::value;
+                if constexpr (HAS_Q) qmfma(j >> 1, j & 1);
+                VS_FENCE();
+                if constexpr (MR == 0 && HAS_P) read_v(sq - 1, j);
+                turn(index);
+                if constexpr (HAS_S) exp_share(j);
+                VS_FENCE();
+            });
+            unroll<0, 16>([&](auto index) __attribute__((always_inline)) {
+                constexpr int j = decltype(index)::value;
+                if constexpr (HAS_S && j == 15)
+                    if (!search) look_again();
+                if constexpr (HAS_P) pmfma(j);
+                VS_FENCE();
+                if constexpr (MR == 1 && HAS_Q) read_k(sq + 1, j);
+                turn(std::integral_constant<int, 16 + j>{});
+                if constexpr (HAS_S) exp_share(16 + j);
+                VS_FENCE();
+            });
+            if constexpr (HAS_S) {
+                expsteps_upto(34);
+                l_run[VR] += lsum;
+            }
+            VS_FENCE();
+        };
+#undef VS_FENCE
+
+        using T = std::true_type;
+        using F = std::false_type;
+        using R0 = std::integral_constant<int, 0>;
+        using R1 = std::integral_constant<int, 1>;
+
+        // ---- the first blocks; `there`: bits of stages 0, 1, 2 end at 0 .. 2 once Y(0) has asked for stage 3 ----
+        const uint8_t* const at0 = next_block();
+        load_k(at0);
+        load_v(at0);
+        const uint4 k0 = raw_k;
+        const uint32_t s0 = raw_s;
+        const uint8_t* const at1 = next_block();
+        load_k(at1);
+        const uint4 k1 = raw_k;
+        const uint32_t s1 = raw_s;
+        at_k = next_block();
+        load_k(at_k);
+        at_v = at1;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the unit before this one is out of every buffer
+        {
+            const uint4 k2 = raw_k;
+            const uint32_t s2 = raw_s;
+            raw_k = k0;
+            raw_s = s0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put_k(0, i);
+            raw_k = k1;
+            raw_s = s1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put_k(1, i);
+            raw_k = k2;
+            raw_s = s2;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 16; ++i) read_k(0, i);
+        slot(R0{}, T{}, F{}, F{}, true, 0, 0);                              // X(0): scores of block 0
+        slot(R1{}, T{}, F{}, T{}, true, 0, 0);                              // Y(0): scores of block 1; softmax of block 0
+        if (nst > 1) {
+            bool search = true;
+            slot(R0{}, T{}, T{}, T{}, true, 1, 0);                          // X(1): softmax of block 1 for stage 0
+            // Y(i) and X(i + 1) have the softmax of stage i: without a mask and a search for the maximum where every row of the wavefront sees all of it and has
+            // a maximum that serves already
+            for (int i = 1; i < nst - 1; ++i) {
+                if (search) {
+                    const float least = fminf(m_run[0], m_run[1]), largest = fmaxf(m_run[0], m_run[1]);
+                    ready = __all(least * p.c >= -kSafe && largest * p.c <= kSafe);
+                }
+                search = !(ready && (there & 2) && (first_block + i) * kBlock + kBlock - 1 <= sure);
+                slot(R1{}, T{}, T{}, T{}, search, i, i);
+                slot(R0{}, T{}, T{}, T{}, search, i + 1, i);
+            }
+            slot(R1{}, T{}, T{}, T{}, true, nst - 1, nst - 1);
+        }
+        slot(R0{}, F{}, T{}, T{}, true, nst, nst - 1);                      // X(nst): P V of block 0; softmax of block 1
+        slot(R1{}, F{}, T{}, F{}, true, nst, nst);                          // Y(nst): P V of block 1
+
+        // ---- what the products of V do not have ----
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(lds.any_far) == steps_done, 0)) {
+            for (int w = 0; 32 * w < nst; ++w)
+                for (uint32_t bits = __builtin_amdgcn_readfirstlane(lds.far[w]); bits; bits &= bits - 1) {
+                    const int st = 32 * w + __builtin_ctz(bits), live = live_of(st);
+                    const uint8_t* const from = cache_block(p.cache, b, g, first_block + st);     // (a block without a page has no bit)
+                    load_k(from);
+                    load_v(from);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) put_k(0, i);
+                    const uint32_t e[4] = {raw_e.x, raw_e.y, raw_e.z, raw_e.w}, v[4] = {raw_v.x, raw_v.y, raw_v.z, raw_v.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int u = i & 1;
+                        uint32_t y[4];
+                        static_for<4>([&](auto k) __attribute__((always_inline)) {
+                            uint32_t x[2];
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const int which = 4 * u + k, E = static_cast<int>((e[which >> 1] >> (8 * (2 * (which & 1) + j))) & 255);
+                                const int up = E - unit_mine + kTop + 127;                        // exponent of the scale in fp32
+                                const bool far = 16 * (which >> 1) + 4 * c + 2 * (which & 1) + j < live && E < 255 && E < unit_mine - kSpan && up > 0;
+                                x[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[i], __uint_as_float(static_cast<uint32_t>(far ? up : 127) << 23), decltype(k)::value));
+                                if (!far) x[j] = 0;
+                            }
+                            y[k] = __builtin_amdgcn_perm(x[1], x[0], 0x07060100u);
+                        });
+                        *(lds_u4)(v_to + 4 * u * kWordBytes + 256 * (i >> 1)) = u32x4{y[0], y[1], y[2], y[3]};
+                    }
+                    __syncthreads();
+                    static_for<2>([&](auto rb_tag) __attribute__((always_inline)) {
+                        constexpr int rb = decltype(rb_tag)::value;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) sc[rb][u][e] = 0.0f;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                read_k(0, 8 * u + k);
+                                sc[rb][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][k], qf[rb][k], sc[rb][u], 0, 0, 0);
+                            }
+                        }
+                        const float at_least = m_run[rb] == -INFINITY ? 0.0f : m_run[rb];
+                        const int last = limit[rb] - (first_block + st) * kBlock - 4 * half;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {                      // 16 tokens
+                            uint32_t high[4], low[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                float x[2];
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    const int e = 8 * (i & 1) + 2 * k + j;
+                                    const bool seen = 32 * (i >> 1) + 16 * ((e >> 2) & 1) + 8 * (e >> 3) + (e & 3) <= last;
+                                    x[j] = seen ? __builtin_amdgcn_exp2f(fmaf(sc[rb][i >> 1][e] - at_least, p.c, kLift)) : 0.0f;
+                                }
+                                high[k] = pack_bf16(x[0], x[1]);
+                                low[k] = pack_bf16(x[0] - __uint_as_float(high[k] << 16), x[1] - __uint_as_float(high[k] & 0xffff0000u));
+                            }
+                            const bf16x8 a = __builtin_bit_cast(bf16x8, u32x4{high[0], high[1], high[2], high[3]});
+                            const bf16x8 z = __builtin_bit_cast(bf16x8, u32x4{low[0], low[1], low[2], low[3]});
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                read_v(0, 4 * i + j);
+                                const bf16x8 y = __builtin_bit_cast(bf16x8, vf[i][j]);
+                                oacc[rb][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, a, oacc[rb][j], 0, 0, 0);
+                                oacc[rb][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, z, oacc[rb][j], 0, 0, 0);
+                            }
+                        }
+                        // groups that are not finite, to the rows that see them
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int E = from[kVScales + 16 * (4 * ((lane >> 2) & 3) + j) + 4 * (lane >> 4) + (lane & 3)];      // of token `lane`
+                            const uint64_t bad = __ballot(lane < live && E == 255);
+                            if (bad && (first_block + st) * kBlock + __builtin_ctzll(bad) <= limit[rb])
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) oacc[rb][j][e] = __uint_as_float(0x7fc00000u);
+                        }
+                    });
+                    __syncthreads();
+                }
+            __syncthreads();                                               // (every wavefront has seen the bits)
+            for (int w = tid; 32 * w < nst; w += kThreads) lds.far[w] = 0;
+        }
+
+        // ---- results ----
+        const bool whole = first_block == 0 && nst == at.blocks;
+        const int slot_of = 2 * share + (first_block == 0 ? 1 : 0);
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) {
+            const float l = half_swap_sum(l_run[rb]);
+            const int row = row0[rb] + col;
+            if (row >= p.n_q) continue;
+            if (whole) {
+                const bool none = at.base + row < 0 || l == 0.0f;
+                const float inv = none ? 0.0f : 1.0f / l;
+                const int64_t r = static_cast<int64_t>(head[rb]) * p.n_q + row;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int a = 0; a < 4; ++a) {
+                        float y[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = none ? 0.0f : __builtin_ldexpf(oacc[rb][j][4 * a + i] * inv, unit_now[j] - 127 - kTop);
+                        *reinterpret_cast<uint2*>(p.o + r * 128 + 32 * j + 8 * a + 4 * half) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+                    }
+                if (p.lse && half == 0) p.lse[r] = none ? -INFINITY : (m_run[rb] * p.c + (log2f(l) - kLift)) * 0.69314718055994530942f;
+            } else {
+                const int64_t r = static_cast<int64_t>(slot_of) * kUnitRows + 32 * (2 * wave + rb) + col;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int a = 0; a < 4; ++a) {
+                        float y[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = __builtin_ldexpf(oacc[rb][j][4 * a + i], unit_now[j] - 127 - kTop);
+                        *reinterpret_cast<float4*>(p.part + r * 128 + 32 * j + 8 * a + 4 * half) = make_float4(y[0], y[1], y[2], y[3]);
+                    }
+                if (half == 0) part_stat(p)[r] = make_float2(m_run[rb] * p.c, l);
             }
         }
-        __syncthreads();
+        steps_done += nst + 2;
     }
+}
 
+// The parts of a unit that several workgroups shared.  Workgroup (s, y): the unit that share s begins with, if it began before and ends there; rows
+// 32 y .. of it.  The first part stands in its share's second slot, the others in their shares' first.
+__global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillParams p) {
+    int64_t per, total;
+    Place at;
+    const int share = blockIdx.x, lane = threadIdx.x & 63;
+    if (!find(p, share, lane, &per, &total, &at) || at.step <= kStart) return;
+    if (kStart + at.blocks - at.step > min(per, total - per * share)) return;              // a later share has the end
+    const int first = static_cast<int>((per * share - at.step + kStart) / per), parts = share - first + 1;
+    const int w = blockIdx.y, row = at.tile * p.tok + 32 * (w / p.hc) + (threadIdx.x >> 3);
+    if (row >= p.n_q) return;
+    const int g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc);
+    const int64_t r = static_cast<int64_t>(at.b * p.q_heads + g * p.group + hchunk * p.hc + w % p.hc) * p.n_q + row;
+    const int in_unit = 32 * w + (threadIdx.x >> 3), channel = 4 * (threadIdx.x & 7);
+    auto slot_of = [&](int i) { return static_cast<int64_t>(i == 0 ? 2 * first + 1 : 2 * (first + i)) * kUnitRows + in_unit; };
+    float m = -INFINITY, l = 0.0f;
+    for (int i = 0; i < parts; ++i) m = fmaxf(m, part_stat(p)[slot_of(i)].x);
+    float4 y[4];
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-        const float l = half_swap_sum(sum[rb]);
-        const int row = row0[rb] + col;
-        if (row >= p.n_q) continue;
-        const bool none = base + row < 0 || l == 0.0f;
-        const float inv = none ? 0.0f : 1.0f / l;
-        const int64_t r = static_cast<int64_t>(head[rb]) * p.n_q + row;
+    for (int j = 0; j < 4; ++j) y[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = 0; i < parts; ++i) {
+        const int64_t slot = slot_of(i);
+        const float2 x = part_stat(p)[slot];
+        const float f = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.x - m);
+        l = fmaf(x.y, f, l);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                float y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = none ? 0.0f : __builtin_ldexpf(o[rb][j][4 * a + i] * inv, unit_now[j] - 127 - kTop);
-                *reinterpret_cast<uint2*>(p.o + r * 128 + 32 * j + 8 * a + 4 * half) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-            }
-        if (p.lse && half == 0) p.lse[r] = none ? -INFINITY : (top[rb] * p.c + log2f(l) - kLift) * 0.69314718055994530942f;
+        for (int j = 0; j < 4; ++j) {
+            const float4 z = *reinterpret_cast<const float4*>(p.part + slot * 128 + 32 * j + channel);
+            y[j] = make_float4(fmaf(z.x, f, y[j].x), fmaf(z.y, f, y[j].y), fmaf(z.z, f, y[j].z), fmaf(z.w, f, y[j].w));
+        }
     }
+    const bool none = at.base + row < 0 || l == 0.0f;
+    const float inv = none ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (none) y[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        *reinterpret_cast<uint2*>(p.o + r * 128 + 32 * j + channel) = make_uint2(pack_bf16(y[j].x * inv, y[j].y * inv), pack_bf16(y[j].z * inv, y[j].w * inv));
+    }
+    if (p.lse && channel == 0) p.lse[r] = none ? -INFINITY : (m + (log2f(l) - kLift)) * 0.69314718055994530942f;
 }
 
 bool sizes_ok(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) {
@@ -306,12 +785,33 @@ bool sizes_ok(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) 
            max_n <= VS_MAX_SEQ && batch <= 65535 && static_cast<int64_t>(batch) * kv_heads <= 65535;
 }
 
+// p.n_q, p.group, .. and the workgroups from the sizes; steps of the longest sequences: fewer workgroups where there are few.
+void plan(PrefillParams& p, int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) {
+    p.batch = batch;
+    p.q_heads = q_heads;
+    p.n_q = static_cast<int>(n_q);
+    p.group = q_heads / kv_heads;
+    p.hc = p.group % 4 == 0 ? 4 : p.group % 2 == 0 ? 2 : 1;
+    p.tok = kUnitRows / p.hc;
+    p.tok_blocks = p.tok / kBlock;
+    p.tiles = (p.n_q + p.tok - 1) / p.tok;
+    p.heads = kv_heads * (p.group / p.hc);
+    const int64_t units = static_cast<int64_t>(batch) * p.heads * p.tiles;
+    const int64_t steps = units * (kStart + (max_n + kBlock - 1) / kBlock);  // no fewer than there are
+    const int64_t shares = (steps + kSteps - 1) / kSteps;
+    p.shares = static_cast<int>(shares < kShares ? shares : kShares);
+}
+
+size_t part_bytes(const PrefillParams& p) { return static_cast<size_t>(2 * p.shares) * kUnitRows * (VS_HEAD_DIM + 2) * sizeof(float); }
+
 }  // namespace
 
 extern "C" size_t vs_cache_prefill_workspace(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) {
     if (!sizes_ok(batch, q_heads, kv_heads, n_q, max_n)) return 0;
     if (n_q <= VS_CACHE_MAX_NEW) return vs_cache_attend_workspace(batch, q_heads, kv_heads, static_cast<int>(n_q), max_n);
-    return 0;
+    PrefillParams p;
+    plan(p, batch, q_heads, kv_heads, n_q, max_n);
+    return part_bytes(p);
 }
 
 extern "C" int vs_cache_prefill(const void* q, const vs_cache_t* cache, int batch, int q_heads, int64_t n_q, const int32_t* lens, int64_t max_n,
@@ -325,24 +825,24 @@ extern "C" int vs_cache_prefill(const void* q, const vs_cache_t* cache, int batc
     const int rc = vs::cache_params(cache, batch, lens, max_n, &p.cache);
     if (rc != VS_OK) return rc;
     if (!sizes_ok(batch, q_heads, cache->kv_heads, n_q, max_n)) return VS_ERR_UNSUPPORTED;
-    if (ws_bytes < vs_cache_prefill_workspace(batch, q_heads, cache->kv_heads, n_q, max_n)) return VS_ERR_WORKSPACE;
+    plan(p, batch, q_heads, cache->kv_heads, n_q, max_n);
+    if (!ws || ws_bytes < part_bytes(p)) return VS_ERR_WORKSPACE;
     p.q = static_cast<const uint16_t*>(q);
     p.o = static_cast<uint16_t*>(o);
     p.lse = lse;
-    p.q_heads = q_heads;
-    p.n_q = static_cast<int>(n_q);
-    p.group = q_heads / cache->kv_heads;
-    p.hc = p.group % 4 == 0 ? 4 : p.group % 2 == 0 ? 2 : 1;
-    p.tok = kUnitRows / p.hc;
-    p.tiles = (p.n_q + p.tok - 1) / p.tok;
+    p.part = static_cast<float*>(ws);
     static vs::PerDeviceOnce once;
     const int set = once.run(nullptr, [](int) -> int {
-        VS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&prefill_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(Tiles))));
+        VS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&prefill_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(Lds))));
         return VS_OK;
     });
     if (set != VS_OK) return set;
-    hipLaunchKernelGGL(prefill_kernel, dim3(static_cast<unsigned>(p.tiles * (p.group / p.hc)), static_cast<unsigned>(batch * cache->kv_heads)), dim3(kThreads),
-                       sizeof(Tiles), static_cast<hipStream_t>(stream), p);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    hipLaunchKernelGGL(prefill_kernel, dim3(p.shares), dim3(kThreads), sizeof(Lds), s, p);
     VS_LAUNCH_CHECK();
+    if (p.shares > 1) {
+        hipLaunchKernelGGL(prefill_join_kernel, dim3(p.shares, kUnitRows / 32), dim3(kThreads), 0, s, p);
+        VS_LAUNCH_CHECK();
+    }
     return VS_OK;
 }

@@ -62,7 +62,8 @@ def test_lengths_of_the_host():
         for x, y in zip(call(q, cache, lens, 700), want):
             assert torch.equal(x, y)
     none = call(q, cache, [-5, 700], 700)
-    assert (none[0][0] == 0).all() and torch.isinf(none[1][0]).all() and torch.equal(none[0][1], want[0][1])
+    assert (none[0][0] == 0).all() and torch.isinf(none[1][0]).all()
+    near(none, attention(q, cache, [0, 700], 700))       # (where a row's keys are divided depends on the lengths of the batch: not the same bits)
 
 
 @pytest.mark.parametrize("rows", [1, 5, 128])
