@@ -18,7 +18,6 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
-typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -30,16 +29,18 @@ constexpr float kGrownSum = 32768.0f;                      // 2^(8 + 7): no weig
 constexpr float kSafe = 1024.0f;                           // scores (log2 units) up to which a product and a difference in one rounding are good enough
 constexpr int kShares = 256;                               // a workgroup for every compute unit
 constexpr int kStart = 3;                                  // steps that a unit's start and end count for
+constexpr int kAhead = 4;                                  // parts that are asked for at once
 constexpr int kSteps = 4;                                  // of a workgroup, if there are so few
 constexpr int kTop = 13;                                   // fp16 exponent of a code with E = R: 6 * 2^13 < 65504
 constexpr int kSpan = 27;                                  // E from R - 27 (2^-14 in fp16) to R
+constexpr uint32_t kLargeUnit = 200;                       // R, from 15 on, up to which any E outside shows in the upper half of the byte E - R + 15
 
 struct PrefillParams {
     CacheParams cache;
     const uint16_t* q;
     uint16_t* o;
     float* lse;
-    float* part;                           // [2 shares][256 rows][128] sums, then [2 shares][256] (maximum, sum of weights)
+    float* part;                           // [2 shares][256 rows][128] sums, then [2 shares][256] (maximum, sum of weights), then [shares] Joined
     int batch, q_heads, n_q, group, hc;
     int tok, tok_blocks;                   // tokens of a unit, 256 / hc, and that in blocks
     int tiles;                             // units of a sequence's head chunk
@@ -68,22 +69,30 @@ struct Sequence {
     __device__ __forceinline__ int64_t steps(const PrefillParams& p) const { return before(p, p.tiles - 1) + kStart + blocks(p, p.tiles - 1); }
 };
 
-__device__ __forceinline__ int64_t scan64(int64_t x, int lane) {
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int64_t scan64(int64_t x) {
+    auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+        const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        const int hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        x += static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32 | static_cast<uint32_t>(lo));
+    };
+    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});        // row_shr 1, 2, 4, 8
+    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});        // last of a row of 16 to the next row
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});        // last of the lower half to the upper
     return x;
 }
 
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
+__device__ __forceinline__ int64_t lane64(int64_t x, int l) {
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(x), l), hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(x >> 32), l);
     return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
 struct Place {
-    int b, head, tile, step, blocks;       // head: of the sequence's head chunks;  step: of the unit, which has kStart + blocks
-    int len, base;
+    int b = 0, head = 0, tile = 0, step = 0, blocks = 0;       // head: of the sequence's head chunks;  step: of the unit, which has kStart + blocks
+    int len = 0, base = 0;
     __device__ __forceinline__ void next(const PrefillParams& p) {                 // the unit behind this one
         step = 0;
         if (++tile == p.tiles) {
@@ -105,30 +114,29 @@ struct Place {
 
 // Steps of a share, and where share `share` begins (false: behind the end).
 __device__ __forceinline__ bool find(const PrefillParams& p, int share, int lane, int64_t* per, int64_t* total, Place* at) {
-    int64_t all = 0;
-    for (int b = 0; b < p.batch; b += 64) {
-        const int64_t mine = b + lane < p.batch ? Sequence(p, b + lane, false).steps(p) : 0;
-        all += uniform64(__shfl(scan64(mine, lane), 63));
-    }
+    int64_t mine = lane < p.batch ? Sequence(p, lane, false).steps(p) : 0, upto = scan64(mine), all = lane64(upto, 63);
+    for (int b = 64; b < p.batch; b += 64) all += lane64(scan64(b + lane < p.batch ? Sequence(p, b + lane, false).steps(p) : 0), 63);
     all *= p.heads;
     *total = all;
     *per = (all + p.shares - 1) / p.shares;
     int64_t x = *per * share;
     if (x >= all) return false;
     for (int b = 0;; b += 64) {
-        const int64_t mine = b + lane < p.batch ? Sequence(p, b + lane, false).steps(p) * p.heads : 0;
-        const int64_t upto = scan64(mine, lane);
-        const int l = __popcll(__ballot(upto <= x));
+        if (b > 0) {
+            mine = b + lane < p.batch ? Sequence(p, b + lane, false).steps(p) : 0;
+            upto = scan64(mine);
+        }
+        const int l = __popcll(__ballot(upto * p.heads <= x));
         if (l < 64) {
             at->b = b + l;
-            x -= uniform64(__shfl(upto - mine, l));
+            x -= lane64(upto - mine, l) * p.heads;
             break;
         }
-        x -= uniform64(__shfl(upto, 63));
+        x -= lane64(upto, 63) * p.heads;
     }
     const Sequence s(p, at->b, true);
     const int64_t each = s.steps(p);
-    at->head = static_cast<int>(x / each);
+    at->head = all >> 31 ? static_cast<int>(x / each) : static_cast<int>(static_cast<uint32_t>(x) / static_cast<uint32_t>(each));
     x -= at->head * each;
     int low = 0, high = p.tiles - 1;
     while (low < high) {
@@ -143,6 +151,13 @@ __device__ __forceinline__ bool find(const PrefillParams& p, int share, int lane
 }
 
 __device__ __forceinline__ float2* part_stat(const PrefillParams& p) { return reinterpret_cast<float2*>(p.part + static_cast<int64_t>(2 * p.shares) * kUnitRows * 128); }
+
+// The unit that a share ends and that others began, for the second kernel; parts: shares that have some of its blocks, 0: there is none.
+struct Joined {
+    int parts, b, head, tile, base, pad[3];
+};
+
+__device__ __forceinline__ Joined* joined(const PrefillParams& p) { return reinterpret_cast<Joined*>(part_stat(p) + static_cast<int64_t>(2 * p.shares) * kUnitRows); }
 
 __device__ __forceinline__ float half_max(float x) {
     auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -163,14 +178,28 @@ __device__ __forceinline__ void unroll(F f) {
 // V: word (eight tokens) after word, 128 channels of 16 bytes each.  Every read is 512 bytes in a row for a half of the wavefront.
 constexpr int kChunkBytes = 64 * 16 + 16, kKBytes = 16 * kChunkBytes, kWordBytes = 128 * 16, kVBytes = 8 * kWordBytes;
 
+// A block as it comes from memory.  Codes are read by the wavefront that asked for them, scales by all (wavefronts 2 and 3 ask for what 0 and 1 do).
+constexpr int kRawBytes = 16384, kRing = 4;                // (a power of two: a stage's place is a shift and a mask)
+
 struct Lds {
     uint8_t k[2][kKBytes];
     uint8_t v[2][kVBytes];
+    uint8_t raw[kRing][kRawBytes];
+    uint16_t scale[kThreads / 64][64];     // V's scales of a wavefront's channels in fp16, by token in the order of the words
     int unit_of[2][4];                     // R of the buffer's block
     int event[2];                          // last step (its number in the workgroup's life) that had a new R
     int any_far;                           // last step with values out of the products' range
     uint32_t far[VS_MAX_SEQ / kBlock / 32];                // a bit for every stage that has some
 };
+
+// 16 or 4 bytes a lane from base + at straight to LDS, lane after lane from `to` on (the kernel itself waits for them)
+__device__ __forceinline__ void lds_load16(uint32_t at, const void* base, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
+}
+
+__device__ __forceinline__ void lds_load4(uint32_t at, const void* base, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
+}
 
 __device__ __forceinline__ int row_of_key(int key) { return (key & 0x27) | ((key >> 1) & 8) | ((key << 1) & 16); }
 
@@ -199,28 +228,42 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
     const int share = blockIdx.x;
     int64_t per, total;
     Place at;
-    if (!find(p, share, lane, &per, &total, &at)) return;
-    const int64_t mine = min(per, total - per * share);
+    const bool some = find(p, share, lane, &per, &total, &at);
+    const int64_t mine = some ? min(per, total - per * share) : 0;
+    if (tid == 0) {
+        // (the first of them has the unit's first block)
+        const bool ends = some && at.step > kStart && kStart + at.blocks - at.step <= mine;
+        *(joined(p) + share) = {ends ? share + 1 - static_cast<int>((per * share - at.step + kStart) / per) : 0, at.b, at.head, at.tile, at.base, {0, 0, 0}};
+    }
     if (tid < 2) lds.event[tid] = -1;
     if (tid == 0) lds.any_far = -1;
     for (int w = tid; w < VS_MAX_SEQ / kBlock / 32; w += kThreads) lds.far[w] = 0;
 
     // a thread's piece of a block: 32 channels of a key, and of V the words of eight tokens 4 c .. of two channels of the wavefront's 32
     const int key = tid >> 2, quarter = tid & 3, c = lane >> 4, m = lane & 15;
-    const uint32_t k_scale = kKScales + 4 * (16 * quarter + (key & 15)) + (key >> 4);
+    const uint32_t k_code = 16 * tid, k_scale = kKScales + 4 * (16 * quarter + (key & 15));       // (a word: byte key / 16, the wavefront's number)
+    const uint32_t scales = kKScales + 4 * (tid & 127);                    // what it asks for of the scales
     const uint32_t v_code = kVCodes + 1024 * wave + 16 * lane, v_scale = kVScales + 16 * (4 * c + wave);
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)smem));
-    const uint32_t k_to = lds0 + 4 * quarter * kChunkBytes + 16 * row_of_key(key);
-    const uint32_t v_to = lds0 + 2 * kKBytes + c * kWordBytes + 16 * (32 * wave + m);
-    const uint32_t k_from = lds0 + half * kChunkBytes + 16 * col;
-    const uint32_t v_from = lds0 + 2 * kKBytes + half * kWordBytes + 16 * col;
+    // buffer 0; the other one is kKBytes and kVBytes behind
+    const uint32_t k_to0 = lds0 + 4 * quarter * kChunkBytes + 16 * row_of_key(key), v_to0 = lds0 + 2 * kKBytes + c * kWordBytes + 16 * (32 * wave + m);
+    const uint32_t k_from0 = lds0 + half * kChunkBytes + 16 * col, v_from0 = lds0 + 2 * kKBytes + half * kWordBytes + 16 * col;
+    uint32_t k_to, v_to, k_from, v_from;                                   // of the stage that is next to be written and read
+    const uint32_t raw0 = lds0 + offsetof(Lds, raw);
+    // the scale byte of token `lane` for the wavefront's channels, and where it goes: word (c, u), token of the word
+    const uint32_t e_from = raw0 + kVScales + 16 * (4 * ((lane >> 2) & 3) + wave) + 4 * (lane >> 4) + (lane & 3);
+    const uint32_t e_to = lds0 + offsetof(Lds, scale) + 128 * wave + 2 * (16 * ((lane >> 2) & 3) + 8 * (lane >> 5) + 4 * ((lane >> 4) & 1) + (lane & 3));
+    const uint32_t scale_from = lds0 + offsetof(Lds, scale) + 128 * wave + 32 * c;
     typedef __attribute__((address_space(3))) u32x4* lds_u4;
+    typedef __attribute__((address_space(3))) uint32_t* lds_u1;
+    typedef __attribute__((address_space(3))) uint16_t* lds_h1;
+    typedef __attribute__((address_space(3))) uint8_t* lds_b1;
 
     bf16x8 qf[2][8], kf[2][8];
     half8_t vf[4][4], pb[2][2][2];
     f32x16 sc[2][2], oacc[2][4];
     float m_run[2], l_run[2];
-    uint4 raw_k, raw_v, raw_e;             // codes of K, codes of V and their scales on their way to LDS
+    u32x4 raw_k, raw_v, scale[2];          // codes of K, codes of V and their scales (tokens 0 .. 3, 16 .. 19 from 4 c on, and 32 further on)
     uint32_t raw_s;                        // K's scale
     int steps_done = 0;                    // numbers the steps for lds.event
     int64_t left = mine;
@@ -246,7 +289,11 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
             sure = min(sure, max(at.base + min(row0[rb], p.n_q - 1), 0));
             const uint16_t* const from = p.q + (static_cast<int64_t>(head[rb]) * p.n_q + row) * 128 + 8 * half;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) qf[rb][j] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(from + 16 * j));
+            for (int j = 0; j < 8; ++j) {
+                u32x4 x = *reinterpret_cast<const u32x4*>(from + 16 * j);
+                asm volatile("" : "+a"(x));                                // (else it is copied from there in front of every product)
+                qf[rb][j] = __builtin_bit_cast(bf16x8, x);
+            }
             m_run[rb] = -INFINITY;
             l_run[rb] = 0.0f;
 #pragma unroll
@@ -260,99 +307,98 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
 
         // ---- blocks: addresses a stage and more ahead ----
         int page = first_block / p.cache.page_blocks, in_page = first_block - page * p.cache.page_blocks, ahead = 0;
-        int entry = cache_page(p.cache, b, page);
         uint32_t there = 0;                                                // bit i: stage `now` + i has a page
+        const uint8_t* next_at = nullptr;                                  // the block that is asked for next
+        bool next_paged = false;
+        auto enter_page = [&]() __attribute__((always_inline)) {
+            const int entry = cache_page(p.cache, b, page);
+            next_paged = len > 0 && cache_paged(p.cache, entry);
+            next_at = p.cache.data + (next_paged ? cache_offset(p.cache, entry, g, in_page) : 0);
+        };
+        enter_page();
         auto next_block = [&]() __attribute__((always_inline)) -> const uint8_t* {
-            const bool paged = len > 0 && cache_paged(p.cache, entry);
-            const uint8_t* const from = p.cache.data + (paged ? cache_offset(p.cache, entry, g, in_page) : 0);
-            there = there >> 1 | (paged ? 8u : 0u);
+            const uint8_t* const from = next_at;
+            there = there >> 1 | (next_paged ? 16u : 0u);
             if (++ahead < nst) {                                           // (behind the last stage: that one again)
                 if (++in_page == p.cache.page_blocks) {
                     in_page = 0;
-                    entry = cache_page(p.cache, b, ++page);
+                    ++page;
+                    enter_page();
+                } else if (next_paged) {
+                    next_at += kBlockBytes;
                 }
             }
             return from;
         };
-        auto load_k = [&](const uint8_t* from) __attribute__((always_inline)) {
-            raw_k = *reinterpret_cast<const uint4*>(from + 16 * tid);
-            raw_s = from[k_scale];
+        auto request = [&](int st, int piece, const uint8_t* from) __attribute__((always_inline)) {       // piece 0 .. 2 of the block at `from`, for stage st
+            const uint32_t to = raw0 + (st & (kRing - 1)) * kRawBytes;
+            if (piece == 0) lds_load16(k_code, from, to + 1024 * wave);
+            if (piece == 1) lds_load16(v_code, from, to + kVCodes + 1024 * wave);
+            if (piece == 2) lds_load4(scales, from, to + kKScales + 256 * (wave & 1));
         };
-        auto load_v = [&](const uint8_t* from) __attribute__((always_inline)) {
-            raw_v = *reinterpret_cast<const uint4*>(from + v_code);
-            raw_e = *reinterpret_cast<const uint4*>(from + v_scale);
+        auto take_k = [&](int st) __attribute__((always_inline)) {
+            const uint32_t at = raw0 + (st & (kRing - 1)) * kRawBytes;
+            raw_k = *(lds_u4)(at + k_code);
+            raw_s = *(lds_u1)(at + k_scale);
+        };
+        auto take_v = [&](int st) __attribute__((always_inline)) {
+            raw_v = *(lds_u4)(raw0 + (st & (kRing - 1)) * kRawBytes + v_code);
+            scale[0] = *(lds_u4)scale_from;
+            scale[1] = *(lds_u4)(scale_from + 16);
         };
         auto live_of = [&](int st) __attribute__((always_inline)) { return min(len - (first_block + st) * kBlock, kBlock); };
-        const uint8_t* at_v;                                               // block that V is asked for next
-        const uint8_t* at_k;
+        const uint8_t* ahead_at = nullptr;                                 // block of stage sq + 4
 
-        // chunk i of this thread's four of K of stage st
-        auto put_k = [&](int st, int i) __attribute__((always_inline)) {
-            const uint32_t w = i == 0 ? raw_k.x : i == 1 ? raw_k.y : i == 2 ? raw_k.z : raw_k.w;
-            *(lds_u4)(k_to + (st & 1) * kKBytes + i * kChunkBytes) = __builtin_bit_cast(u32x4, dequantise8(w, __uint_as_float(raw_s << 23)));
+        // chunk i of this thread's four of K
+        auto put_k = [&](int i) __attribute__((always_inline)) {
+            if (i == 0) raw_s = (raw_s >> (8 * wave)) << 23;
+            *(lds_u4)(k_to + i * kChunkBytes) = __builtin_bit_cast(u32x4, dequantise8(raw_k[i], __uint_as_float(raw_s)));
         };
-        ushort2_t scale[8], most;
-        auto put_v_scale = [&](int i) __attribute__((always_inline)) {     // tokens 16 (i / 2) + 4 c + 2 (i % 2) and the next
-            const uint32_t e = i < 2 ? raw_e.x : i < 4 ? raw_e.y : i < 6 ? raw_e.z : raw_e.w;
-            const ushort2_t pair = __builtin_bit_cast(ushort2_t, __builtin_amdgcn_perm(0u, e, i & 1 ? 0x0c030c02u : 0x0c010c00u));
-            const ushort2_t over = pair - static_cast<uint16_t>(unit_mine - kSpan);
-            most = i == 0 ? over : __builtin_elementwise_max(most, over);
-            scale[i] = pair * static_cast<uint16_t>(1024) - static_cast<uint16_t>((unit_mine - kSpan - 1) << 10);
-        };
-        auto check_v = [&](int st, bool paged) __attribute__((always_inline)) {
-            if (__builtin_expect(__ballot(most[0] > kSpan || most[1] > kSpan) != 0, 0)) {   // not all of E in [R - 27, R]
-                const int live = paged ? live_of(st) : 0;
-                const uint32_t e[4] = {raw_e.x, raw_e.y, raw_e.z, raw_e.w};
-                int largest = 0;
-                auto in = [&](int i, int j) { return 16 * (i >> 1) + 4 * c + 2 * (i & 1) + j < live; };
-                auto byte = [&](int i, int j) { return static_cast<int>((e[i >> 1] >> (8 * (2 * (i & 1) + j))) & 255); };
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        if (in(i, j) && byte(i, j) < 255) largest = max(largest, byte(i, j));
-                largest = wave_max_int(largest);
+        // Scales of stage st's V: a lane turns one token's E into fp16, 2^(E - R + 13).
+        int e_of = 0;
+        auto ask_scale = [&](int st) __attribute__((always_inline)) { e_of = *(lds_b1)(e_from + (st & (kRing - 1)) * kRawBytes); };
+        auto put_scale = [&](int st, bool paged) __attribute__((always_inline)) {
+            int x = e_of - unit_mine + kSpan + 1;                          // 1 .. 28, or V is out of the range of fp16
+            bool fits = e_of != 0;
+            if (__builtin_expect(__ballot(fits && static_cast<uint32_t>(x - 1) > kSpan) != 0, 0)) {
+                const bool in = st < nst && lane < (paged ? live_of(st) : 0);
+                const int largest = wave_max_int(in && e_of < 255 ? e_of : 0);
                 if (largest > unit_mine) {
                     unit_mine = min(largest + 2, 254);
                     lds.event[st & 1] = steps_done + st;
+                    x = e_of - unit_mine + kSpan + 1;
                 }
-                bool far = false;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int x = byte(i, j) - unit_mine + kSpan + 1;
-                        const bool fits = in(i, j) && byte(i, j) < 255 && x > 0;
-                        scale[i][j] = fits ? static_cast<uint16_t>(x << 10) : 0;
-                        far |= in(i, j) && byte(i, j) > 0 && !fits;
-                    }
-                if (__any(far)) {
+                fits = in && e_of < 255 && x > 0;
+                const uint64_t far = __ballot(in && e_of > 0 && !fits);
+                if (far) {
                     lds.any_far = steps_done;
                     if (lane == 0) atomicOr(&lds.far[st >> 5], 1u << (st & 31));
                 }
             }
             lds.unit_of[st & 1][wave] = unit_mine;
+            *(lds_h1)e_to = static_cast<uint16_t>(fits ? x << 10 : 0);
         };
         uint32_t word[4];
-        auto put_v = [&](int st, int piece) __attribute__((always_inline)) {   // word 2 b + u (piece / 4), tokens 2 k, 2 k + 1 of its eight
+        auto put_v = [&](int piece) __attribute__((always_inline)) {   // word 2 b + u (piece / 4), tokens 2 k, 2 k + 1 of its eight
             const int i = piece >> 2, k = piece & 3, u = i & 1;
-            const uint32_t w = i == 0 ? raw_v.x : i == 1 ? raw_v.y : i == 2 ? raw_v.z : raw_v.w;
-            const half2_t s = __builtin_bit_cast(half2_t, scale[4 * u + k]);
+            const uint32_t w = raw_v[i];
+            const uint32_t of_tokens = scale[u][k];
+            const half2_t s = __builtin_bit_cast(half2_t, of_tokens);
             half2_t y;
             if (k == 0) y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0);
             if (k == 1) y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1);
             if (k == 2) y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2);
             if (k == 3) y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3);
             word[k] = __builtin_bit_cast(uint32_t, y * s);
-            if (k == 3) *(lds_u4)(v_to + (st & 1) * kVBytes + 4 * u * kWordBytes + 256 * (i >> 1)) = u32x4{word[0], word[1], word[2], word[3]};
+            if (k == 3) *(lds_u4)(v_to + 4 * u * kWordBytes + 256 * (i >> 1)) = u32x4{word[0], word[1], word[2], word[3]};
         };
 
-        auto read_k = [&](int st, int i) __attribute__((always_inline)) {  // fragment i % 8 of tile i / 8
-            const u32x4 x = *(lds_u4)(k_from + (st & 1) * kKBytes + 512 * (i >> 3) + 2 * kChunkBytes * (i & 7));
+        auto read_k = [&](int i) __attribute__((always_inline)) {  // fragment i % 8 of tile i / 8
+            const u32x4 x = *(lds_u4)(k_from + 512 * (i >> 3) + 2 * kChunkBytes * (i & 7));
             kf[i >> 3][i & 7] = __builtin_bit_cast(bf16x8, x);
         };
-        auto read_v = [&](int st, int i) __attribute__((always_inline)) {  // tokens 16 (i / 4) .., channels 32 (i % 4) ..
-            const u32x4 x = *(lds_u4)(v_from + (st & 1) * kVBytes + 2 * kWordBytes * (i >> 2) + 512 * (i & 3));
+        auto read_v = [&](int i) __attribute__((always_inline)) {  // tokens 16 (i / 4) .., channels 32 (i % 4) ..
+            const u32x4 x = *(lds_u4)(v_from + 2 * kWordBytes * (i >> 2) + 512 * (i & 3));
             vf[i >> 2][i & 3] = __builtin_bit_cast(half8_t, x);
         };
 
@@ -369,6 +415,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                 unit_now[j] = unit;
             }
         };
+        int event = -1;                                                    // lds.event of the stage whose P V is next
 #define VS_FENCE() __builtin_amdgcn_sched_barrier(0)
         // MR: the row block whose matrix products are issued; VR = 1 - MR: the one whose softmax runs.  sq: stage whose scores are computed (HAS_Q);
         // sq - 1: stage whose P V is accumulated (HAS_P); sv: stage whose scores go through the softmax (HAS_S).
@@ -389,15 +436,12 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                 oacc[MR][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[i >> 2][i & 3], pb[MR][i >> 3][(i >> 2) & 1], oacc[MR][i & 3], 0, 0, 0);
             };
             if constexpr (MR == 1) {
-                if constexpr (HAS_Q) {
-                    at_v = at_k;
-                    at_k = next_block();                                   // block of stage sq + 3 (of sq + 2: at_v)
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                if constexpr (HAS_Q) ahead_at = next_block();
+                asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (stage sq + 3 is on its way)
                 VS_FENCE();
             }
             if constexpr (MR == 0 && HAS_P) {
-                if (__builtin_expect(__builtin_amdgcn_readfirstlane(lds.event[(sq - 1) & 1]) == steps_done + sq - 1, 0)) new_units(sq - 1);
+                if (__builtin_expect(__builtin_amdgcn_readfirstlane(event) == steps_done + sq - 1, 0)) new_units(sq - 1);
                 VS_FENCE();
             }
             // Softmax elements as a three-deep pipeline: step k scales element k, takes the exponential of element k - 1 and adds element k - 2 to the row
@@ -446,14 +490,18 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
             auto turn = [&](auto index) __attribute__((always_inline)) {
                 constexpr int j = decltype(index)::value;
                 if constexpr (HAS_Q && MR == 0) {
-                    if constexpr (j < 8) put_v_scale(j);
-                    if constexpr (j == 9) check_v(sq, there & 2);          // (`there` is at the stage in front)
-                    if constexpr (j >= 10 && j < 26) put_v(sq, j - 10);
-                    if constexpr (j == 27) load_v(at_v);
+                    if constexpr (j == 0) take_v(sq);
+                    if constexpr (j >= 4 && j < 28 && (j - 4) % 3 != 2) put_v((j - 4) / 3 * 2 + (j - 4) % 3);
+                    if constexpr (j == 28) v_to = 2 * v_to0 + kVBytes - v_to;
                 }
                 if constexpr (HAS_Q && MR == 1) {
-                    if constexpr (j >= 2 && j < 18 && (j - 2) % 4 == 0) put_k(sq + 2, (j - 2) / 4);
-                    if constexpr (j == 18) load_k(at_k);
+                    if constexpr (j == 0) take_k(sq + 2);
+                    if constexpr (j >= 4 && j < 16 && j % 3 == 1) put_k((j - 4) / 3);
+                    if constexpr (j == 14) k_to = 2 * k_to0 + kKBytes - k_to;
+                    if constexpr (j == 15) ask_scale(sq + 1);
+                    if constexpr (j >= 17 && j < 20) request(sq + 4, j - 17, ahead_at);
+                    if constexpr (j == 22) put_scale(sq + 1, there & 2);
+                    if constexpr (j == 30) event = lds.event[sq & 1];
                 }
             };
             auto rescale = [&](float mx) __attribute__((always_inline)) -> bool {
@@ -523,7 +571,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                 constexpr int j = decltype(index)::value;
                 if constexpr (HAS_Q) qmfma(j >> 1, j & 1);
                 VS_FENCE();
-                if constexpr (MR == 0 && HAS_P) read_v(sq - 1, j);
+                if constexpr (MR == 0 && HAS_P) read_v(j);
                 turn(index);
                 if constexpr (HAS_S) exp_share(j);
                 VS_FENCE();
@@ -532,7 +580,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                 constexpr int j = decltype(index)::value;
                 if constexpr (HAS_Q) qmfma(j >> 1, j & 1);
                 VS_FENCE();
-                if constexpr (MR == 0 && HAS_P) read_v(sq - 1, j);
+                if constexpr (MR == 0 && HAS_P) read_v(j);
                 turn(index);
                 if constexpr (HAS_S) exp_share(j);
                 VS_FENCE();
@@ -543,7 +591,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                     if (!search) look_again();
                 if constexpr (HAS_P) pmfma(j);
                 VS_FENCE();
-                if constexpr (MR == 1 && HAS_Q) read_k(sq + 1, j);
+                if constexpr (MR == 1 && HAS_Q) read_k(j);
                 turn(std::integral_constant<int, 16 + j>{});
                 if constexpr (HAS_S) exp_share(16 + j);
                 VS_FENCE();
@@ -552,6 +600,8 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                 expsteps_upto(34);
                 l_run[VR] += lsum;
             }
+            if constexpr (MR == 1 && HAS_Q) k_from = 2 * k_from0 + kKBytes - k_from;
+            if constexpr (MR == 0 && HAS_P) v_from = 2 * v_from0 + kVBytes - v_from;
             VS_FENCE();
         };
 #undef VS_FENCE
@@ -561,37 +611,32 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
         using R0 = std::integral_constant<int, 0>;
         using R1 = std::integral_constant<int, 1>;
 
-        // ---- the first blocks; `there`: bits of stages 0, 1, 2 end at 0 .. 2 once Y(0) has asked for stage 3 ----
-        const uint8_t* const at0 = next_block();
-        load_k(at0);
-        load_v(at0);
-        const uint4 k0 = raw_k;
-        const uint32_t s0 = raw_s;
-        const uint8_t* const at1 = next_block();
-        load_k(at1);
-        const uint4 k1 = raw_k;
-        const uint32_t s1 = raw_s;
-        at_k = next_block();
-        load_k(at_k);
-        at_v = at1;
+        // ---- the first blocks ----
+        k_to = k_to0;
+        v_to = v_to0;
+        k_from = k_from0;
+        v_from = v_from0;
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the unit before this one is out of every buffer
-        {
-            const uint4 k2 = raw_k;
-            const uint32_t s2 = raw_s;
-            raw_k = k0;
-            raw_s = s0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) put_k(0, i);
-            raw_k = k1;
-            raw_s = s1;
+        for (int st = 0; st < kRing; ++st) {
+            const uint8_t* const from = next_block();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) put_k(1, i);
-            raw_k = k2;
-            raw_s = s2;
+            for (int piece = 0; piece < 3; ++piece) request(st, piece, from);
+        }
+        asm volatile("s_waitcnt vmcnt(6)\n\ts_barrier" ::: "memory");           // (scales are read by all)
+        ask_scale(0);
+        put_scale(0, there & 2);
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            take_k(st);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put_k(i);
+            k_to = 2 * k_to0 + kKBytes - k_to;
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < 16; ++i) read_k(0, i);
+        for (int i = 0; i < 16; ++i) read_k(i);
+        k_from = 2 * k_from0 + kKBytes - k_from;
         slot(R0{}, T{}, F{}, F{}, true, 0, 0);                              // X(0): scores of block 0
         slot(R1{}, T{}, F{}, T{}, true, 0, 0);                              // Y(0): scores of block 1; softmax of block 0
         if (nst > 1) {
@@ -613,18 +658,22 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
         slot(R0{}, F{}, T{}, T{}, true, nst, nst - 1);                      // X(nst): P V of block 0; softmax of block 1
         slot(R1{}, F{}, T{}, F{}, true, nst, nst);                          // Y(nst): P V of block 1
 
-        // ---- what the products of V do not have ----
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        // ---- what the products of V do not have (and nothing that was asked for beyond the last stage is on its way any more) ----
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (__builtin_expect(__builtin_amdgcn_readfirstlane(lds.any_far) == steps_done, 0)) {
             for (int w = 0; 32 * w < nst; ++w)
                 for (uint32_t bits = __builtin_amdgcn_readfirstlane(lds.far[w]); bits; bits &= bits - 1) {
                     const int st = 32 * w + __builtin_ctz(bits), live = live_of(st);
                     const uint8_t* const from = cache_block(p.cache, b, g, first_block + st);     // (a block without a page has no bit)
-                    load_k(from);
-                    load_v(from);
+                    raw_k = *reinterpret_cast<const u32x4*>(from + k_code);
+                    raw_s = *reinterpret_cast<const uint32_t*>(from + k_scale);
+                    raw_v = *reinterpret_cast<const u32x4*>(from + v_code);
+                    const u32x4 raw_e = *reinterpret_cast<const u32x4*>(from + v_scale);
+                    k_to = k_to0;
+                    k_from = k_from0;
+                    v_from = v_from0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) put_k(0, i);
-                    const uint32_t e[4] = {raw_e.x, raw_e.y, raw_e.z, raw_e.w}, v[4] = {raw_v.x, raw_v.y, raw_v.z, raw_v.w};
+                    for (int i = 0; i < 4; ++i) put_k(i);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int u = i & 1;
@@ -633,15 +682,15 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                             uint32_t x[2];
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
-                                const int which = 4 * u + k, E = static_cast<int>((e[which >> 1] >> (8 * (2 * (which & 1) + j))) & 255);
+                                const int which = 4 * u + k, E = static_cast<int>((raw_e[which >> 1] >> (8 * (2 * (which & 1) + j))) & 255);
                                 const int up = E - unit_mine + kTop + 127;                        // exponent of the scale in fp32
                                 const bool far = 16 * (which >> 1) + 4 * c + 2 * (which & 1) + j < live && E < 255 && E < unit_mine - kSpan && up > 0;
-                                x[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[i], __uint_as_float(static_cast<uint32_t>(far ? up : 127) << 23), decltype(k)::value));
+                                x[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw_v[i], __uint_as_float(static_cast<uint32_t>(far ? up : 127) << 23), decltype(k)::value));
                                 if (!far) x[j] = 0;
                             }
                             y[k] = __builtin_amdgcn_perm(x[1], x[0], 0x07060100u);
                         });
-                        *(lds_u4)(v_to + 4 * u * kWordBytes + 256 * (i >> 1)) = u32x4{y[0], y[1], y[2], y[3]};
+                        *(lds_u4)(v_to0 + 4 * u * kWordBytes + 256 * (i >> 1)) = u32x4{y[0], y[1], y[2], y[3]};
                     }
                     __syncthreads();
                     static_for<2>([&](auto rb_tag) __attribute__((always_inline)) {
@@ -652,7 +701,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                             for (int e = 0; e < 16; ++e) sc[rb][u][e] = 0.0f;
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
-                                read_k(0, 8 * u + k);
+                                read_k(8 * u + k);
                                 sc[rb][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][k], qf[rb][k], sc[rb][u], 0, 0, 0);
                             }
                         }
@@ -677,7 +726,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                             const bf16x8 z = __builtin_bit_cast(bf16x8, u32x4{low[0], low[1], low[2], low[3]});
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                read_v(0, 4 * i + j);
+                                read_v(4 * i + j);
                                 const bf16x8 y = __builtin_bit_cast(bf16x8, vf[i][j]);
                                 oacc[rb][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, a, oacc[rb][j], 0, 0, 0);
                                 oacc[rb][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, z, oacc[rb][j], 0, 0, 0);
@@ -742,12 +791,10 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
 // The parts of a unit that several workgroups shared.  Workgroup (s, y): the unit that share s begins with, if it began before and ends there; rows
 // 32 y .. of it.  The first part stands in its share's second slot, the others in their shares' first.
 __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillParams p) {
-    int64_t per, total;
-    Place at;
-    const int share = blockIdx.x, lane = threadIdx.x & 63;
-    if (!find(p, share, lane, &per, &total, &at) || at.step <= kStart) return;
-    if (kStart + at.blocks - at.step > min(per, total - per * share)) return;              // a later share has the end
-    const int first = static_cast<int>((per * share - at.step + kStart) / per), parts = share - first + 1;
+    const int share = blockIdx.x;
+    const Joined at = joined(p)[share];
+    const int parts = at.parts, first = share + 1 - parts;
+    if (parts <= 1) return;
     const int w = blockIdx.y, row = at.tile * p.tok + 32 * (w / p.hc) + (threadIdx.x >> 3);
     if (row >= p.n_q) return;
     const int g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc);
@@ -755,19 +802,37 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillPar
     const int in_unit = 32 * w + (threadIdx.x >> 3), channel = 4 * (threadIdx.x & 7);
     auto slot_of = [&](int i) { return static_cast<int64_t>(i == 0 ? 2 * first + 1 : 2 * (first + i)) * kUnitRows + in_unit; };
     float m = -INFINITY, l = 0.0f;
-    for (int i = 0; i < parts; ++i) m = fmaxf(m, part_stat(p)[slot_of(i)].x);
     float4 y[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i = 0; i < parts; ++i) {
-        const int64_t slot = slot_of(i);
-        const float2 x = part_stat(p)[slot];
-        const float f = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.x - m);
-        l = fmaf(x.y, f, l);
+    for (int i = 0; i < parts; i += kAhead) {
+        float4 z[kAhead][4];
+        float2 x[kAhead];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float4 z = *reinterpret_cast<const float4*>(p.part + slot * 128 + 32 * j + channel);
-            y[j] = make_float4(fmaf(z.x, f, y[j].x), fmaf(z.y, f, y[j].y), fmaf(z.z, f, y[j].z), fmaf(z.w, f, y[j].w));
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t slot = slot_of(min(i + k, parts - 1));
+            x[k] = part_stat(p)[slot];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[k][j] = *reinterpret_cast<const float4*>(p.part + slot * 128 + 32 * j + channel);
+        }
+        float most = m;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i + k >= parts) x[k].x = -INFINITY;                        // the last one again: no weight
+            most = fmaxf(most, x[k].x);
+        }
+        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - most);
+        m = most;
+        l *= f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = make_float4(y[j].x * f, y[j].y * f, y[j].z * f, y[j].w * f);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (x[k].x == -INFINITY) continue;
+            const float g = __builtin_amdgcn_exp2f(x[k].x - m);
+            l = fmaf(x[k].y, g, l);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = make_float4(fmaf(z[k][j].x, g, y[j].x), fmaf(z[k][j].y, g, y[j].y), fmaf(z[k][j].z, g, y[j].z), fmaf(z[k][j].w, g, y[j].w));
         }
     }
     const bool none = at.base + row < 0 || l == 0.0f;
@@ -802,7 +867,7 @@ void plan(PrefillParams& p, int batch, int q_heads, int kv_heads, int64_t n_q, i
     p.shares = static_cast<int>(shares < kShares ? shares : kShares);
 }
 
-size_t part_bytes(const PrefillParams& p) { return static_cast<size_t>(2 * p.shares) * kUnitRows * (VS_HEAD_DIM + 2) * sizeof(float); }
+size_t part_bytes(const PrefillParams& p) { return static_cast<size_t>(p.shares) * (2 * kUnitRows * (VS_HEAD_DIM + 2) * sizeof(float) + sizeof(Joined)); }
 
 }  // namespace
 
