@@ -27,10 +27,12 @@ constexpr float kGrown = 8.0f;                             // log2 units by whic
 constexpr float kLift = 7.0f;                              // weights are held times 2^7
 constexpr float kGrownSum = 32768.0f;                      // 2^(8 + 7): no weight of a lane is larger if their sum is not
 constexpr float kSafe = 1024.0f;                           // scores (log2 units) up to which a product and a difference in one rounding are good enough
+constexpr int kPartFloats = kUnitRows * 128 + 1088;          // (4352 bytes more: parts a power of two apart would all begin in the same memory channels)
 constexpr int kShares = 256;                               // a workgroup for every compute unit
 constexpr int kStart = 3;                                  // steps that a unit's start and end count for
 constexpr int kAhead = 4;                                  // parts that are asked for at once
-constexpr int kSteps = 4;                                  // of a workgroup, if there are so few
+constexpr int kJoinRows = kThreads / 32;                   // rows of a workgroup of the second kernel
+constexpr int kSteps = 2;                                  // of a workgroup, if there are so few
 constexpr int kTop = 13;                                   // fp16 exponent of a code with E = R: 6 * 2^13 < 65504
 constexpr int kSpan = 27;                                  // E from R - 27 (2^-14 in fp16) to R
 constexpr uint32_t kLargeUnit = 200;                       // R, from 15 on, up to which any E outside shows in the upper half of the byte E - R + 15
@@ -40,7 +42,7 @@ struct PrefillParams {
     const uint16_t* q;
     uint16_t* o;
     float* lse;
-    float* part;                           // [2 shares][256 rows][128] sums, then [2 shares][256] (maximum, sum of weights), then [shares] Joined
+    float* part;                           // [2 shares][kPartFloats] sums, rows of 128, then [2 shares][256] (maximum, sum of weights), then [shares] Joined
     int batch, q_heads, n_q, group, hc;
     int tok, tok_blocks;                   // tokens of a unit, 256 / hc, and that in blocks
     int tiles;                             // units of a sequence's head chunk
@@ -53,8 +55,8 @@ struct PrefillParams {
 // A unit of sequence b has kStart steps in front (its start and end cost as much) and one for each block up to its last row's position.
 struct Sequence {
     int len, base, first;                  // base: position of row 0;  first: blocks up to row 0, may be negative
-    __device__ __forceinline__ Sequence(const PrefillParams& p, int b, bool scalar) {
-        len = b < p.batch ? (scalar ? cache_length_scalar(p.cache, b) : cache_length(p.cache, b)) : 0;
+    __device__ __forceinline__ Sequence(const PrefillParams& p, int length) {
+        len = length;
         base = len - p.n_q;
         first = (base + kBlock - 1) >> 6;
     }
@@ -99,14 +101,13 @@ struct Place {
             tile = 0;
             if (++head == p.heads) {
                 head = 0;
-                ++b;
+                if (++b < p.batch) len = cache_length_scalar(p.cache, b);
             }
         }
         enter(p);
     }
     __device__ __forceinline__ void enter(const PrefillParams& p) {
-        const Sequence s(p, b, true);
-        len = s.len;
+        const Sequence s(p, len);
         base = s.base;
         blocks = s.blocks(p, tile);
     }
@@ -114,8 +115,11 @@ struct Place {
 
 // Steps of a share, and where share `share` begins (false: behind the end).
 __device__ __forceinline__ bool find(const PrefillParams& p, int share, int lane, int64_t* per, int64_t* total, Place* at) {
-    int64_t mine = lane < p.batch ? Sequence(p, lane, false).steps(p) : 0, upto = scan64(mine), all = lane64(upto, 63);
-    for (int b = 64; b < p.batch; b += 64) all += lane64(scan64(b + lane < p.batch ? Sequence(p, b + lane, false).steps(p) : 0), 63);
+    auto length = [&](int b) { return b < p.batch ? cache_length(p.cache, b) : 0; };
+    auto steps = [&](int b, int len) { return b < p.batch ? Sequence(p, len).steps(p) : 0; };
+    int len = length(lane);
+    int64_t mine = steps(lane, len), upto = scan64(mine), all = lane64(upto, 63);
+    for (int b = 64; b < p.batch; b += 64) all += lane64(scan64(steps(b + lane, length(b + lane))), 63);
     all *= p.heads;
     *total = all;
     *per = (all + p.shares - 1) / p.shares;
@@ -123,18 +127,20 @@ __device__ __forceinline__ bool find(const PrefillParams& p, int share, int lane
     if (x >= all) return false;
     for (int b = 0;; b += 64) {
         if (b > 0) {
-            mine = b + lane < p.batch ? Sequence(p, b + lane, false).steps(p) : 0;
+            len = length(b + lane);
+            mine = steps(b + lane, len);
             upto = scan64(mine);
         }
         const int l = __popcll(__ballot(upto * p.heads <= x));
         if (l < 64) {
             at->b = b + l;
+            at->len = __builtin_amdgcn_readlane(len, l);
             x -= lane64(upto - mine, l) * p.heads;
             break;
         }
         x -= lane64(upto, 63) * p.heads;
     }
-    const Sequence s(p, at->b, true);
+    const Sequence s(p, at->len);
     const int64_t each = s.steps(p);
     at->head = all >> 31 ? static_cast<int>(x / each) : static_cast<int>(static_cast<uint32_t>(x) / static_cast<uint32_t>(each));
     x -= at->head * each;
@@ -150,7 +156,7 @@ __device__ __forceinline__ bool find(const PrefillParams& p, int share, int lane
     return true;
 }
 
-__device__ __forceinline__ float2* part_stat(const PrefillParams& p) { return reinterpret_cast<float2*>(p.part + static_cast<int64_t>(2 * p.shares) * kUnitRows * 128); }
+__device__ __forceinline__ float2* part_stat(const PrefillParams& p) { return reinterpret_cast<float2*>(p.part + static_cast<int64_t>(2 * p.shares) * kPartFloats); }
 
 // The unit that a share ends and that others began, for the second kernel; parts: shares that have some of its blocks, 0: there is none.
 struct Joined {
@@ -287,13 +293,6 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
             const int row = min(row0[rb] + col, p.n_q - 1);                // (rows behind the last one are not stored)
             limit[rb] = max(at.base + row, 0);                             // (nor are rows in front of their sequence)
             sure = min(sure, max(at.base + min(row0[rb], p.n_q - 1), 0));
-            const uint16_t* const from = p.q + (static_cast<int64_t>(head[rb]) * p.n_q + row) * 128 + 8 * half;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                u32x4 x = *reinterpret_cast<const u32x4*>(from + 16 * j);
-                asm volatile("" : "+a"(x));                                // (else it is copied from there in front of every product)
-                qf[rb][j] = __builtin_bit_cast(bf16x8, x);
-            }
             m_run[rb] = -INFINITY;
             l_run[rb] = 0.0f;
 #pragma unroll
@@ -491,15 +490,15 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                 constexpr int j = decltype(index)::value;
                 if constexpr (HAS_Q && MR == 0) {
                     if constexpr (j == 0) take_v(sq);
-                    if constexpr (j >= 4 && j < 28 && (j - 4) % 3 != 2) put_v((j - 4) / 3 * 2 + (j - 4) % 3);
-                    if constexpr (j == 28) v_to = 2 * v_to0 + kVBytes - v_to;
+                    if constexpr (j >= 14 && j < 30) put_v(j - 14);
+                    if constexpr (j == 30) v_to = 2 * v_to0 + kVBytes - v_to;
                 }
                 if constexpr (HAS_Q && MR == 1) {
                     if constexpr (j == 0) take_k(sq + 2);
-                    if constexpr (j >= 4 && j < 16 && j % 3 == 1) put_k((j - 4) / 3);
+                    if constexpr (j >= 4 && j < 12 && j % 2 == 0) put_k((j - 4) / 2);
                     if constexpr (j == 14) k_to = 2 * k_to0 + kKBytes - k_to;
                     if constexpr (j == 15) ask_scale(sq + 1);
-                    if constexpr (j >= 17 && j < 20) request(sq + 4, j - 17, ahead_at);
+                    if constexpr (j == 6 || j == 9 || j == 12) request(sq + 4, (j - 6) / 3, ahead_at);
                     if constexpr (j == 22) put_scale(sq + 1, there & 2);
                     if constexpr (j == 30) event = lds.event[sq & 1];
                 }
@@ -622,6 +621,17 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
             const uint8_t* const from = next_block();
 #pragma unroll
             for (int piece = 0; piece < 3; ++piece) request(st, piece, from);
+        }
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) {
+            const int row = min(row0[rb] + col, p.n_q - 1);
+            const uint16_t* const from = p.q + (static_cast<int64_t>(head[rb]) * p.n_q + row) * 128 + 8 * half;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                u32x4 x = *reinterpret_cast<const u32x4*>(from + 16 * j);
+                asm volatile("" : "+a"(x));                                // (else it is copied from there in front of every product)
+                qf[rb][j] = __builtin_bit_cast(bf16x8, x);
+            }
         }
         asm volatile("s_waitcnt vmcnt(6)\n\ts_barrier" ::: "memory");           // (scales are read by all)
         ask_scale(0);
@@ -771,7 +781,8 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                     }
                 if (p.lse && half == 0) p.lse[r] = none ? -INFINITY : (m_run[rb] * p.c + (log2f(l) - kLift)) * 0.69314718055994530942f;
             } else {
-                const int64_t r = static_cast<int64_t>(slot_of) * kUnitRows + 32 * (2 * wave + rb) + col;
+                const int r = 32 * (2 * wave + rb) + col;
+                float* const to = p.part + static_cast<int64_t>(slot_of) * kPartFloats + r * 128;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -779,41 +790,38 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                         float y[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) y[i] = __builtin_ldexpf(oacc[rb][j][4 * a + i], unit_now[j] - 127 - kTop);
-                        *reinterpret_cast<float4*>(p.part + r * 128 + 32 * j + 8 * a + 4 * half) = make_float4(y[0], y[1], y[2], y[3]);
+                        *reinterpret_cast<float4*>(to + 32 * j + 8 * a + 4 * half) = make_float4(y[0], y[1], y[2], y[3]);
                     }
-                if (half == 0) part_stat(p)[r] = make_float2(m_run[rb] * p.c, l);
+                if (half == 0) part_stat(p)[static_cast<int64_t>(slot_of) * kUnitRows + r] = make_float2(m_run[rb] * p.c, l);
             }
         }
         steps_done += nst + 2;
     }
 }
 
-// The parts of a unit that several workgroups shared.  Workgroup (s, y): the unit that share s begins with, if it began before and ends there; rows
-// 32 y .. of it.  The first part stands in its share's second slot, the others in their shares' first.
+// The parts of a unit that several workgroups shared.  Workgroup (x, s): the unit that share s ends, if others began it; rows 8 x .. of its 256, 32 lanes
+// each.  The first part stands in its share's second slot, the others in their shares' first.
 __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillParams p) {
-    const int share = blockIdx.x;
+    const int share = blockIdx.y;
     const Joined at = joined(p)[share];
     const int parts = at.parts, first = share + 1 - parts;
     if (parts <= 1) return;
-    const int w = blockIdx.y, row = at.tile * p.tok + 32 * (w / p.hc) + (threadIdx.x >> 3);
+    const int in_unit = kJoinRows * blockIdx.x + (threadIdx.x >> 5), channel = 4 * (threadIdx.x & 31);
+    const int w = in_unit >> 5, row = at.tile * p.tok + 32 * (w / p.hc) + (in_unit & 31);
     if (row >= p.n_q) return;
     const int g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc);
     const int64_t r = static_cast<int64_t>(at.b * p.q_heads + g * p.group + hchunk * p.hc + w % p.hc) * p.n_q + row;
-    const int in_unit = 32 * w + (threadIdx.x >> 3), channel = 4 * (threadIdx.x & 7);
-    auto slot_of = [&](int i) { return static_cast<int64_t>(i == 0 ? 2 * first + 1 : 2 * (first + i)) * kUnitRows + in_unit; };
     float m = -INFINITY, l = 0.0f;
-    float4 y[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     for (int i = 0; i < parts; i += kAhead) {
-        float4 z[kAhead][4];
+        float4 z[kAhead];
         float2 x[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const int64_t slot = slot_of(min(i + k, parts - 1));
-            x[k] = part_stat(p)[slot];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) z[k][j] = *reinterpret_cast<const float4*>(p.part + slot * 128 + 32 * j + channel);
+            const int part = min(i + k, parts - 1);
+            const int64_t slot = part == 0 ? 2 * first + 1 : 2 * (first + part);
+            x[k] = part_stat(p)[slot * kUnitRows + in_unit];
+            z[k] = *reinterpret_cast<const float4*>(p.part + slot * kPartFloats + in_unit * 128 + channel);
         }
         float most = m;
 #pragma unroll
@@ -824,24 +832,19 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillPar
         const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - most);
         m = most;
         l *= f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = make_float4(y[j].x * f, y[j].y * f, y[j].z * f, y[j].w * f);
+        y = make_float4(y.x * f, y.y * f, y.z * f, y.w * f);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (x[k].x == -INFINITY) continue;
-            const float g = __builtin_amdgcn_exp2f(x[k].x - m);
-            l = fmaf(x[k].y, g, l);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = make_float4(fmaf(z[k][j].x, g, y[j].x), fmaf(z[k][j].y, g, y[j].y), fmaf(z[k][j].z, g, y[j].z), fmaf(z[k][j].w, g, y[j].w));
+            const float h = __builtin_amdgcn_exp2f(x[k].x - m);
+            l = fmaf(x[k].y, h, l);
+            y = make_float4(fmaf(z[k].x, h, y.x), fmaf(z[k].y, h, y.y), fmaf(z[k].z, h, y.z), fmaf(z[k].w, h, y.w));
         }
     }
     const bool none = at.base + row < 0 || l == 0.0f;
     const float inv = none ? 0.0f : 1.0f / l;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (none) y[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        *reinterpret_cast<uint2*>(p.o + r * 128 + 32 * j + channel) = make_uint2(pack_bf16(y[j].x * inv, y[j].y * inv), pack_bf16(y[j].z * inv, y[j].w * inv));
-    }
+    if (none) y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    *reinterpret_cast<uint2*>(p.o + r * 128 + channel) = make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
     if (p.lse && channel == 0) p.lse[r] = none ? -INFINITY : (m + (log2f(l) - kLift)) * 0.69314718055994530942f;
 }
 
@@ -867,7 +870,7 @@ void plan(PrefillParams& p, int batch, int q_heads, int kv_heads, int64_t n_q, i
     p.shares = static_cast<int>(shares < kShares ? shares : kShares);
 }
 
-size_t part_bytes(const PrefillParams& p) { return static_cast<size_t>(p.shares) * (2 * kUnitRows * (VS_HEAD_DIM + 2) * sizeof(float) + sizeof(Joined)); }
+size_t part_bytes(const PrefillParams& p) { return static_cast<size_t>(p.shares) * (2 * kPartFloats * sizeof(float) + 2 * kUnitRows * sizeof(float2) + sizeof(Joined)); }
 
 }  // namespace
 
@@ -906,7 +909,7 @@ extern "C" int vs_cache_prefill(const void* q, const vs_cache_t* cache, int batc
     hipLaunchKernelGGL(prefill_kernel, dim3(p.shares), dim3(kThreads), sizeof(Lds), s, p);
     VS_LAUNCH_CHECK();
     if (p.shares > 1) {
-        hipLaunchKernelGGL(prefill_join_kernel, dim3(p.shares, kUnitRows / 32), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL(prefill_join_kernel, dim3(kUnitRows / kJoinRows, p.shares), dim3(kThreads), 0, s, p);
         VS_LAUNCH_CHECK();
     }
     return VS_OK;
