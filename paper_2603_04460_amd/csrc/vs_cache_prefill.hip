@@ -31,7 +31,6 @@ constexpr int kPartFloats = kUnitRows * 128 + 1088;          // (4352 bytes more
 constexpr int kShares = 256;                               // a workgroup for every compute unit
 constexpr int kStart = 3;                                  // steps that a unit's start and end count for
 constexpr int kAhead = 4;                                  // parts that are asked for at once
-constexpr int kJoinRows = kThreads / 32;                   // rows of a workgroup of the second kernel
 constexpr int kSteps = 2;                                  // of a workgroup, if there are so few
 constexpr int kTop = 13;                                   // fp16 exponent of a code with E = R: 6 * 2^13 < 65504
 constexpr int kSpan = 27;                                  // E from R - 27 (2^-14 in fp16) to R
@@ -649,12 +648,11 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
         k_from = 2 * k_from0 + kKBytes - k_from;
         slot(R0{}, T{}, F{}, F{}, true, 0, 0);                              // X(0): scores of block 0
         slot(R1{}, T{}, F{}, T{}, true, 0, 0);                              // Y(0): scores of block 1; softmax of block 0
-        if (nst > 1) {
-            bool search = true;
-            slot(R0{}, T{}, T{}, T{}, true, 1, 0);                          // X(1): softmax of block 1 for stage 0
-            // Y(i) and X(i + 1) have the softmax of stage i: without a mask and a search for the maximum where every row of the wavefront sees all of it and has
-            // a maximum that serves already
-            for (int i = 1; i < nst - 1; ++i) {
+        // Y(i) and X(i + 1) have the softmax of stage i: without a mask and a search for the maximum where every row of the wavefront sees all of it and has
+        // a maximum that serves already
+        bool search = true;
+        slot(R0{}, T{}, T{}, T{}, true, 1, 0);                             // X(1): softmax of block 1 for stage 0
+        for (int i = 1; i < nst; ++i) {
                 if (search) {
                     const float least = fminf(m_run[0], m_run[1]), largest = fmaxf(m_run[0], m_run[1]);
                     ready = __all(least * p.c >= -kSafe && largest * p.c <= kSafe);
@@ -662,10 +660,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                 search = !(ready && (there & 2) && (first_block + i) * kBlock + kBlock - 1 <= sure);
                 slot(R1{}, T{}, T{}, T{}, search, i, i);
                 slot(R0{}, T{}, T{}, T{}, search, i + 1, i);
-            }
-            slot(R1{}, T{}, T{}, T{}, true, nst - 1, nst - 1);
         }
-        slot(R0{}, F{}, T{}, T{}, true, nst, nst - 1);                      // X(nst): P V of block 0; softmax of block 1
         slot(R1{}, F{}, T{}, F{}, true, nst, nst);                          // Y(nst): P V of block 1
 
         // ---- what the products of V do not have (and nothing that was asked for beyond the last stage is on its way any more) ----
@@ -781,8 +776,8 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                     }
                 if (p.lse && half == 0) p.lse[r] = none ? -INFINITY : (m_run[rb] * p.c + (log2f(l) - kLift)) * 0.69314718055994530942f;
             } else {
-                const int r = 32 * (2 * wave + rb) + col;
-                float* const to = p.part + static_cast<int64_t>(slot_of) * kPartFloats + r * 128;
+                // (in the order of the registers: lanes write memory in a row)
+                float4* const to = reinterpret_cast<float4*>(p.part + static_cast<int64_t>(slot_of) * kPartFloats) + 16 * 64 * (2 * wave + rb) + lane;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -790,38 +785,38 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                         float y[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) y[i] = __builtin_ldexpf(oacc[rb][j][4 * a + i], unit_now[j] - 127 - kTop);
-                        *reinterpret_cast<float4*>(to + 32 * j + 8 * a + 4 * half) = make_float4(y[0], y[1], y[2], y[3]);
+                        to[64 * (4 * j + a)] = make_float4(y[0], y[1], y[2], y[3]);
                     }
-                if (half == 0) part_stat(p)[static_cast<int64_t>(slot_of) * kUnitRows + r] = make_float2(m_run[rb] * p.c, l);
+                if (half == 0) part_stat(p)[static_cast<int64_t>(slot_of) * kUnitRows + 32 * (2 * wave + rb) + col] = make_float2(m_run[rb] * p.c, l);
             }
         }
         steps_done += nst + 2;
     }
 }
 
-// The parts of a unit that several workgroups shared.  Workgroup (x, s): the unit that share s ends, if others began it; rows 8 x .. of its 256, 32 lanes
-// each.  The first part stands in its share's second slot, the others in their shares' first.
+// The parts of a unit that several workgroups shared.  Workgroup (x, s): the unit that share s ends, if others began it; half the channels of its row block
+// x / 2.  The first part stands in its share's second slot, the others in their shares' first.
 __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillParams p) {
     const int share = blockIdx.y;
     const Joined at = joined(p)[share];
     const int parts = at.parts, first = share + 1 - parts;
     if (parts <= 1) return;
-    const int in_unit = kJoinRows * blockIdx.x + (threadIdx.x >> 5), channel = 4 * (threadIdx.x & 31);
-    const int w = in_unit >> 5, row = at.tile * p.tok + 32 * (w / p.hc) + (in_unit & 31);
-    if (row >= p.n_q) return;
-    const int g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc);
-    const int64_t r = static_cast<int64_t>(at.b * p.q_heads + g * p.group + hchunk * p.hc + w % p.hc) * p.n_q + row;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int w = blockIdx.x >> 1, piece = 8 * (blockIdx.x & 1) + 2 * wave;                // and the next: channels 8 piece + 4 half ..
+    const int row = at.tile * p.tok + 32 * (w / p.hc) + col;
     float m = -INFINITY, l = 0.0f;
-    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float4 y[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
     for (int i = 0; i < parts; i += kAhead) {
-        float4 z[kAhead];
+        float4 z[kAhead][2];
         float2 x[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int part = min(i + k, parts - 1);
             const int64_t slot = part == 0 ? 2 * first + 1 : 2 * (first + part);
-            x[k] = part_stat(p)[slot * kUnitRows + in_unit];
-            z[k] = *reinterpret_cast<const float4*>(p.part + slot * kPartFloats + in_unit * 128 + channel);
+            x[k] = part_stat(p)[slot * kUnitRows + 32 * w + col];
+            const float4* const from = reinterpret_cast<const float4*>(p.part + slot * kPartFloats) + 64 * (16 * w + piece) + lane;
+            z[k][0] = from[0];
+            z[k][1] = from[64];
         }
         float most = m;
 #pragma unroll
@@ -832,20 +827,29 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillPar
         const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - most);
         m = most;
         l *= f;
-        y = make_float4(y.x * f, y.y * f, y.z * f, y.w * f);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) y[j] = make_float4(y[j].x * f, y[j].y * f, y[j].z * f, y[j].w * f);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (x[k].x == -INFINITY) continue;
             const float h = __builtin_amdgcn_exp2f(x[k].x - m);
             l = fmaf(x[k].y, h, l);
-            y = make_float4(fmaf(z[k].x, h, y.x), fmaf(z[k].y, h, y.y), fmaf(z[k].z, h, y.z), fmaf(z[k].w, h, y.w));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) y[j] = make_float4(fmaf(z[k][j].x, h, y[j].x), fmaf(z[k][j].y, h, y[j].y), fmaf(z[k][j].z, h, y[j].z), fmaf(z[k][j].w, h, y[j].w));
         }
     }
+    if (row >= p.n_q) return;
+    const int g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc);
+    const int64_t r = static_cast<int64_t>(at.b * p.q_heads + g * p.group + hchunk * p.hc + w % p.hc) * p.n_q + row;
     const bool none = at.base + row < 0 || l == 0.0f;
     const float inv = none ? 0.0f : 1.0f / l;
-    if (none) y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    *reinterpret_cast<uint2*>(p.o + r * 128 + channel) = make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
-    if (p.lse && channel == 0) p.lse[r] = none ? -INFINITY : (m + (log2f(l) - kLift)) * 0.69314718055994530942f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        if (none) y[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        *reinterpret_cast<uint2*>(p.o + r * 128 + 8 * (piece + j) + 4 * half) =
+            make_uint2(pack_bf16(y[j].x * inv, y[j].y * inv), pack_bf16(y[j].z * inv, y[j].w * inv));
+    }
+    if (p.lse && piece == 0 && half == 0) p.lse[r] = none ? -INFINITY : (m + (log2f(l) - kLift)) * 0.69314718055994530942f;
 }
 
 bool sizes_ok(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) {
@@ -909,7 +913,7 @@ extern "C" int vs_cache_prefill(const void* q, const vs_cache_t* cache, int batc
     hipLaunchKernelGGL(prefill_kernel, dim3(p.shares), dim3(kThreads), sizeof(Lds), s, p);
     VS_LAUNCH_CHECK();
     if (p.shares > 1) {
-        hipLaunchKernelGGL(prefill_join_kernel, dim3(kUnitRows / kJoinRows, p.shares), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL(prefill_join_kernel, dim3(kUnitRows / 32 * 2, p.shares), dim3(kThreads), 0, s, p);
         VS_LAUNCH_CHECK();
     }
     return VS_OK;

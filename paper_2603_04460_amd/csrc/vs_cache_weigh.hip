@@ -1,11 +1,14 @@
 // The weight that every token of the 4-bit paged cache gets from the last tokens' queries, added to what it had:
 //   w_j = decay old_j + sum over the query heads of a KV head and over the rows r that see j of exp(scale q_r . K_j - lse_r)
-// K of a block of 64 tokens is turned into bf16 once and stays in a wavefront's registers (scales in the conversion, exact), query rows pass by in tiles
-// of 32: S = K Q^T, keys x rows, 32 x 32 x 16 matrix instructions.  A lane keeps the sums of its 32 keys over its rows, which meet across the
-// lanes once at the end: no key belongs to two wavefronts, no atomics, the same call gives the same bits.
+// K of a block of 64 tokens comes straight from memory into the registers of the matrix operands, is turned into bf16 by the conversions (scales among
+// it, exact) and stays there while the rows pass by: S = K Q^T, keys x rows.  A lane keeps the sums of its keys over its rows, which meet across the lanes
+// once at the end: no key belongs to two wavefronts, no atomics, the same call gives the same bits.
 // The exponent is scale s - lse near zero for every weight that counts, of terms that are not: what the products' factor c = scale log2(e) loses by its
 // rounding is put into lse's factor (c / scale), and what is left of lse's product goes to the row as a factor, which costs nothing since the sum is a
 // multiply-add.
+//   weigh_few_kernel   up to 16 rows of a KV head: 16 x 16 x 32 products, the rows in registers; bound by the memory (68 + 8 bytes a token)
+//   weigh_many_kernel  more: 32 x 32 x 16 products, four wavefronts of 64 keys share the rows, which come to LDS in tiles of 32
+//   weigh_add_kernel   few keys and many rows: workgroups share the rows, their sums meet here, in the order of the rows
 #include <float.h>
 
 #include "vs_cache.h"
@@ -13,9 +16,13 @@
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kWaves = 4;
+constexpr int kFewRows = 16;
+constexpr int kRing = 4;                                   // tiles of rows in LDS
+constexpr int kTileBytes = 32 * 256;
 
 struct WeighParams {
     CacheParams cache;
@@ -24,102 +31,320 @@ struct WeighParams {
     const float* old;              // or null: zeros
     float* weights;
     int64_t stride;
+    float* part;                   // [parts][units][padded] sums, or null: one workgroup has all rows of its keys
+    int64_t padded;
+    int parts;
     int n_q, rows;                 // query rows of a KV head: group * n_q
+    int runs, run_rows, tiles;     // rows are taken in `runs` runs (all of them, or a head each) of run_rows rows, `tiles` tiles each
+    int blocks;                    // of a wavefront
     int fresh;                     // last tokens that have no weight yet
     float c, ratio, ratio_low;     // scale log2(e); c / scale in two terms
     float decay;
 };
 
-// sum over the 32 lanes of a half
-__device__ __forceinline__ float half_sum(float x) {
-    auto dpp = [](float v, auto ctrl) __attribute__((always_inline)) {
-        return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, true));
-    };
-    x = dpp(x, std::integral_constant<int, 0xB1>{});
-    x = dpp(x, std::integral_constant<int, 0x4E>{});
-    x = dpp(x, std::integral_constant<int, 0x141>{});
-    x = dpp(x, std::integral_constant<int, 0x140>{});
-    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
-    const unsigned r0 = r[0], r1 = r[1];
-    return __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1);
-}
-
 __device__ __forceinline__ bf16x8 operand(uint4 x) { return __builtin_bit_cast(bf16x8, x); }
 
-__global__ __launch_bounds__(64 * kWaves) void weigh_kernel(WeighParams p) {
+// A row's weights are 2^(c s - high) factor; a row without a key (lse = -inf) has none.
+struct RowConst {
+    float high, factor;
+};
+
+__device__ __forceinline__ RowConst row_const(const WeighParams& p, float lse) {
+    RowConst x;
+    x.high = lse * p.ratio;
+    x.factor = fabsf(x.high) < INFINITY ? __builtin_amdgcn_exp2f(-fmaf(lse, p.ratio_low, fmaf(lse, p.ratio, -x.high))) : 1.0f;
+    if (lse == -INFINITY) x.high = INFINITY;
+    return x;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+
+// Sixteen values of each lane, summed over a row of 16 lanes: lane m gets the sum of value m.  Lanes that differ in a bit of their number exchange the
+// halves that the other one keeps.
+__device__ __forceinline__ float sum_to_lane(float (&v)[16], int lane) {
+    static_for<8>([&](auto i) __attribute__((always_inline)) {
+        const bool b = lane & 8;
+        const float keep = b ? v[i + 8] : v[i], send = b ? v[i] : v[i + 8];
+        v[i] = keep + dpp<0x140>(send);                    // lane 15 - m
+    });
+    static_for<4>([&](auto i) __attribute__((always_inline)) {
+        const bool b = lane & 4;
+        const float keep = b ? v[i + 4] : v[i], send = b ? v[i] : v[i + 4];
+        v[i] = keep + dpp<0x141>(send);                    // 7 - m
+    });
+    static_for<2>([&](auto i) __attribute__((always_inline)) {
+        const bool b = lane & 2;
+        const float keep = b ? v[i + 2] : v[i], send = b ? v[i] : v[i + 2];
+        v[i] = keep + dpp<0x1B>(send);                     // 3 - m
+    });
+    const bool b = lane & 1;
+    const float keep = b ? v[1] : v[0], send = b ? v[0] : v[1];
+    return keep + dpp<0xB1>(send);                         // m ^ 1
+}
+
+__global__ __launch_bounds__(64 * kWaves) void weigh_few_kernel(WeighParams p) {
     const int unit = blockIdx.y, b = unit / p.cache.kv_heads, h = unit - b * p.cache.kv_heads;
-    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-    const int block = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int len = cache_length_scalar(p.cache, b), first = block * kBlock;
-    if (first >= len) return;
-    const uint8_t* const from = cache_block(p.cache, b, h, block);
-    float sum[2][16];
+    const int lane = threadIdx.x & 63, col = lane & 15, c = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int len = cache_length_scalar(p.cache, b), end = (len + kBlock - 1) / kBlock;
+    int block = blockIdx.x * kWaves * p.blocks + wave;
+    const int last = min(block + kWaves * (p.blocks - 1), end - 1);
+    if (block > last) return;
+    struct Held {
+        uint4 k[4];
+        uint32_t scale;
+        float old;
+        bool paged;
+    };
+    // after the turning round a lane has one key
+    const int key = 16 * (col >> 2) + 4 * c + (col & 3);
+    auto load = [&](Held& x, int block) __attribute__((always_inline)) {
+        const uint8_t* from = cache_block(p.cache, b, h, block);
+        x.paged = from != nullptr;
+        if (!from) from = p.cache.data;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 4; ++t) x.k[t] = *reinterpret_cast<const uint4*>(from + 1024 * t + 64 * col + 16 * c);
+        x.scale = *reinterpret_cast<const uint32_t*>(from + kKScales + 4 * lane);
+        const int j = block * kBlock + key;
+        x.old = p.old && p.decay != 0.0f && j < len - p.fresh ? p.old[unit * p.stride + j] : 0.0f;
+    };
+    Held x;
+    load(x, block);
+    const int row = min(col, p.rows - 1);
+    const int64_t r = static_cast<int64_t>(unit) * p.rows + row;
+    bf16x8 q[4];                                           // channels 32 c + 8 j ..
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sum[t][e] = 0.0f;
-    if (from) {
-        bf16x8 k[2][8];                                    // channels 64 half + 8 j .. of token 32 t + col
+    for (int j = 0; j < 4; ++j) q[j] = operand(*reinterpret_cast<const uint4*>(p.q + r * 128 + 32 * c + 8 * j));
+    RowConst row_of = row_const(p, p.lse[r]);
+    const int limit = col < p.rows ? len - p.n_q + row % p.n_q : -1;       // last key that the row sees
+    for (;; block += kWaves) {
+        Held next;
+        const bool more = block + kWaves <= last;
+        load(next, more ? block + kWaves : block);
+        f32x4 s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const uint32_t w = j == 0 ? x.k[t].x : j == 1 ? x.k[t].y : j == 2 ? x.k[t].z : x.k[t].w;
+                const float scale = __uint_as_float(t == 0 ? x.scale << 23 : t == 1 ? x.scale << 15 : t == 2 ? x.scale << 7 : x.scale >> 1);
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(dequantise8(w, scale)), q[j], s[t], 0, 0, 0);
+            }
+        float v[16];
+        const int before = limit - block * kBlock - 4 * c;                 // key 16 t + i of the lane's is seen up to here
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float y = fmaf(s[t][i], p.c, -row_of.high);
+                if (16 * t + i > before) y = -INFINITY;
+                v[4 * t + i] = __builtin_amdgcn_exp2f(y) * row_of.factor;
+            }
+        float mine = sum_to_lane(v, lane);
+        if (!x.paged) mine = 0.0f;
+        const int j = block * kBlock + key;
+        if (j < len) p.weights[unit * p.stride + j] = fmaf(x.old, p.decay, mine);
+        if (!more) return;
+        x = next;
+    }
+}
+
+// 16 or 4 bytes a lane straight to LDS, lane after lane from `to` on (the kernel itself waits for them)
+__device__ __forceinline__ void lds_load4(const void* from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(to), "v"(from) : "memory", "m0");
+}
+
+__device__ __forceinline__ void lds_load16(const void* from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
+}
+
+// Workgroup (x, unit, part): wavefronts take blocks 4 i + wave of the workgroup's p.blocks groups of four; part: a stretch of the tiles of rows.
+// A tile of rows is in LDS as it is in memory, but for its 16-byte chunks: chunk c of row r stands at c ^ (r % 16), so that 16 lanes that read a
+// chunk of 16 rows use all banks.  Where all of a part's tiles fit in LDS they are read once; otherwise each is asked for kRing - 1 tiles ahead.
+__global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams p) {
+    __shared__ __align__(16) uint8_t tile_of[kRing][kTileBytes];
+    __shared__ __align__(16) float lse_of[kRing][kWaves][64];
+    const int unit = blockIdx.y, b = unit / p.cache.kv_heads, h = unit - b * p.cache.kv_heads, part = blockIdx.z;
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int len = cache_length_scalar(p.cache, b), end = (len + kBlock - 1) / kBlock;
+    const int group0 = blockIdx.x * p.blocks, groups = min(p.blocks, (end + kWaves - 1) / kWaves - group0);
+    if (groups <= 0) return;
+    const int base = len - p.n_q;                          // position of row 0
+    const int all = p.runs * p.tiles, i0 = static_cast<int>(static_cast<int64_t>(all) * part / p.parts), i1 = static_cast<int>(static_cast<int64_t>(all) * (part + 1) / p.parts);
+    const bool resident = i1 - i0 <= kRing;
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)tile_of));
+    const uint32_t lds1 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)lse_of));
+
+    // Tiles that some row of which sees a key of the group: of a run those from `skip` on
+    struct Tile {
+        int run, at;
+    };
+    auto tile_number = [&](int i) { return Tile{i / p.tiles, i % p.tiles}; };
+    auto forward = [&](Tile& t, int skip) __attribute__((always_inline)) {
+        if (++t.at == p.tiles) {
+            ++t.run;
+            t.at = skip;
+        }
+    };
+    auto rows_of = [&](const Tile& t) __attribute__((always_inline)) { return static_cast<int64_t>(unit) * p.rows + t.run * p.run_rows; };
+    auto request = [&](const Tile& t, int slot) __attribute__((always_inline)) {
+        const int64_t r = rows_of(t);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int row = 8 * wave + 4 * k + (lane >> 4), chunk = (lane & 15) ^ (row & 15);
+            lds_load16(p.q + (r + min(32 * t.at + row, p.run_rows - 1)) * 128 + 8 * chunk, lds0 + slot * kTileBytes + 1024 * (2 * wave + k));
+        }
+        lds_load4(p.lse + r + min(32 * t.at + col, p.run_rows - 1), lds1 + 256 * (kWaves * slot + wave));
+    };
+
+    struct Held {
+        uint4 k[2][2];
+        uint32_t scale[2][2];
+        bool paged;
+    };
+    auto load = [&](Held& x, int block) __attribute__((always_inline)) {
+        const uint8_t* from = block < end ? cache_block(p.cache, b, h, block) : nullptr;
+        x.paged = from != nullptr;
+        if (!from) from = p.cache.data;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int token = 32 * t + col;
-            const uint4* const codes = reinterpret_cast<const uint4*>(from + 64 * token + 32 * half);
-            const uint4 x = codes[0], y = codes[1];
-            const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+            const uint4* const codes = reinterpret_cast<const uint4*>(from + 64 * (32 * t + col) + 32 * half);
+            x.k[t][0] = codes[0];
+            x.k[t][1] = codes[1];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const uint32_t e = from[kKScales + 4 * (16 * (2 * half + g) + (token & 15)) + (token >> 4)];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) k[t][4 * g + j] = operand(dequantise8(w[4 * g + j], __uint_as_float(e << 23)));
-            }
+            for (int g = 0; g < 2; ++g) x.scale[t][g] = from[kKScales + 4 * (16 * (2 * half + g) + (col & 15)) + 2 * t + (col >> 4)];
         }
-        const bool edge = first + kBlock - 1 > len - p.n_q;
-        for (int at = 0; at < p.rows; at += 32) {
-            const int row = min(at + col, p.rows - 1);
-            const int64_t r = static_cast<int64_t>(unit) * p.rows + row;
-            const uint16_t* const q = p.q + r * 128 + 64 * half;
-            f32x16 s[2];
+    };
+    uint32_t chunk_at[8];                                  // of channels 64 half + 8 j of row `col`
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+    for (int j = 0; j < 8; ++j) chunk_at[j] = 256 * col + 16 * ((8 * half + j) ^ (col & 15));
+
+    Held next;
+    load(next, group0 * kWaves + wave);
+    if (resident) {
+        Tile t = tile_number(i0);
+        for (int i = i0; i < i1; ++i) {
+            request(t, i - i0);
+            forward(t, 0);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    }
+    for (int group = group0; group < group0 + groups; ++group) {
+        const int block = group * kWaves + wave, first = block * kBlock;
+        const bool paged = next.paged;
+        bf16x8 k[2][8];                                    // channels 64 half + 8 j .. of token 32 t + col
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[t][e] = 0.0f;
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bf16x8 y = operand(*reinterpret_cast<const uint4*>(q + 8 * j));
-#pragma unroll
-                for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[t][j], y, s[t], 0, 0, 0);
+                const uint4& x = next.k[t][j >> 2];
+                k[t][j] = operand(dequantise8((j & 3) == 0 ? x.x : (j & 3) == 1 ? x.y : (j & 3) == 2 ? x.z : x.w, __uint_as_float(next.scale[t][j >> 2] << 23)));
             }
-            // 2^(c s - high) factor; a row without a key has no weights
-            const float lse = p.lse[r];
-            float high = lse * p.ratio, factor = 1.0f;
-            if (fabsf(high) < INFINITY) factor = __builtin_amdgcn_exp2f(-fmaf(lse, p.ratio_low, fmaf(lse, p.ratio, -high)));
-            if (lse == -INFINITY) high = INFINITY;
-            const int limit = at + col < p.rows ? len - p.n_q + row % p.n_q : -1;   // last key that the row sees
-            const bool masked = edge || at + 32 > p.rows;
+        load(next, group + 1 < group0 + groups ? block + kWaves : block);
+        float sum[2][16];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float x = fmaf(s[t][e], p.c, -high);
-                    if (masked && first + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3) > limit) x = -INFINITY;
-                    sum[t][e] = fmaf(__builtin_amdgcn_exp2f(x), factor, sum[t][e]);
-                }
+            for (int e = 0; e < 16; ++e) sum[t][e] = 0.0f;
+        const bool edge = first + kBlock - 1 > base;
+
+        auto take = [&](const Tile& t, int slot) __attribute__((always_inline)) {
+            const uint8_t* const tile = tile_of[slot];
+            const RowConst row_of = row_const(p, lse_of[slot][wave][lane]);
+            f32x16 s[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bf16x8 y = operand(*reinterpret_cast<const uint4*>(tile + chunk_at[j]));
+#pragma unroll
+                for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[u][j], y, s[u], 0, 0, 0);
+            }
+            if (edge || 32 * t.at + 32 > p.run_rows) {
+                const int in_run = 32 * t.at + col, row = p.runs == 1 ? in_run % p.n_q : in_run;
+                const int before = (in_run < p.run_rows ? base + row : -1) - first - 4 * half;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float x = fmaf(s[u][e], p.c, -row_of.high);
+                        if (32 * u + 8 * (e >> 2) + (e & 3) > before) x = -INFINITY;
+                        sum[u][e] = fmaf(__builtin_amdgcn_exp2f(x), row_of.factor, sum[u][e]);
+                    }
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        sum[u][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[u][e], p.c, -row_of.high)), row_of.factor, sum[u][e]);
+            }
+        };
+        if (resident) {
+            Tile t = tile_number(i0);
+            for (int i = i0; i < i1; ++i) {
+                take(t, i - i0);
+                forward(t, 0);
+            }
+        } else {
+            // rows in front of the group's first key see nothing of it
+            const int skip = p.runs == 1 ? 0 : min(max(group * kWaves * kBlock - base, 0) >> 5, p.tiles - 1);
+            Tile t = tile_number(i0);
+            t.at = max(t.at, skip);
+            auto here = [&](const Tile& x) __attribute__((always_inline)) { return x.run * p.tiles + x.at < i1; };
+            Tile ahead = t;
+            __syncthreads();                               // the group before this one is out of the ring
+#pragma unroll
+            for (int i = 0; i < kRing - 1; ++i) {
+                request(here(ahead) ? ahead : t, i);
+                if (here(ahead)) forward(ahead, skip);
+            }
+            for (int i = 0; here(t); ++i) {
+                asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+                __syncthreads();                           // tile i is there, tile i - 1 has been read
+                request(here(ahead) ? ahead : t, (i + kRing - 1) & (kRing - 1));
+                if (here(ahead)) forward(ahead, skip);
+                take(t, i & (kRing - 1));
+                forward(t, skip);
+            }
+        }
+        // key 32 u + 8 (e / 4) + 4 half + e % 4 to a lane: first over 16 lanes, then over the two rows of 16
+        float total[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const float x = sum_to_lane(sum[u], lane);
+            const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+            const unsigned r0 = r[0], r1 = r[1];
+            total[u] = __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1);
+        }
+        const int e = lane & 15, j = first + 32 * (col >> 4) + 8 * (e >> 2) + 4 * half + (e & 3);
+        const float mine = !paged ? 0.0f : col < 16 ? total[0] : total[1];
+        if (j < len) {
+            if (p.part) {
+                p.part[(static_cast<int64_t>(part) * gridDim.y + unit) * p.padded + j] = mine;
+            } else {
+                const int64_t at = unit * p.stride + j;
+                p.weights[at] = p.old && p.decay != 0.0f && j < len - p.fresh ? fmaf(p.old[at], p.decay, mine) : mine;
+            }
         }
     }
-    // key 32 t + 8 (e / 4) + 4 half + e % 4 to the lane with col = 16 t + e
-    float mine = 0.0f;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float x = half_sum(sum[t][e]);
-            if (col == 16 * t + e) mine = x;
-        }
-    const int e = col & 15, j = first + 32 * (col >> 4) + 8 * (e >> 2) + 4 * half + (e & 3);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (what was asked for beyond the last tile)
+}
+
+__global__ __launch_bounds__(256) void weigh_add_kernel(WeighParams p) {
+    const int unit = blockIdx.y, len = cache_length_scalar(p.cache, unit / p.cache.kv_heads), j = blockIdx.x * 256 + threadIdx.x;
     if (j >= len) return;
+    float sum = 0.0f;
+#pragma unroll 8
+    for (int part = 0; part < p.parts; ++part) sum += p.part[(static_cast<int64_t>(part) * gridDim.y + unit) * p.padded + j];
     const int64_t at = unit * p.stride + j;
-    if (p.old && p.decay != 0.0f && j < len - p.fresh) mine = fmaf(p.old[at], p.decay, mine);
-    p.weights[at] = mine;
+    p.weights[at] = p.old && p.decay != 0.0f && j < len - p.fresh ? fmaf(p.old[at], p.decay, sum) : sum;
 }
 
 bool sizes_ok(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) {
@@ -127,11 +352,48 @@ bool sizes_ok(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) 
            max_n <= VS_MAX_SEQ && batch <= 65535 && static_cast<int64_t>(batch) * kv_heads <= 65535 && q_heads / kv_heads * n_q <= INT32_MAX / 2;
 }
 
+// The form, and how workgroups share the work.
+void plan(WeighParams& p, int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) {
+    const int64_t units = static_cast<int64_t>(batch) * kv_heads, blocks = (max_n + kBlock - 1) / kBlock;
+    p.n_q = static_cast<int>(n_q);
+    p.rows = static_cast<int>(q_heads / kv_heads * n_q);
+    p.parts = 1;
+    p.padded = blocks * kBlock;
+    if (p.rows <= kFewRows) {
+        const int64_t each = units * blocks / 8192;        // a wavefront's, with eight on a SIMD
+        p.blocks = static_cast<int>(each < 1 ? 1 : each < 16 ? each : 16);
+        return;
+    }
+    // short runs would leave tiles half empty; long ones leave out what their first rows do not see
+    p.runs = n_q >= 256 ? static_cast<int>(q_heads / kv_heads) : 1;
+    p.run_rows = p.runs == 1 ? p.rows : p.n_q;
+    p.tiles = (p.run_rows + 31) / 32;
+    const int64_t groups = (blocks + kWaves - 1) / kWaves, all = static_cast<int64_t>(p.runs) * p.tiles;
+    int64_t parts = (2 * 256 + units * groups - 1) / (units * groups);       // two workgroups on every compute unit
+    if (parts > (all + 7) / 8) parts = (all + 7) / 8;      // of eight tiles at least
+    if (parts > 64) parts = 64;
+    p.parts = static_cast<int>(parts);
+    const int64_t each = all <= kRing ? units * groups / 1024 : 1;
+    p.blocks = static_cast<int>(each < 1 ? 1 : each < 16 ? each : 16);
+}
+
+size_t part_bytes(const WeighParams& p, int64_t units) { return p.parts > 1 ? static_cast<size_t>(p.parts * units * p.padded) * sizeof(float) : 0; }
+
 }  // namespace
 
 extern "C" size_t vs_cache_weigh_workspace(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) {
     if (!sizes_ok(batch, q_heads, kv_heads, n_q, max_n)) return 0;
-    return 0;
+    // (fewer keys are shared by more workgroups: the most that any length up to max_n takes)
+    size_t most = 0;
+    const int64_t units = static_cast<int64_t>(batch) * kv_heads;
+    for (int64_t n = kBlock * kWaves;; n += kBlock * kWaves) {
+        WeighParams p;
+        plan(p, batch, q_heads, kv_heads, n_q, n < max_n ? n : max_n);
+        const size_t x = part_bytes(p, units);
+        if (x > most) most = x;
+        if (n >= max_n || p.parts == 1) break;
+    }
+    return most;
 }
 
 extern "C" int vs_cache_weigh(const void* q, const float* lse, const vs_cache_t* cache, int batch, int q_heads, int64_t n_q, const int32_t* lens,
@@ -145,24 +407,35 @@ extern "C" int vs_cache_weigh(const void* q, const float* lse, const vs_cache_t*
     const int rc = vs::cache_params(cache, batch, lens, max_n, &p.cache);
     if (rc != VS_OK) return rc;
     if (!sizes_ok(batch, q_heads, cache->kv_heads, n_q, max_n)) return VS_ERR_UNSUPPORTED;
-    const size_t units = static_cast<size_t>(batch) * cache->kv_heads;
-    size_t bytes;
-    if (stride < max_n || __builtin_mul_overflow(units * 4, static_cast<size_t>(stride), &bytes)) return VS_ERR_INVALID_ARG;
-    if (ws_bytes < vs_cache_weigh_workspace(batch, q_heads, cache->kv_heads, n_q, max_n)) return VS_ERR_WORKSPACE;
+    const int64_t units = static_cast<int64_t>(batch) * cache->kv_heads;
+    int64_t bytes;
+    if (stride < max_n || __builtin_mul_overflow(units * 4, stride, &bytes)) return VS_ERR_INVALID_ARG;
+    plan(p, batch, q_heads, cache->kv_heads, n_q, max_n);
+    const size_t need = part_bytes(p, units);
+    if (need && (!ws || ws_bytes < need)) return VS_ERR_WORKSPACE;
     p.q = static_cast<const uint16_t*>(q);
     p.lse = lse;
     p.old = old;
     p.weights = weights;
     p.stride = stride;
-    p.n_q = static_cast<int>(n_q);
-    p.rows = static_cast<int>(q_heads / cache->kv_heads * n_q);
+    p.part = p.parts > 1 ? static_cast<float*>(ws) : nullptr;
     p.fresh = static_cast<int>(fresh < max_n ? fresh : max_n);
     const double ratio = static_cast<double>(p.c) / scale;
     p.ratio = static_cast<float>(ratio);
     p.ratio_low = static_cast<float>(ratio - p.ratio);
     p.decay = decay;
-    const unsigned blocks = static_cast<unsigned>((max_n + kBlock * kWaves - 1) / (kBlock * kWaves));
-    hipLaunchKernelGGL(weigh_kernel, dim3(blocks, static_cast<unsigned>(units)), dim3(64 * kWaves), 0, static_cast<hipStream_t>(stream), p);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const unsigned y = static_cast<unsigned>(units), x = static_cast<unsigned>((max_n + kBlock * kWaves * p.blocks - 1) / (kBlock * kWaves * p.blocks));
+    if (p.rows <= kFewRows) {
+        hipLaunchKernelGGL(weigh_few_kernel, dim3(x, y), dim3(64 * kWaves), 0, s, p);
+        VS_LAUNCH_CHECK();
+        return VS_OK;
+    }
+    hipLaunchKernelGGL(weigh_many_kernel, dim3(x, y, p.parts), dim3(64 * kWaves), 0, s, p);
     VS_LAUNCH_CHECK();
+    if (p.part) {
+        hipLaunchKernelGGL(weigh_add_kernel, dim3(static_cast<unsigned>((max_n + 255) / 256), y), dim3(256), 0, s, p);
+        VS_LAUNCH_CHECK();
+    }
     return VS_OK;
 }
