@@ -21,7 +21,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kWaves = 4;
 constexpr int kFewRows = 16;
-constexpr int kRing = 4;                                   // tiles of rows in LDS
+constexpr int kRing = 8;                                   // tiles of rows in LDS
+constexpr int kAhead = 4;                                  // tiles that are asked for in advance
 constexpr int kTileBytes = 32 * 256;
 
 struct WeighParams {
@@ -164,7 +165,10 @@ __device__ __forceinline__ void lds_load16(const void* from, uint32_t to) {
 
 // Workgroup (x, unit, part): wavefronts take blocks 4 i + wave of the workgroup's p.blocks groups of four; part: a stretch of the tiles of rows.
 // A tile of rows is in LDS as it is in memory, but for its 16-byte chunks: chunk c of row r stands at c ^ (r % 16), so that 16 lanes that read a
-// chunk of 16 rows use all banks.  Where all of a part's tiles fit in LDS they are read once; otherwise each is asked for kRing - 1 tiles ahead.
+// chunk of 16 rows use all banks.  Where all of a part's tiles fit in LDS they are read once; otherwise each is asked for kAhead tiles ahead.
+// The two halves of a group's keys run half a step apart: between the products of one stand the exponentials of the other.  Operands of the next
+// tile are read behind the last products of this one's.
+template <bool RESIDENT>
 __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams p) {
     __shared__ __align__(16) uint8_t tile_of[kRing][kTileBytes];
     __shared__ __align__(16) float lse_of[kRing][kWaves][64];
@@ -175,7 +179,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
     if (groups <= 0) return;
     const int base = len - p.n_q;                          // position of row 0
     const int all = p.runs * p.tiles, i0 = static_cast<int>(static_cast<int64_t>(all) * part / p.parts), i1 = static_cast<int>(static_cast<int64_t>(all) * (part + 1) / p.parts);
-    const bool resident = i1 - i0 <= kRing;
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)tile_of));
     const uint32_t lds1 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)lse_of));
 
@@ -201,9 +204,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
         lds_load4(p.lse + r + min(32 * t.at + col, p.run_rows - 1), lds1 + 256 * (kWaves * slot + wave));
     };
 
+    struct Step {
+        Tile tile;
+        int slot, next;
+    };
     struct Held {
         uint4 k[2][2];
-        uint32_t scale[2][2];
+        uint32_t scale[2];                                 // of groups 2 half, 2 half + 1: words of tokens 16 t + col % 16
         bool paged;
     };
     auto load = [&](Held& x, int block) __attribute__((always_inline)) {
@@ -215,17 +222,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
             const uint4* const codes = reinterpret_cast<const uint4*>(from + 64 * (32 * t + col) + 32 * half);
             x.k[t][0] = codes[0];
             x.k[t][1] = codes[1];
-#pragma unroll
-            for (int g = 0; g < 2; ++g) x.scale[t][g] = from[kKScales + 4 * (16 * (2 * half + g) + (col & 15)) + 2 * t + (col >> 4)];
         }
-    };
-    uint32_t chunk_at[8];                                  // of channels 64 half + 8 j of row `col`
 #pragma unroll
-    for (int j = 0; j < 8; ++j) chunk_at[j] = 256 * col + 16 * ((8 * half + j) ^ (col & 15));
+        for (int g = 0; g < 2; ++g) x.scale[g] = *reinterpret_cast<const uint32_t*>(from + kKScales + 4 * (16 * (2 * half + g) + (col & 15)));
+    };
+    const uint32_t chunk_at = 256 * col + 16 * ((8 * half) ^ (col & 15));                 // of channels 64 half of row `col`; 8 j further on: ^ 16 j
 
+    bf16x8 y[8];                                           // channels 64 half + 8 j .. of row `col` of a tile
     Held next;
-    load(next, group0 * kWaves + wave);
-    if (resident) {
+    if constexpr (RESIDENT) {
+        load(next, group0 * kWaves + wave);
         Tile t = tile_number(i0);
         for (int i = i0; i < i1; ++i) {
             request(t, i - i0);
@@ -236,6 +242,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
     }
     for (int group = group0; group < group0 + groups; ++group) {
         const int block = group * kWaves + wave, first = block * kBlock;
+        if constexpr (!RESIDENT) load(next, block);
         const bool paged = next.paged;
         bf16x8 k[2][8];                                    // channels 64 half + 8 j .. of token 32 t + col
 #pragma unroll
@@ -243,9 +250,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint4& x = next.k[t][j >> 2];
-                k[t][j] = operand(dequantise8((j & 3) == 0 ? x.x : (j & 3) == 1 ? x.y : (j & 3) == 2 ? x.z : x.w, __uint_as_float(next.scale[t][j >> 2] << 23)));
+                k[t][j] = operand(dequantise8((j & 3) == 0 ? x.x : (j & 3) == 1 ? x.y : (j & 3) == 2 ? x.z : x.w, __uint_as_float((next.scale[j >> 2] >> (8 * (2 * t + (col >> 4)))) << 23)));
             }
-        load(next, group + 1 < group0 + groups ? block + kWaves : block);
+        if constexpr (RESIDENT) load(next, group + 1 < group0 + groups ? block + kWaves : block);
         float sum[2][16];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -253,66 +260,107 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
             for (int e = 0; e < 16; ++e) sum[t][e] = 0.0f;
         const bool edge = first + kBlock - 1 > base;
 
-        auto take = [&](const Tile& t, int slot) __attribute__((always_inline)) {
-            const uint8_t* const tile = tile_of[slot];
-            const RowConst row_of = row_const(p, lse_of[slot][wave][lane]);
-            f32x16 s[2];
+        f32x16 s[2];                                       // scores of the group's first and second 32 keys
+        float high = 0.0f, used = 0.0f, factor = 0.0f, by = 0.0f;          // of the tile that is weighed: weights 2^(by s - used) factor
+        auto read = [&](int slot, int j) __attribute__((always_inline)) {
+            y[j] = operand(*reinterpret_cast<const uint4*>(tile_of[slot] + (chunk_at ^ (16 * j))));
+        };
+        auto weigh = [&](int u, int j) __attribute__((always_inline)) {    // elements 2 j and 2 j + 1
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bf16x8 y = operand(*reinterpret_cast<const uint4*>(tile + chunk_at[j]));
-#pragma unroll
-                for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[u][j], y, s[u], 0, 0, 0);
-            }
-            if (edge || 32 * t.at + 32 > p.run_rows) {
-                const int in_run = 32 * t.at + col, row = p.runs == 1 ? in_run % p.n_q : in_run;
-                const int before = (in_run < p.run_rows ? base + row : -1) - first - 4 * half;
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float x = fmaf(s[u][e], p.c, -row_of.high);
-                        if (32 * u + 8 * (e >> 2) + (e & 3) > before) x = -INFINITY;
-                        sum[u][e] = fmaf(__builtin_amdgcn_exp2f(x), row_of.factor, sum[u][e]);
-                    }
-            } else {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        sum[u][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[u][e], p.c, -row_of.high)), row_of.factor, sum[u][e]);
+            for (int e = 2 * j; e < 2 * j + 2; ++e) {
+                sum[u][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[u][e], by, -used)), factor, sum[u][e]);
+                asm volatile("" : "+v"(sum[u][e]));        // (at this place)
             }
         };
-        if (resident) {
-            Tile t = tile_number(i0);
-            for (int i = i0; i < i1; ++i) {
-                take(t, i - i0);
-                forward(t, 0);
+        // Products of the tile at `slot` with keys 32 u ..; OTHER: weights of the other 32 keys (of this tile for u = 1, of the one in front for u = 0)
+        auto products = [&](auto half_of, auto other, int next_slot) __attribute__((always_inline)) {
+            constexpr int U = decltype(half_of)::value;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j == 0) {
+                    f32x16 zero;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) zero[e] = 0.0f;
+                    s[U] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[U][0], y[0], zero, 0, 0, 0);
+                } else {
+                    s[U] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[U][j], y[j], s[U], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (U == 1) read(next_slot, j);
+                if constexpr (decltype(other)::value) weigh(1 - U, j);
+                __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        // exponents as they are, where the row sees the key
+        auto mask = [&](int u, const Tile& t) __attribute__((always_inline)) {
+            const int in_run = 32 * t.at + col, row = p.runs == 1 ? in_run % p.n_q : in_run;
+            const int before = (in_run < p.run_rows ? base + row : -1) - first - 4 * half - 32 * u;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[u][e] = fmaf(s[u][e], p.c, -high);
+                if (8 * (e >> 2) + (e & 3) > before) s[u][e] = -INFINITY;
+            }
+        };
+        using Z = std::integral_constant<int, 0>;
+        using O = std::integral_constant<int, 1>;
+        auto step = [&](auto old, const Tile& t, int slot, int next_slot) __attribute__((always_inline)) {
+            const float lse = lse_of[slot][wave][lane];
+            const bool masked = edge || 32 * t.at + 32 > p.run_rows;
+            products(Z{}, old, 0);
+            const RowConst row = row_const(p, lse);
+            high = row.high;
+            factor = row.factor;
+            if (masked) mask(0, t);
+            by = masked ? 1.0f : p.c;
+            used = masked ? 0.0f : high;
+            products(O{}, std::true_type{}, next_slot);
+            if (masked) mask(1, t);
+        };
+        // tiles 0, 1, ..: begin(i) in front of the products of the i-th (its tile, its slot and the next one's), more: is there another one
+        auto run = [&](auto begin, auto more) __attribute__((always_inline)) {
+            Step x = begin(0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) read(x.slot, j);
+            step(std::false_type{}, x.tile, x.slot, x.next);
+            for (int i = 1; more(i); ++i) {
+                x = begin(i);
+                step(std::true_type{}, x.tile, x.slot, x.next);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) weigh(1, j);
+        };
+        if constexpr (RESIDENT) {
+            Tile t = tile_number(i0);
+            run([&](int i) __attribute__((always_inline)) {
+                if (i > 0) forward(t, 0);
+                return Step{t, i, i0 + i + 1 < i1 ? i + 1 : 0};
+            }, [&](int i) __attribute__((always_inline)) { return i0 + i < i1; });
         } else {
             // rows in front of the group's first key see nothing of it
             const int skip = p.runs == 1 ? 0 : min(max(group * kWaves * kBlock - base, 0) >> 5, p.tiles - 1);
             Tile t = tile_number(i0);
             t.at = max(t.at, skip);
             auto here = [&](const Tile& x) __attribute__((always_inline)) { return x.run * p.tiles + x.at < i1; };
-            Tile ahead = t;
+            Tile ahead = t, now = t;
             __syncthreads();                               // the group before this one is out of the ring
+            auto ask = [&](int i) __attribute__((always_inline)) {         // for the i-th tile (behind the last one: the first again)
+                request(here(ahead) ? ahead : t, i & (kRing - 1));
+                if (here(ahead)) forward(ahead, skip);
+            };
 #pragma unroll
-            for (int i = 0; i < kRing - 1; ++i) {
-                request(here(ahead) ? ahead : t, i);
-                if (here(ahead)) forward(ahead, skip);
-            }
-            for (int i = 0; here(t); ++i) {
-                asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
-                __syncthreads();                           // tile i is there, tile i - 1 has been read
-                request(here(ahead) ? ahead : t, (i + kRing - 1) & (kRing - 1));
-                if (here(ahead)) forward(ahead, skip);
-                take(t, i & (kRing - 1));
-                forward(t, skip);
-            }
+            for (int i = 0; i < kAhead; ++i) ask(i);
+            if (here(t))
+                run([&](int i) __attribute__((always_inline)) {
+                    if (i > 0) forward(now, skip);
+                    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * (kAhead - 2)) : "memory");
+                    __syncthreads();                       // tiles i and i + 1 are there, tile i - 1 has been read
+                    ask(i + kAhead);
+                    return Step{now, i & (kRing - 1), (i + 1) & (kRing - 1)};
+                }, [&](int) __attribute__((always_inline)) {
+                    Tile x = now;
+                    forward(x, skip);
+                    return here(x);
+                });
         }
         // key 32 u + 8 (e / 4) + 4 half + e % 4 to a lane: first over 16 lanes, then over the two rows of 16
         float total[2];
@@ -431,7 +479,7 @@ extern "C" int vs_cache_weigh(const void* q, const float* lse, const vs_cache_t*
         VS_LAUNCH_CHECK();
         return VS_OK;
     }
-    hipLaunchKernelGGL(weigh_many_kernel, dim3(x, y, p.parts), dim3(64 * kWaves), 0, s, p);
+    hipLaunchKernelGGL(p.runs * p.tiles <= kRing * p.parts ? weigh_many_kernel<true> : weigh_many_kernel<false>, dim3(x, y, p.parts), dim3(64 * kWaves), 0, s, p);
     VS_LAUNCH_CHECK();
     if (p.part) {
         hipLaunchKernelGGL(weigh_add_kernel, dim3(static_cast<unsigned>((max_n + 255) / 256), y), dim3(256), 0, s, p);
