@@ -154,13 +154,13 @@ __global__ __launch_bounds__(64 * kWaves) void weigh_few_kernel(WeighParams p) {
     }
 }
 
-// 16 or 4 bytes a lane straight to LDS, lane after lane from `to` on (the kernel itself waits for them)
-__device__ __forceinline__ void lds_load4(const void* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(to), "v"(from) : "memory", "m0");
+// 16 or 4 bytes a lane from base + at straight to LDS, lane after lane from `to` on (the kernel itself waits for them)
+__device__ __forceinline__ void lds_load16(uint32_t at, const void* base, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
 }
 
-__device__ __forceinline__ void lds_load16(const void* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
+__device__ __forceinline__ void lds_load4(uint32_t at, const void* base, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
 }
 
 // Workgroup (x, unit, part): wavefronts take blocks 4 i + wave of the workgroup's p.blocks groups of four; part: a stretch of the tiles of rows.
@@ -195,13 +195,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
     };
     auto rows_of = [&](const Tile& t) __attribute__((always_inline)) { return static_cast<int64_t>(unit) * p.rows + t.run * p.run_rows; };
     auto request = [&](const Tile& t, int slot) __attribute__((always_inline)) {
-        const int64_t r = rows_of(t);
+        const int64_t r = rows_of(t) + 32 * t.at;
+        const int most = p.run_rows - 1 - 32 * t.at;       // (the last tile's rows behind the last one: that one again, masked)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int row = 8 * wave + 4 * k + (lane >> 4), chunk = (lane & 15) ^ (row & 15);
-            lds_load16(p.q + (r + min(32 * t.at + row, p.run_rows - 1)) * 128 + 8 * chunk, lds0 + slot * kTileBytes + 1024 * (2 * wave + k));
+            lds_load16(static_cast<uint32_t>(256 * min(row, most) + 16 * chunk), p.q + r * 128, lds0 + slot * kTileBytes + 1024 * (2 * wave + k));
         }
-        lds_load4(p.lse + r + min(32 * t.at + col, p.run_rows - 1), lds1 + 256 * (kWaves * slot + wave));
+        lds_load4(static_cast<uint32_t>(4 * min(col, most)), p.lse + r, lds1 + 256 * (kWaves * slot + wave));
     };
 
     struct Step {
@@ -352,8 +353,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
             if (here(t))
                 run([&](int i) __attribute__((always_inline)) {
                     if (i > 0) forward(now, skip);
-                    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * (kAhead - 2)) : "memory");
-                    __syncthreads();                       // tiles i and i + 1 are there, tile i - 1 has been read
+                    // tiles i and i + 1 are there, tile i - 1 has been read
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(3 * (kAhead - 2)) : "memory");
                     ask(i + kAhead);
                     return Step{now, i & (kRing - 1), (i + 1) & (kRing - 1)};
                 }, [&](int) __attribute__((always_inline)) {
@@ -417,7 +418,9 @@ void plan(WeighParams& p, int batch, int q_heads, int kv_heads, int64_t n_q, int
     p.run_rows = p.runs == 1 ? p.rows : p.n_q;
     p.tiles = (p.run_rows + 31) / 32;
     const int64_t groups = (blocks + kWaves - 1) / kWaves, all = static_cast<int64_t>(p.runs) * p.tiles;
-    int64_t parts = (2 * 256 + units * groups - 1) / (units * groups);       // two workgroups on every compute unit
+    // Two workgroups run on a compute unit, the older one faster: with fewer than 16 for each the last ones run alone.  512 / 2048 / 4096 / 8192 workgroups, us:
+    // 1024 tokens of 32749 335 / 303 / 293 / 298, 128 of 32768 48.2 / 46.4 / 46.2 / -, 4096 of 4096 177 / 171 / 178 / 178.
+    int64_t parts = (4096 + units * groups - 1) / (units * groups);
     if (parts > (all + 7) / 8) parts = (all + 7) / 8;      // of eight tiles at least
     if (parts > 64) parts = 64;
     p.parts = static_cast<int>(parts);
