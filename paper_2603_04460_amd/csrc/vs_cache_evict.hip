@@ -1,7 +1,10 @@
 // Eviction from the 4-bit paged cache: of every sequence and KV head the first tokens, the last ones and those with the largest weights stay, in
 // their order, at the front of the same cache or of another one.
-//   select_kernel  a workgroup for each head: the smallest key that stays by four passes over the weights, 8 bits each (weights as unsigned numbers in
-//                  their order; first and last tokens above all, NaN below all), then the numbers of the tokens that stay, ascending
+// Weights become unsigned numbers in their order (first and last tokens above all, NaN below all); the smallest one that stays is found by three counts
+// of 11, 11 and 10 bits, and of those that equal it the first ones stay.
+//   select_kernel  up to 16384 tokens: a workgroup has a head, its keys in registers, the counts in LDS
+//   count_kernel, emit_kernel  more: workgroups share a head.  Each writes the counts of its tokens, the next kernel adds up those of the head; three
+//                  counts, then the numbers are written
 //   gather_kernel  a workgroup for each block of 64 tokens that stay: codes and scales of 64 tokens from wherever they are
 //   put_kernel     a cache that is made smaller in place: blocks go through the workspace, so that all are read before one is written
 // Moving a token moves codes, nothing is rounded again.
@@ -10,8 +13,13 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr uint32_t kAlways = 0xffffffffu, kNever = 0;      // keys of tokens that stay in any case, and that are not there
+constexpr int kBins = 2048, kRounds = 3;
+constexpr int kAlone = 16384;                              // tokens up to which one workgroup has a head
+constexpr int kCountThreads = 1024, kCountBlocks = 128, kMaxChunks = 32;   // workgroups that share a head: blocks of each at least, and their number
+
+__device__ __forceinline__ constexpr int shift_of(int round) { return round == 0 ? 21 : round == 1 ? 10 : 0; }
+__device__ __forceinline__ constexpr uint32_t digit_of(uint32_t key, int round) { return (key >> shift_of(round)) & (round == 2 ? 1023u : 2047u); }
 
 struct EvictParams {
     CacheParams from, to;
@@ -24,7 +32,11 @@ struct EvictParams {
     int32_t* index;                // [units][keep]
     float* weight_stage;           // [units][keep] or null: weights_out is written at once
     uint8_t* block_stage;          // [units][blocks][kBlockBytes] or null: `to` is written at once
+    int32_t* hist;                 // [kRounds][units][chunks][kBins] counts of the workgroups that share a head
+    int32_t* above;                // [2][units][chunks]: tokens of a workgroup that the first and second count already let stay
+    int2* state;                   // [2][units]: digits found so far, tokens still to be found
     int keep, n_sink, n_recent, blocks;
+    int chunks, chunk_blocks;      // workgroups that share a head, blocks of each
     bool same;                     // `to` is `from`
 };
 
@@ -40,103 +52,296 @@ __device__ __forceinline__ uint32_t key_at(const EvictParams& p, const float* we
     return j < p.n_sink || j >= n - p.n_recent ? kAlways : key_of(weights[j]);
 }
 
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictParams p) {
-    __shared__ int hist[kSelectWaves][256];
-    __shared__ int above[kSelectWaves], equal[kSelectWaves];
-    __shared__ int shared_need, shared_digit;
+__device__ __forceinline__ bool block_paged(const EvictParams& p, int b, int block) {
+    return cache_paged(p.from, cache_page(p.from, b, block / p.from.page_blocks));
+}
+
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);    // last of a row of 16 to the next row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);    // last of the lower half to the upper
+    return x;
+}
+
+// Counts in LDS: bin d at 64 (d % 32) + d / 32, so that a lane's 32 bins, read one after the other, are no two in one bank with its neighbours'.
+__device__ __forceinline__ int bin_at(uint32_t d) { return static_cast<int>(64 * (d & 31) + (d >> 5)); }
+
+struct Found {
+    int digit, need, total;        // digit that the `need`-th largest key has, how many with that digit stay, all keys
+};
+
+// By one wavefront: lane l has the bins 2047 - 32 l down to 2016 - 32 l.
+__device__ __forceinline__ Found find_digit(const int* hist, int need, int lane) {
+    int sum = 0;
+    const int mine = 63 - lane;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sum += hist[64 * i + mine];
+    const int upto = wave_scan(sum);
+    Found x;
+    x.total = __builtin_amdgcn_readlane(upto, 63);
+    const int l = __popcll(__ballot(upto < need));         // the lane that has it (need between 1 and the total)
+    const int before = __builtin_amdgcn_readlane(upto - sum, l & 63);
+    const int count = lane < 32 ? hist[64 * (31 - lane) + 63 - l] : 0;     // its bins, the largest first
+    const int within = wave_scan(count);
+    const int k = __popcll(__ballot(before + within < need));
+    x.digit = 2047 - 32 * l - k;
+    x.need = need - before - __builtin_amdgcn_readlane(within - count, k & 63);
+    return x;
+}
+
+// Numbers of a wavefront's tokens that stay, ascending.  at: place of the first of them; ties: tokens in front whose key is the smallest that stays.
+struct Emit {
+    int32_t *index, *kept;
+    uint32_t least;
+    int need, at, ties;
+    __device__ __forceinline__ void take(int j, uint32_t key, int lane) {
+        const uint64_t below = (1ull << lane) - 1, tied = __ballot(key == least);
+        const bool stays = key > least || (key == least && ties + __popcll(tied & below) < need);
+        const uint64_t staying = __ballot(stays);
+        if (stays) {
+            const int i = at + __popcll(staying & below);
+            index[i] = j;
+            if (kept) kept[i] = j;
+        }
+        at += __popcll(staying);
+        ties += __popcll(tied);
+    }
+};
+
+// A wavefront has the tokens from 64 R * its number on, R of each lane.
+template <int T, int R>
+__global__ __launch_bounds__(T) void select_kernel(EvictParams p) {
+    __shared__ int hist[kRounds][kBins];
+    __shared__ int more_of[T / 64], same_of[T / 64];
+    __shared__ Found found[kRounds];
     const int unit = blockIdx.x, b = unit / p.from.kv_heads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = cache_length_scalar(p.from, b);
     const float* const weights = p.weights + unit * p.stride;
-    // a wavefront's share: blocks [first, last)
-    const int blocks = (n + kBlock - 1) / kBlock, each = (blocks + kSelectWaves - 1) / kSelectWaves;
-    const int first = min(wave * each, blocks), last = min(first + each, blocks);
+    uint32_t key[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int block = wave * R + i;
+        key[i] = block * kBlock < n && block_paged(p, b, block) ? key_at(p, weights, block * kBlock + lane, n, true) : kNever;
+    }
+#pragma unroll
+    for (int round = 0; round < kRounds; ++round)
+        for (int i = threadIdx.x; i < kBins; i += T) hist[round][i] = 0;
+    __syncthreads();
+    uint32_t prefix = 0;
+    int need = p.keep, count = 0;
+#pragma unroll
+    for (int round = 0; round < kRounds; ++round) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (key[i] != kNever && (round == 0 || key[i] >> shift_of(round - 1) == prefix)) atomicAdd(&hist[round][bin_at(digit_of(key[i], round))], 1);
+        __syncthreads();
+        if (wave == 0) {
+            if (round == 0) {                              // no more than there are
+                int all = 0;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) all += hist[0][64 * i + lane];
+                need = min(need, __builtin_amdgcn_readlane(wave_scan(all), 63));
+            }
+            Found x = {0, 0, 0};
+            if (need > 0) x = find_digit(hist[round], need, lane);
+            if (round == 0) x.total = need;
+            if (lane == 0) found[round] = x;
+        }
+        __syncthreads();
+        const Found x = found[round];
+        if (round == 0) count = x.total;
+        prefix = prefix << (round == 2 ? 10 : 11) | static_cast<uint32_t>(round == 2 ? x.digit & 1023 : x.digit);
+        need = x.need;
+    }
+    int more = 0, same = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        more += __popcll(__ballot(key[i] > prefix));
+        same += __popcll(__ballot(key[i] == prefix));
+    }
+    if (lane == 0) {
+        more_of[wave] = more;
+        same_of[wave] = same;
+    }
+    __syncthreads();
+    Emit out;
+    out.index = p.index + static_cast<int64_t>(unit) * p.keep;
+    out.kept = p.kept ? p.kept + static_cast<int64_t>(unit) * p.keep : nullptr;
+    out.least = prefix;
+    out.need = need;
+    out.at = out.ties = 0;
+    for (int w = 0; w < wave; ++w) {
+        out.at += more_of[w];
+        out.ties += same_of[w];
+    }
+    out.at += min(out.ties, need);
+    if (count > 0)
+#pragma unroll
+        for (int i = 0; i < R; ++i) out.take((wave * R + i) * kBlock + lane, key[i], lane);
+    if (out.kept)
+        for (int i = count + threadIdx.x; i < p.keep; i += T) out.kept[i] = -1;
+    if (threadIdx.x == 0 && unit == b * p.from.kv_heads) p.count[b] = count;
+}
+
+// ---- workgroups that share a head ----
+__device__ __forceinline__ int32_t* chunk_hist(const EvictParams& p, int round, int unit, int chunk) {
+    return p.hist + ((static_cast<int64_t>(round) * gridDim.y + unit) * p.chunks + chunk) * kBins;
+}
+
+// The counts of a round of all of the head's workgroups into `hist`, those in front of this one into `before` (if it is wanted).
+__device__ __forceinline__ void add_up(const EvictParams& p, int round, int unit, int live, int* hist, int* before) {
+    for (int d = threadIdx.x; d < kBins; d += kCountThreads) {             // (the order of the bins is theirs)
+        int sum = 0, front = 0;
+        for (int c = 0; c < live; c += 8) {
+            int x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = chunk_hist(p, round, unit, min(c + k, live - 1))[d];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (c + k < static_cast<int>(blockIdx.x)) front += x[k];
+                if (c + k < live) sum += x[k];
+            }
+        }
+        hist[d] = sum;
+        if (before) before[d] = front;
+    }
+}
+
+// What round `round` is about: keys that begin with prefix, need of them stay.  By all threads of the workgroup; the first count's total is count.
+__device__ __forceinline__ void find_round(const EvictParams& p, int round, int unit, int live, int* hist, int* before, Found* found, uint32_t* prefix, int* need,
+                                           int* count) {
+    const int lane = threadIdx.x & 63;
+    add_up(p, round, unit, live, hist, before);
+    int2 last = make_int2(0, p.keep);
+    if (round > 0) last = p.state[(round - 1) * gridDim.y + unit];
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        int want = last.y;
+        if (round == 0) {
+            int all = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) all += hist[64 * i + lane];
+            want = min(want, __builtin_amdgcn_readlane(wave_scan(all), 63));
+        }
+        Found x = {0, 0, 0};
+        if (want > 0) x = find_digit(hist, want, lane);
+        if (round == 0) x.total = want;
+        if (lane == 0) *found = x;
+    }
+    __syncthreads();
+    *prefix = static_cast<uint32_t>(last.x) << (round == 2 ? 10 : 11) | static_cast<uint32_t>(round == 2 ? found->digit & 1023 : found->digit);
+    *need = found->need;
+    if (round == 0) *count = found->total;
+}
+
+// sum over the workgroup of the bins of `hist` above digit
+__device__ __forceinline__ int bins_above(const int* hist, int digit, int* scratch) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int sum = 0;
+    for (int at = threadIdx.x; at < kBins; at += kCountThreads)
+        if (32 * (at & 63) + (at >> 6) > digit) sum += hist[at];
+    sum = __builtin_amdgcn_readlane(wave_scan(sum), 63);
+    __syncthreads();
+    if (lane == 0) scratch[wave] = sum;
+    __syncthreads();
+    sum = 0;
+    for (int w = 0; w < kCountThreads / 64; ++w) sum += scratch[w];
+    return sum;
+}
+
+// Workgroup (chunk, unit): counts of its tokens in round ROUND; what the rounds before found is added up first.
+template <int ROUND>
+__global__ __launch_bounds__(kCountThreads) void count_kernel(EvictParams p) {
+    __shared__ int hist[kBins], scratch[kCountThreads / 64];
+    __shared__ Found found;
+    const int unit = blockIdx.y, b = unit / p.from.kv_heads;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = cache_length_scalar(p.from, b), blocks = (n + kBlock - 1) / kBlock, live = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
+    const int first = blockIdx.x * p.chunk_blocks, last = min(first + p.chunk_blocks, blocks);
+    if (first >= last) {
+        if (ROUND == 0 && blocks == 0 && blockIdx.x == 0 && threadIdx.x == 0 && unit == b * p.from.kv_heads) p.count[b] = 0;
+        return;
+    }
+    const float* const weights = p.weights + unit * p.stride;
+    uint32_t prefix = 0;
+    int need = p.keep, count = 0;
+    if constexpr (ROUND > 0) {
+        find_round(p, ROUND - 1, unit, live, hist, nullptr, &found, &prefix, &need, &count);
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            p.state[(ROUND - 1) * gridDim.y + unit] = make_int2(static_cast<int>(prefix), need);
+            if (ROUND == 1 && unit == b * p.from.kv_heads) p.count[b] = count;
+        }
+        for (int d = threadIdx.x; d < kBins; d += kCountThreads) hist[d] = chunk_hist(p, ROUND - 1, unit, blockIdx.x)[d];
+        __syncthreads();
+        const int above = bins_above(hist, found.digit, scratch);
+        if (threadIdx.x == 0) p.above[((ROUND - 1) * gridDim.y + unit) * p.chunks + blockIdx.x] = above;
+        __syncthreads();
+    }
+    for (int d = threadIdx.x; d < kBins; d += kCountThreads) hist[d] = 0;
+    __syncthreads();
+    for (int block = first + wave; block < last; block += kCountThreads / 64) {
+        if (!block_paged(p, b, block)) continue;
+        const uint32_t key = key_at(p, weights, block * kBlock + lane, n, true);
+        if (key != kNever && (ROUND == 0 || key >> shift_of(ROUND - 1) == prefix)) atomicAdd(&hist[bin_at(digit_of(key, ROUND))], 1);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < kBins; d += kCountThreads) chunk_hist(p, ROUND, unit, blockIdx.x)[d] = hist[d];
+}
+
+__global__ __launch_bounds__(kCountThreads) void emit_kernel(EvictParams p) {
+    __shared__ int hist[kBins], before[kBins], scratch[kCountThreads / 64], more_of[kCountThreads / 64], same_of[kCountThreads / 64];
+    __shared__ Found found;
+    const int unit = blockIdx.y, b = unit / p.from.kv_heads;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = cache_length_scalar(p.from, b), blocks = (n + kBlock - 1) / kBlock, live = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
+    const int first = blockIdx.x * p.chunk_blocks, last = min(first + p.chunk_blocks, blocks);
+    const int count = p.count[b];
+    int32_t* const kept = p.kept ? p.kept + static_cast<int64_t>(unit) * p.keep : nullptr;
+    if (kept && blockIdx.x == 0)
+        for (int i = count + threadIdx.x; i < p.keep; i += kCountThreads) kept[i] = -1;
+    if (first >= last || count == 0) return;
+    uint32_t prefix;
+    int need, unused;
+    find_round(p, 2, unit, live, hist, before, &found, &prefix, &need, &unused);
+    Emit out;
+    out.index = p.index + static_cast<int64_t>(unit) * p.keep;
+    out.kept = kept;
+    out.least = prefix;
+    out.need = need;
+    out.at = bins_above(before, found.digit, scratch);
+    out.ties = before[bin_at(found.digit)];
+    for (int c = 0; c < static_cast<int>(blockIdx.x); ++c)
+        for (int round = 0; round < 2; ++round) out.at += p.above[(round * gridDim.y + unit) * p.chunks + c];
+    // a wavefront's share of the workgroup's blocks
+    const float* const weights = p.weights + unit * p.stride;
+    const int each = (last - first + kCountThreads / 64 - 1) / (kCountThreads / 64), from = min(first + wave * each, last), to = min(from + each, last);
     auto for_keys = [&](auto f) __attribute__((always_inline)) {
-        for (int block = first; block < last; ++block) {
-            const bool paged = cache_paged(p.from, cache_page(p.from, b, block / p.from.page_blocks));
+        for (int block = from; block < to; ++block) {
+            const bool paged = block_paged(p, b, block);
             f(block * kBlock + lane, key_at(p, weights, block * kBlock + lane, n, paged));
         }
     };
-    // tokens that are there
-    int there = 0;
-    for_keys([&](int, uint32_t key) { there += __popcll(__ballot(key != kNever)); });
-    if (lane == 0) above[wave] = there;
-    __syncthreads();
-    int present = 0;
-#pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) present += above[w];
-    const int count = min(p.keep, present);
-    uint32_t prefix = 0;                                   // of the smallest key that stays
-    int need = count;                                      // tokens that stay among those with that prefix
-    for (int shift = 24; shift >= 0 && count > 0; shift -= 8) {
-        for (int i = lane; i < 256; i += 64) hist[wave][i] = 0;
-        __syncthreads();
-        for_keys([&](int, uint32_t key) {
-            if (key != kNever && (shift == 24 || key >> (shift + 8) == prefix)) atomicAdd(&hist[wave][(key >> shift) & 255], 1);
-        });
-        __syncthreads();
-        if (wave == 0) {                                   // four digits a lane, from the largest down
-            int sum[4], total = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sum[i] = 0;
-                for (int w = 0; w < kSelectWaves; ++w) sum[i] += hist[w][255 - 4 * lane - i];
-                total += sum[i];
-            }
-            int upto = total;
-            for (int d = 1; d < 64; d *= 2) {
-                const int x = __shfl_up(upto, d);
-                if (lane >= d) upto += x;
-            }
-            int before = upto - total;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (before < need && need <= before + sum[i]) {
-                    shared_digit = 255 - 4 * lane - i;
-                    shared_need = need - before;
-                }
-                before += sum[i];
-            }
-        }
-        __syncthreads();
-        prefix = prefix << 8 | static_cast<uint32_t>(shared_digit);
-        need = shared_need;
-    }
     int more = 0, same = 0;
     for_keys([&](int, uint32_t key) {
         more += __popcll(__ballot(key > prefix));
         same += __popcll(__ballot(key == prefix));
     });
-    __syncthreads();
     if (lane == 0) {
-        above[wave] = more;
-        equal[wave] = same;
+        more_of[wave] = more;
+        same_of[wave] = same;
     }
     __syncthreads();
-    int at = 0, ties = 0;                                  // larger ones, and equal ones, in front of this share
     for (int w = 0; w < wave; ++w) {
-        at += above[w];
-        ties += equal[w];
+        out.at += more_of[w];
+        out.ties += same_of[w];
     }
-    at += min(ties, need);
-    int32_t* const index = p.index + static_cast<int64_t>(unit) * p.keep;
-    int32_t* const kept = p.kept ? p.kept + static_cast<int64_t>(unit) * p.keep : nullptr;
-    if (count > 0)
-        for_keys([&](int j, uint32_t key) {
-            const uint64_t below = (1ull << lane) - 1, tied = __ballot(key == prefix);
-            const bool stays = key > prefix || (key == prefix && ties + __popcll(tied & below) < need);
-            const uint64_t staying = __ballot(stays);
-            if (stays) {
-                const int i = at + __popcll(staying & below);
-                index[i] = j;
-                if (kept) kept[i] = j;
-            }
-            at += __popcll(staying);
-            ties += __popcll(tied);
-        });
-    if (kept)
-        for (int i = count + threadIdx.x; i < p.keep; i += kSelectThreads) kept[i] = -1;
-    if (threadIdx.x == 0 && unit == b * p.from.kv_heads) p.count[b] = count;
+    out.at += min(out.ties, need);
+    for_keys([&](int j, uint32_t key) { out.take(j, key, lane); });
 }
 
 // block `block` of sequence b, head h; null where the page table names no page.  (cache_block for a block that differs from lane to lane)
@@ -153,9 +358,19 @@ __device__ __forceinline__ bool unmoved(const EvictParams& p, int unit, int bloc
     return p.same && p.index[static_cast<int64_t>(unit) * p.keep + last] == last;
 }
 
+// Blocks of which the codes of V and all scales go through LDS.  0 / 2 / 4 / 8 of them, us: 64 sequences of up to 1088 tokens to 1024, read back 140 / 126 / 132 / 134, 16 of
+// 4160 to 4096 135 / 117 / 122 / 127, 12 of up to 12001 to 2000 59.1 / 57.0 / 59.9 / 60.5, one of 131072 to 1024 69.6 / 72.9 / 73.2 / 70.4.
+constexpr int kSpan = 2;
+constexpr int kHeldBytes = kBlockBytes - kVCodes;
+
+// K's rows come from where they are.  Of V a word is eight tokens of a channel: a thread puts its four words (two channels, 16 tokens) together from 16 pieces
+// of 16 bytes, each with both channels of one token.  Where the tokens stand in no more than kSpan blocks, which is so while most of them stay, those
+// blocks' codes of V and scales are read once, into LDS.
 __global__ __launch_bounds__(kThreads) void gather_kernel(EvictParams p) {
+    __shared__ __align__(16) uint8_t held[kSpan][kHeldBytes];
     __shared__ const uint8_t* from[kBlock];
     __shared__ int place[kBlock];
+    __shared__ const uint8_t* source[kSpan];
     const int unit = blockIdx.y, b = unit / p.from.kv_heads, h = unit - b * p.from.kv_heads, block = blockIdx.x;
     const int count = p.count[b];
     if (!p.block_stage && !p.weight_stage && block == 0 && h == 0 && threadIdx.x == 0) p.lens_out[b] = count;
@@ -163,12 +378,15 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictParams p) {
     const int64_t head = static_cast<int64_t>(unit) * p.keep;
     uint8_t* const there = cache_block(p.to, b, h, block);
     uint8_t* const to = p.block_stage ? p.block_stage + (static_cast<int64_t>(unit) * p.blocks + block) * kBlockBytes : there;
+    const int tokens = min(count - block * kBlock, kBlock);
+    const int j0 = p.index[head + block * kBlock] / kBlock, j1 = p.index[head + block * kBlock + tokens - 1] / kBlock;     // blocks of the first and the last
+    const bool near = tokens == kBlock && j1 - j0 < kSpan;
     if (threadIdx.x < kBlock) {
         const int i = block * kBlock + threadIdx.x;
-        if (i < count) {
+        if (threadIdx.x < tokens) {
             const int j = p.index[head + i];
             from[threadIdx.x] = block_of_lane(p.from, b, h, j / kBlock);
-            place[threadIdx.x] = j % kBlock;
+            place[threadIdx.x] = (j / kBlock - j0) * kBlock + j % kBlock;
             if (p.weights_out) {
                 const float w = p.weights[unit * p.stride + j];
                 if (p.weight_stage) p.weight_stage[head + i] = w;
@@ -178,43 +396,58 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictParams p) {
             from[threadIdx.x] = there;
             place[threadIdx.x] = threadIdx.x;
         }
+    } else if (threadIdx.x < kBlock + kSpan) {
+        const int k = threadIdx.x - kBlock;
+        source[k] = near && j0 + k <= j1 ? block_of_lane(p.from, b, h, j0 + k) : nullptr;
     }
     __syncthreads();
     if (!there || unmoved(p, unit, block, count)) return;
-    {
-        const int token = threadIdx.x >> 2, quarter = threadIdx.x & 3;
-        const uint4 x = *reinterpret_cast<const uint4*>(from[token] + 64 * place[token] + 16 * quarter);
-        // words (channel, u) of tokens 32 u + 4 c + 0 .. 3 and 16 more: two channels, u = 0, 1
-        const int c = (threadIdx.x >> 4) & 3, channel = 32 * (threadIdx.x >> 6) + (threadIdx.x & 15);
-        uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = 32 * u + (e < 4 ? 0 : 16) + 4 * c + (e & 3), j = place[i];
-                const uint8_t* const at = from[i];
+    const int token = threadIdx.x >> 2, quarter = threadIdx.x & 3;
+    const uint4 x = *reinterpret_cast<const uint4*>(from[token] + 64 * (place[token] & 63) + 16 * quarter);
+    // words (channel, u) of tokens 32 u + 4 c + 0 .. 3 and 16 more: channels 32 p + m and 16 more, u = 0, 1
+    const int c = (threadIdx.x >> 4) & 3, piece = 1024 * (threadIdx.x >> 6) + 16 * (threadIdx.x & 15);
+    const int scale_lane = threadIdx.x & 63;
+    const bool is_k = threadIdx.x < 64;                    // scales: threads 0 .. 63 of K (group g, tokens 16 k + m), 64 .. 127 of V (tokens 16 t + 4 c + k of group g)
+    uint32_t w[4] = {0, 0, 0, 0}, scales = 0;
+    auto put_together = [&](auto v_piece, auto byte) __attribute__((always_inline)) {
+        static_for<2>([&](auto u) __attribute__((always_inline)) {         // eight tokens at once
+            uint4 y[8];
+            static_for<8>([&](auto e) __attribute__((always_inline)) {
+                const int i = 32 * u + 16 * (e >> 2) + 4 * c + (e & 3);
+                y[e] = v_piece(i, piece + 256 * ((place[i] >> 2) & 3));
+            });
+            static_for<8>([&](auto e) __attribute__((always_inline)) {
+                const int j = place[32 * u + 16 * (e >> 2) + 4 * c + (e & 3)];
                 const int shift = 4 * ((j & 3) + ((j >> 4) & 1) * 4);
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    w[2 * half + u] |= ((*reinterpret_cast<const uint32_t*>(at + v_word(channel + 16 * half, (j >> 2) & 3, j >> 5)) >> shift) & 15u) << (4 * e);
-            }
-        uint32_t scales = 0;
+                const uint32_t low = j & 32 ? y[e].y : y[e].x, high = j & 32 ? y[e].w : y[e].z;
+                w[u] |= ((low >> shift) & 15u) << (4 * e);
+                w[2 + u] |= ((high >> shift) & 15u) << (4 * e);
+            });
+        });
         if (threadIdx.x < 128) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                // K: group g, tokens 16 k + m;  V: tokens 16 t + 4 c + k of group g
-                const int x = threadIdx.x & 63;
-                const bool is_k = threadIdx.x < 64;
-                const int i = is_k ? 16 * k + (x & 15) : 16 * (x & 3) + 4 * (x >> 4) + k, g = is_k ? x >> 4 : (x >> 2) & 3, j = place[i];
+                const int i = is_k ? 16 * k + (scale_lane & 15) : 16 * (scale_lane & 3) + 4 * (scale_lane >> 4) + k, g = is_k ? scale_lane >> 4 : (scale_lane >> 2) & 3, j = place[i] & 63;
                 const int at = is_k ? kKScales + 4 * (16 * g + (j & 15)) + (j >> 4) : kVScales + 16 * (4 * ((j >> 2) & 3) + g) + 4 * (j >> 4) + (j & 3);
-                scales |= static_cast<uint32_t>(from[i][at]) << (8 * k);
+                scales |= static_cast<uint32_t>(byte(i, at)) << (8 * k);
             }
         }
-        __syncthreads();                                   // (`to` may be where some of it was read)
-        reinterpret_cast<uint4*>(to)[threadIdx.x] = x;
-        reinterpret_cast<uint4*>(to + kVCodes)[threadIdx.x] = make_uint4(w[0], w[1], w[2], w[3]);
-        if (threadIdx.x < 128) reinterpret_cast<uint32_t*>(to + kKScales)[threadIdx.x] = scales;
+    };
+    if (near) {
+        for (int i = threadIdx.x; i < (j1 - j0 + 1) * (kHeldBytes / 16); i += kThreads) {
+            const int k = i / (kHeldBytes / 16), at = 16 * (i - k * (kHeldBytes / 16));
+            if (source[k]) *reinterpret_cast<uint4*>(held[k] + at) = *reinterpret_cast<const uint4*>(source[k] + kVCodes + at);
+        }
+        __syncthreads();
+        put_together([&](int i, int at) { return *reinterpret_cast<const uint4*>(held[place[i] >> 6] + at); },
+                     [&](int i, int at) { return held[place[i] >> 6][at - kVCodes]; });
+    } else {
+        put_together([&](int i, int at) { return *reinterpret_cast<const uint4*>(from[i] + kVCodes + at); }, [&](int i, int at) { return from[i][at]; });
     }
+    __syncthreads();                                       // (`to` may be where some of it was read)
+    reinterpret_cast<uint4*>(to)[threadIdx.x] = x;
+    reinterpret_cast<uint4*>(to + kVCodes)[threadIdx.x] = make_uint4(w[0], w[1], w[2], w[3]);
+    if (threadIdx.x < 128) reinterpret_cast<uint32_t*>(to + kKScales)[threadIdx.x] = scales;
 }
 
 __global__ __launch_bounds__(kThreads) void put_kernel(EvictParams p) {
@@ -236,16 +469,24 @@ bool sizes_ok(int batch, int kv_heads, int64_t max_n, int64_t keep) {
 }
 
 struct Parts {                                             // of the workspace: bytes in front of each
-    size_t index, weights, blocks, all;
+    size_t index, weights, blocks, above, state, hist, all;
+    int chunks, chunk_blocks;
 };
 
-Parts parts(int batch, int kv_heads, int64_t keep) {
+Parts parts(int batch, int kv_heads, int64_t max_n, int64_t keep) {
     const size_t units = static_cast<size_t>(batch) * kv_heads, k = static_cast<size_t>(keep);
     Parts x;
+    const int64_t all = (max_n + kBlock - 1) / kBlock;
+    x.chunk_blocks = static_cast<int>(all > kMaxChunks * kCountBlocks ? (all + kMaxChunks - 1) / kMaxChunks : kCountBlocks);
+    x.chunks = max_n <= kAlone ? 0 : static_cast<int>((all + x.chunk_blocks - 1) / x.chunk_blocks);
     x.index = vs::round_up(static_cast<size_t>(batch) * 4, 256);
     x.weights = x.index + vs::round_up(units * k * 4, 256);
     x.blocks = x.weights + vs::round_up(units * k * 4, 256);
-    x.all = x.blocks + units * ((k + kBlock - 1) / kBlock) * kBlockBytes;
+    x.above = x.blocks + units * ((k + kBlock - 1) / kBlock) * kBlockBytes;
+    x.state = x.above + vs::round_up(2 * units * kMaxChunks * 4, 256);
+    x.hist = x.state + vs::round_up(2 * units * 8, 256);
+    // (as many chunks as any length up to max_n has)
+    x.all = x.hist + (x.chunks ? kRounds * units * static_cast<size_t>(all < kMaxChunks * kCountBlocks ? x.chunks : kMaxChunks) * kBins * 4 : 0);
     return x;
 }
 
@@ -258,7 +499,7 @@ bool meet(const void* a, size_t n, const void* b, size_t m) {
 }  // namespace
 
 extern "C" size_t vs_cache_evict_workspace(int batch, int kv_heads, int64_t max_n, int64_t keep) {
-    return sizes_ok(batch, kv_heads, max_n, keep) ? parts(batch, kv_heads, keep).all : 0;
+    return sizes_ok(batch, kv_heads, max_n, keep) ? parts(batch, kv_heads, max_n, keep).all : 0;
 }
 
 extern "C" int vs_cache_evict(const vs_cache_t* cache, const float* weights, int64_t stride, int batch, const int32_t* lens, int64_t max_n,
@@ -277,7 +518,7 @@ extern "C" int vs_cache_evict(const vs_cache_t* cache, const float* weights, int
     size_t in, out;                                        // bytes of the weights: in 64 bits, or they are no array
     if (__builtin_mul_overflow(units * 4, static_cast<size_t>(stride), &in) ||
         (weights_out && __builtin_mul_overflow(units * 4, static_cast<size_t>(stride_out), &out))) return VS_ERR_INVALID_ARG;
-    const Parts x = parts(batch, p.from.kv_heads, keep);
+    const Parts x = parts(batch, p.from.kv_heads, max_n, keep);
     if (!ws || ws_bytes < x.all) return VS_ERR_WORKSPACE;
     uint8_t* const base = static_cast<uint8_t*>(ws);
     p.weights = weights;
@@ -288,6 +529,11 @@ extern "C" int vs_cache_evict(const vs_cache_t* cache, const float* weights, int
     p.lens_out = lens_out;
     p.count = reinterpret_cast<int32_t*>(base);
     p.index = reinterpret_cast<int32_t*>(base + x.index);
+    p.above = reinterpret_cast<int32_t*>(base + x.above);
+    p.state = reinterpret_cast<int2*>(base + x.state);
+    p.hist = reinterpret_cast<int32_t*>(base + x.hist);
+    p.chunks = x.chunks;
+    p.chunk_blocks = x.chunk_blocks;
     p.keep = static_cast<int>(keep);
     p.n_sink = static_cast<int>(n_sink);
     p.n_recent = static_cast<int>(n_recent);
@@ -298,7 +544,25 @@ extern "C" int vs_cache_evict(const vs_cache_t* cache, const float* weights, int
     p.block_stage = one_memory ? base + x.blocks : nullptr;
     p.weight_stage = weights_out && meet(weights, in, weights_out, out) ? reinterpret_cast<float*>(base + x.weights) : nullptr;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(select_kernel, dim3(static_cast<unsigned>(units)), dim3(kSelectThreads), 0, s, p);
+    const unsigned y = static_cast<unsigned>(units);
+    if (x.chunks) {
+        const dim3 grid(x.chunks, y);
+        hipLaunchKernelGGL(count_kernel<0>, grid, dim3(kCountThreads), 0, s, p);
+        VS_LAUNCH_CHECK();
+        hipLaunchKernelGGL(count_kernel<1>, grid, dim3(kCountThreads), 0, s, p);
+        VS_LAUNCH_CHECK();
+        hipLaunchKernelGGL(count_kernel<2>, grid, dim3(kCountThreads), 0, s, p);
+        VS_LAUNCH_CHECK();
+        hipLaunchKernelGGL(emit_kernel, grid, dim3(kCountThreads), 0, s, p);
+    } else if (max_n <= 2048) {
+        hipLaunchKernelGGL((select_kernel<256, 8>), dim3(y), dim3(256), 0, s, p);
+    } else if (max_n <= 4096) {
+        hipLaunchKernelGGL((select_kernel<512, 8>), dim3(y), dim3(512), 0, s, p);
+    } else if (max_n <= 8192) {
+        hipLaunchKernelGGL((select_kernel<1024, 8>), dim3(y), dim3(1024), 0, s, p);
+    } else {
+        hipLaunchKernelGGL((select_kernel<1024, 16>), dim3(y), dim3(1024), 0, s, p);
+    }
     VS_LAUNCH_CHECK();
     hipLaunchKernelGGL(gather_kernel, dim3(p.blocks, static_cast<unsigned>(units)), dim3(kThreads), 0, s, p);
     VS_LAUNCH_CHECK();
