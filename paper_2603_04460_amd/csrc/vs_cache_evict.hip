@@ -2,7 +2,7 @@
 // their order, at the front of the same cache or of another one.
 // Weights become unsigned numbers in their order (first and last tokens above all, NaN below all); the smallest one that stays is found by three counts
 // of 11, 11 and 10 bits, and of those that equal it the first ones stay.
-//   select_kernel  up to 16384 tokens: a workgroup has a head, its keys in registers, the counts in LDS
+//   select_kernel  up to 32768 tokens: a workgroup has a head, its keys in registers, the counts in LDS
 //   count_kernel, emit_kernel  more: workgroups share a head.  Each writes the counts of its tokens, the next kernel adds up those of the head; three
 //                  counts, then the numbers are written
 //   gather_kernel  a workgroup for each block of 64 tokens that stay: codes and scales of 64 tokens from wherever they are
@@ -15,7 +15,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kAlways = 0xffffffffu, kNever = 0;      // keys of tokens that stay in any case, and that are not there
 constexpr int kBins = 2048, kRounds = 3;
-constexpr int kAlone = 16384;                              // tokens up to which one workgroup has a head
+// Tokens up to which one workgroup has a head.  Alone / shared, us with the tokens that stay read back: 8 heads, 16384 tokens to 2048 28.4 / 42.7, 20000 35.1 / 43.0, four sequences
+// of 20000 40.3 / 48.2, 16 of them 75.9 / 93.9, 32768 40.8 / 43.5.
+constexpr int kAlone = 32768;
+constexpr int kAtOnce = 8;                                 // blocks of a wavefront that are asked for at once
 constexpr int kCountThreads = 1024, kCountBlocks = 128, kMaxChunks = 32;   // workgroups that share a head: blocks of each at least, and their number
 
 __device__ __forceinline__ constexpr int shift_of(int round) { return round == 0 ? 21 : round == 1 ? 10 : 0; }
@@ -47,13 +50,26 @@ __device__ __forceinline__ uint32_t key_of(float w) {
     return x & 0x80000000u ? ~x : x | 0x80000000u;
 }
 
-__device__ __forceinline__ uint32_t key_at(const EvictParams& p, const float* weights, int j, int n, bool paged) {
-    if (j >= n || !paged) return kNever;
-    return j < p.n_sink || j >= n - p.n_recent ? kAlways : key_of(weights[j]);
-}
-
-__device__ __forceinline__ bool block_paged(const EvictParams& p, int b, int block) {
-    return cache_paged(p.from, cache_page(p.from, b, block / p.from.page_blocks));
+// Keys of R blocks from `block` on (those from `end` on have none), a token of each for every lane: all that they need is asked for at once.
+template <int R>
+__device__ __forceinline__ void load_keys(const EvictParams& p, int b, const float* weights, int n, int block, int end, int lane, uint32_t (&key)[R]) {
+    float w[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int j = (block + i) * kBlock + lane;
+        w[i] = j < n ? weights[j] : 0.0f;
+    }
+    bool paged = false;                                    // of block `lane`
+    if (lane < R && block + lane < end) {
+        const int64_t entry = static_cast<int64_t>(b) * p.from.max_pages + (block + lane) / p.from.page_blocks;
+        paged = cache_paged(p.from, p.from.table ? p.from.table[entry] : static_cast<int>(entry));
+    }
+    const uint64_t there = __ballot(paged);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int j = (block + i) * kBlock + lane;
+        key[i] = (there >> i & 1) == 0 || j >= n ? kNever : j < p.n_sink || j >= n - p.n_recent ? kAlways : key_of(w[i]);
+    }
 }
 
 // inclusive sum over the lanes up to this one
@@ -123,11 +139,7 @@ __global__ __launch_bounds__(T) void select_kernel(EvictParams p) {
     const int n = cache_length_scalar(p.from, b);
     const float* const weights = p.weights + unit * p.stride;
     uint32_t key[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const int block = wave * R + i;
-        key[i] = block * kBlock < n && block_paged(p, b, block) ? key_at(p, weights, block * kBlock + lane, n, true) : kNever;
-    }
+    load_keys<R>(p, b, weights, n, wave * R, (n + kBlock - 1) / kBlock, lane, key);
 #pragma unroll
     for (int round = 0; round < kRounds; ++round)
         for (int i = threadIdx.x; i < kBins; i += T) hist[round][i] = 0;
@@ -284,10 +296,12 @@ __global__ __launch_bounds__(kCountThreads) void count_kernel(EvictParams p) {
     }
     for (int d = threadIdx.x; d < kBins; d += kCountThreads) hist[d] = 0;
     __syncthreads();
-    for (int block = first + wave; block < last; block += kCountThreads / 64) {
-        if (!block_paged(p, b, block)) continue;
-        const uint32_t key = key_at(p, weights, block * kBlock + lane, n, true);
-        if (key != kNever && (ROUND == 0 || key >> shift_of(ROUND - 1) == prefix)) atomicAdd(&hist[bin_at(digit_of(key, ROUND))], 1);
+    for (int block = first + kAtOnce * wave; block < last; block += kAtOnce * (kCountThreads / 64)) {
+        uint32_t key[kAtOnce];
+        load_keys<kAtOnce>(p, b, weights, n, block, last, lane, key);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+            if (key[i] != kNever && (ROUND == 0 || key[i] >> shift_of(ROUND - 1) == prefix)) atomicAdd(&hist[bin_at(digit_of(key[i], ROUND))], 1);
     }
     __syncthreads();
     for (int d = threadIdx.x; d < kBins; d += kCountThreads) chunk_hist(p, ROUND, unit, blockIdx.x)[d] = hist[d];
@@ -315,15 +329,20 @@ __global__ __launch_bounds__(kCountThreads) void emit_kernel(EvictParams p) {
     out.need = need;
     out.at = bins_above(before, found.digit, scratch);
     out.ties = before[bin_at(found.digit)];
-    for (int c = 0; c < static_cast<int>(blockIdx.x); ++c)
-        for (int round = 0; round < 2; ++round) out.at += p.above[(round * gridDim.y + unit) * p.chunks + c];
+    {                                                      // (a lane for each workgroup in front: there are kMaxChunks at most)
+        const bool front = lane < static_cast<int>(blockIdx.x);
+        const int x = front ? p.above[unit * p.chunks + lane] : 0, y = front ? p.above[(gridDim.y + unit) * p.chunks + lane] : 0;
+        out.at += __builtin_amdgcn_readlane(wave_scan(x + y), 63);
+    }
     // a wavefront's share of the workgroup's blocks
     const float* const weights = p.weights + unit * p.stride;
     const int each = (last - first + kCountThreads / 64 - 1) / (kCountThreads / 64), from = min(first + wave * each, last), to = min(from + each, last);
     auto for_keys = [&](auto f) __attribute__((always_inline)) {
-        for (int block = from; block < to; ++block) {
-            const bool paged = block_paged(p, b, block);
-            f(block * kBlock + lane, key_at(p, weights, block * kBlock + lane, n, paged));
+        for (int block = from; block < to; block += kAtOnce) {
+            uint32_t key[kAtOnce];
+            load_keys<kAtOnce>(p, b, weights, n, block, to, lane, key);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) f((block + i) * kBlock + lane, key[i]);
         }
     };
     int more = 0, same = 0;
@@ -560,8 +579,10 @@ extern "C" int vs_cache_evict(const vs_cache_t* cache, const float* weights, int
         hipLaunchKernelGGL((select_kernel<512, 8>), dim3(y), dim3(512), 0, s, p);
     } else if (max_n <= 8192) {
         hipLaunchKernelGGL((select_kernel<1024, 8>), dim3(y), dim3(1024), 0, s, p);
-    } else {
+    } else if (max_n <= 16384) {
         hipLaunchKernelGGL((select_kernel<1024, 16>), dim3(y), dim3(1024), 0, s, p);
+    } else {
+        hipLaunchKernelGGL((select_kernel<1024, 32>), dim3(y), dim3(1024), 0, s, p);
     }
     VS_LAUNCH_CHECK();
     hipLaunchKernelGGL(gather_kernel, dim3(p.blocks, static_cast<unsigned>(units)), dim3(kThreads), 0, s, p);

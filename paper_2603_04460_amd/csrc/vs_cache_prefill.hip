@@ -821,7 +821,7 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillPar
         float most = m;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (i + k >= parts) x[k].x = -INFINITY;                        // the last one again: no weight
+            if (i + k >= parts) x[k] = make_float2(-INFINITY, 0.0f);       // the last one again: no weight
             most = fmaxf(most, x[k].x);
         }
         const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - most);
@@ -831,7 +831,7 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillPar
         for (int j = 0; j < 2; ++j) y[j] = make_float4(y[j].x * f, y[j].y * f, y[j].z * f, y[j].w * f);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (x[k].x == -INFINITY) continue;
+            if (x[k].y == 0.0f) continue;                                  // (a sum that is not a number has to stay one)
             const float h = __builtin_amdgcn_exp2f(x[k].x - m);
             l = fmaf(x[k].y, h, l);
 #pragma unroll

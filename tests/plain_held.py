@@ -58,7 +58,7 @@ def scores(q, k, n, there, scale):
     rows = q.shape[0]
     x = q @ k.T * scale
     seen = (torch.arange(n) <= torch.arange(n - rows, n).unsqueeze(1)) & torch.from_numpy(there)
-    size = (q.abs() @ torch.nan_to_num(k.abs(), 0, 0, 0).T * scale).max().item() if n else 0.0
+    size = (torch.nan_to_num(q.abs(), 0, 0, 0) @ torch.nan_to_num(k.abs(), 0, 0, 0).T * scale).max().item() if n else 0.0
     return torch.where(seen, x, -torch.inf), seen, size
 
 

@@ -94,13 +94,14 @@ def test_tokens(lens, keep, n_sink, n_recent, place):
     check(cache, some_weights(keep, batch, 2, max(n, keep)), lens, n, keep, n_sink, n_recent, to, place.endswith("too"), place.endswith("too"))
 
 
-@pytest.mark.parametrize("n, keep", [(5000, 700), (40000, 3000), (70001, 20000)])
+@pytest.mark.parametrize("n, keep", [(2048, 5), (3000, 2999), (5000, 700), (8193, 64), (16385, 1000), (32768, 20000), (32769, 100), (40000, 3000), (70001, 20000), (300000, 777)])
 def test_long(n, keep):
     """Only numbers and weights, and what is read back: the bytes are as many as the tests above."""
     k, v = kv(n, 1, 2, n)
     cache, to = filled(n, k, v, 256), other(n, 1, 2, 64, keep)
     w = some_weights(n, 1, 2, n)
-    kept, out, after = evict(cache, w, [n], n, keep, 4, 100, to)
+    sink, recent = min(4, keep // 2), min(100, keep // 2)
+    kept, out, after = evict(cache, w, [n], n, keep, sink, recent, to)
     assert after.tolist() == [keep]
     a, b = [torch.empty(1, 2, n, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
     vs.cache_read(cache, a, b, n)
@@ -109,11 +110,32 @@ def test_long(n, keep):
     host = w.cpu().numpy()
     for h in range(2):
         x = host[0, h].astype(np.float64)
-        x[:4] = x[n - 100:] = np.inf
+        x[:sink] = x[n - recent:] = np.inf
         want = np.sort(np.lexsort((np.arange(n), -x))[:keep])
         assert np.array_equal(kept[0, h], want) and np.array_equal(out[0, h, :keep], host[0, h, want])
         at = torch.from_numpy(want).cuda()
         assert torch.equal(c[0, h], a[0, h, at]) and torch.equal(d[0, h], b[0, h, at])
+
+
+@pytest.mark.parametrize("n", [3000, 20000, 40000])
+def test_long_batches(n):
+    """Lengths of all kinds beside a long one, pages missing, equal weights by the thousand."""
+    lens, keep = [n, 0, 100, n - 777, 65], 900
+    k, v = kv(n, 1, 1, 64)
+    batch = len(lens)
+    pages = -(-n // 256)
+    data = torch.zeros(batch * pages, 1, 4, vs.CACHE_BLOCK_BYTES, dtype=torch.uint8, device="cuda")
+    table = torch.arange(batch * pages, dtype=torch.int32, device="cuda").view(batch, pages)
+    table[0, 3], table[3, 0], table[3, pages - 2] = -1, batch * pages, -5
+    cache, to = vs.Cache(data, table), other(n, batch, 1, 64, keep)
+    w = torch.round(some_weights(n, batch, 1, n) * 50) / 50
+    kept, out, after = evict(cache, w, lens, n, keep, 10, 50, to)
+    for b in range(batch):
+        there = present(cache, b, lens[b])
+        want = stays(w[b, 0, :lens[b]].cpu().numpy(), there, keep, 10, 50)
+        assert after[b] == len(want) == min(keep, there.sum())
+        assert kept[b, 0, :len(want)].tolist() == want and (kept[b, 0, len(want):] == -1).all()
+        assert np.array_equal(out[b, 0, :len(want)], w[b, 0].cpu().numpy()[want])
 
 
 def test_weights_of_every_kind():

@@ -204,6 +204,44 @@ def test_large_scores():
         assert abs(lse[0, 0, r].item() / (s.max().item() * 2.0 ** 26) - 1) <= 2.0 ** -21
 
 
+def test_many_sequences():
+    """More sequences than a wavefront has lanes, most of them short."""
+    lens = [(37 * i) % 150 for i in range(70)]
+    k, v = kv(33, 70, 1, 150)
+    cache = filled(29, k, v, 64)
+    q = queries(28, 70, 2, 131)
+    near(call(q, cache, lens, 150), attention(q, cache, lens, 150))
+
+
+def test_stream():
+    """On a stream of its own, beside another call with another workspace."""
+    k, v = kv(35, 1, 2, 2000)
+    cache = filled(31, k, v, 64)
+    qs = [queries(30 + i, 1, 8, 200 + 50 * i) for i in range(2)]
+    want = [call(q, cache, [2000], 2000) for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    got = [(torch.zeros_like(q), torch.zeros(1, 8, q.shape[2], device="cuda"), torch.zeros(vs.cache_prefill_workspace(1, 8, 2, q.shape[2], 2000), dtype=torch.uint8, device="cuda"))
+           for q in qs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for q, (o, lse, ws), s in zip(qs, got, streams):
+            vs.cache_prefill(q, cache, o, 2000, lse=lse, ws=ws, stream=s)
+    torch.cuda.synchronize()
+    for (o, lse, _), w in zip(got, want):
+        assert torch.equal(o, w[0]) and torch.equal(lse, w[1])
+
+
+def test_queries_that_are_not_finite():
+    """A row whose query is not finite is not a number; the other rows of its tile are what they are."""
+    k, v = kv(37, 1, 1, 500)
+    cache = filled(33, k, v, 64)
+    q = queries(34, 1, 4, 180)
+    q[0, 2, 77, 5], q[0, 1, 0, 0] = float("nan"), float("nan")
+    got = call(q, cache, [500], 500)
+    assert torch.isnan(got[0][0, 2, 77]).all() and torch.isnan(got[1][0, 1, 0])
+    near(got, attention(q, cache, [500], 500))
+
+
 def test_same_bits():
     k, v = kv(29, 3, 2, 3000)
     cache = filled(25, k, v, 64)
