@@ -412,13 +412,14 @@ int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch, int q_hea
                     float scale, void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /*
- * The same attention for any number of new tokens (1 .. VS_MAX_SEQ), a chunk of a prompt for instance; sequences of a batch may differ in length, prompts shorter
- * than n_q are padded in front.  Layouts, masks, rows without a key and missing pages as for vs_cache_attend, which takes calls of up to
- * VS_CACHE_MAX_NEW rows.
- * Arithmetic of more rows: K is exact in bf16, V in fp16 in units of the largest scale so far of its 32 channels (what is below 2^-27 of that, and groups that are not
- * finite, goes through fp32), P in fp16 (11 significant bits), fp32 accumulation and softmax.  The same call always gives the same bits.
+ * The same attention for any number of new tokens (1 .. VS_MAX_SEQ), a chunk of a prompt for instance; sequences of a batch may differ in length, prompts
+ * shorter than n_q are padded in front.  Layouts, masks, rows without a key (zeros, lse = -inf) and missing pages as for vs_cache_attend, whose kernels take
+ * up to VS_CACHE_MAX_NEW rows, within its limits, where there is little work (by batch, q_heads, n_q and max_n, not by lens).
+ * Arithmetic otherwise: K is exact in bf16; V in fp16 in units of the largest scale so far of its 32 channels, and what is below 2^-27 of that or not finite in
+ * bf16, exact too; P in fp16 (11 significant bits); fp32 accumulation and softmax.  The same call always gives the same bits.
  * A key whose weight is below 2^-31 of the row's largest counts as zero in the output, V below 2^-126 of the largest of its 32 channels, too.  Scores have to lie
- * within fp32's range, and V within 2^96.  At most 4096 query heads.  Workspace: vs_cache_prefill_workspace; the answer for max_n is enough for every smaller max_n of the same call.
+ * within fp32's range, and V within 2^96.  At most 4096 query heads.  Workspace: vs_cache_prefill_workspace; the answer for max_n is enough for every smaller
+ * max_n of the same call.
  */
 size_t vs_cache_prefill_workspace(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n);
 
@@ -435,7 +436,7 @@ int vs_cache_prefill(const void* q, const vs_cache_t* cache, int batch, int q_he
  *   old     [batch, kv_heads, stride] fp32 or NULL (zeros); may be `weights`, must not overlap it otherwise
  *   decay   0 .. 1; with 0 `old` is not read
  *   weights [batch, kv_heads, stride] fp32 out, stride >= max_n
- * A row without a key (lse = -inf) adds nothing.  A token of a missing page gets nothing and keeps decay * old.  scale * log2(e) has to be a normal fp32 number.
+ * A row without a key (lse = -inf; padding in front of a prompt, too) adds nothing.  A token of a missing page gets nothing and keeps decay * old.  scale * log2(e) has to be a normal fp32 number.
  * Arithmetic: K is exact in bf16; bf16 MFMA, fp32 exponentials and sums in a fixed order: the same call always gives the same bits.
  * At most 4096 query heads and 2^30 - 1 rows of a KV head (q_heads / kv_heads * n_q).  Workspace: vs_cache_weigh_workspace; the answer for max_n is enough for every smaller max_n of the same call.
  */

@@ -1,11 +1,11 @@
-// Attention of a chunk of new tokens over the 4-bit paged cache, more rows than vs_cache_attend takes.
+// Attention of a chunk of new tokens over the 4-bit paged cache, for more rows than vs_cache_attend takes or serves well.
 //   o = softmax(scale q K^T) V over the keys up to the query's own position
 // A workgroup has 256 query rows of a KV head, eight row blocks of 32 (hc query heads times 8 / hc stretches of 32 tokens), two to a wavefront:
 //   S^T = K Q^T (keys x rows, bf16),  O^T = V^T P^T (channels x rows, fp16), 32 x 32 x 16 matrix instructions
 // A block of 64 keys is turned into 16-bit numbers in LDS by all four wavefronts: K in bf16 with its scales (exact); V in fp16.  A wavefront has the
 // 32 channels of V that share scales and holds their unit 2^(R - 127), R at least the largest scale byte so far: an element is code 2^(E - R + 13), exact
-// for E from R - 27 to R.  What lies below, and groups that are not finite, stays out of the tile and is added to the rows that see it
-// in fp32; when R grows, everybody's sums are scaled.  Weights are held as 128 p (up to 2^15: the running maximum may be exceeded by 2^8) in fp16,
+// for E from R - 27 to R.  What lies below, and groups that are not finite, stays out of the tile; a unit that has such blocks goes over them once more at its end
+// (bf16, weights in two terms; NaN to the rows that see it).  When R grows, everybody's sums are scaled.  Weights are held as 128 p (up to 2^15: the running maximum may be exceeded by 2^8) in fp16,
 // 11 significant bits, which is why V is fp16: weights of 8 bits would double the rounding error of the output.
 // The rows of a K tile stand in LDS in the order (bits 3 and 4 of a key's number exchanged) in which a lane of S^T holds the weights that
 // the second product wants beside one word of V's codes, eight tokens of a channel: a word becomes one 16-byte operand.
@@ -29,8 +29,12 @@ constexpr float kGrownSum = 32768.0f;                      // 2^(8 + 7): no weig
 constexpr float kSafe = 1024.0f;                           // scores (log2 units) up to which a product and a difference in one rounding are good enough
 constexpr int kPartFloats = kUnitRows * 128 + 1088;          // (4352 bytes more: parts a power of two apart would all begin in the same memory channels)
 constexpr int kShares = 256;                               // a workgroup for every compute unit
+// A unit's start and end take 7 us, a step 2.6.  Without them in the division the workgroups with many short units end last: six prompts of up to 9001 tokens,
+// 32 / 8 heads, 470 us with 0, 424 with 3.
 constexpr int kStart = 3;                                  // steps that a unit's start and end count for
 constexpr int kAhead = 4;                                  // parts that are asked for at once
+// Small calls: shorter shares against more parts to join.  Us with 2 / 3 / 6 / 8: 8 / 2 heads, 300 rows of 1201 26.0 / 26.5 / 30.3 / 35.0, 32 / 8 heads, 130 of 1000
+// 29.6 / 28.5 / 31.9 / 35.7 (with 4 26.5 and 29.3).
 constexpr int kSteps = 2;                                  // of a workgroup, if there are so few
 constexpr int kTop = 13;                                   // fp16 exponent of a code with E = R: 6 * 2^13 < 65504
 constexpr int kSpan = 27;                                  // E from R - 27 (2^-14 in fp16) to R
@@ -220,6 +224,12 @@ __device__ __forceinline__ void no_keys(const PrefillParams& p, const Place& at,
     }
 }
 
+// What bounds it: a step of 64 keys x 256 rows is 64 matrix instructions of 32 cycles a wavefront, 2048, and takes about 2650: the vector instructions between them
+// (exponentials and their sums 1100, the turning of codes into 16 bits 400) share its issue slots.  2048 rows of 131072, 32 / 8 heads: 3650 us, 1.20 PFLOP/s
+// (a large product in bf16 reaches 1.39 here).  512 of 32768: 254 us.  Small calls are bound by their start (codes on their way, the search of a share's
+// place) and the join: 300 rows of 1201, 8 / 2 heads, 24.5 us for 5 us of products.
+// Eight row blocks for a workgroup: the turning of a block is shared by 256 rows; 160 KB of LDS hold one workgroup, whose wavefronts have 512 registers each.
+//
 // Softmax, products and the turning into 16 bits in one instruction stream, written out in issue order (one wavefront a SIMD hides nothing): the two row
 // blocks run half a stage apart, as in vs_dense_kernel.
 //   slot X(i): matrix: scores of block 0 for stage i, P V of block 0 for stage i - 1;  vector: softmax of block 1, stage i - 1, and V of stage i to LDS
@@ -874,30 +884,43 @@ void plan(PrefillParams& p, int batch, int q_heads, int kv_heads, int64_t n_q, i
     p.shares = static_cast<int>(shares < kShares ? shares : kShares);
 }
 
+// Up to VS_CACHE_MAX_NEW rows vs_cache_attend's kernels start faster; this one has the cheaper step.  It takes those rows where they fill more than half of its
+// units and there is work for 12 blocks of 256 rows a workgroup.  Us there / here, 32 / 8 heads: 128 rows of 8000 tokens (7.8 blocks) 34 / 48, 40 of 32768 (10) 54 / 55,
+// 48 of 32768 (12) 56 / 56, 100 of 16000 (12.2) 63 / 59, 128 of 16000 (15.6) 67 / 58, 128 of 131072 363 / 263, 64 of 131072 191 / 146, 128 of four sequences of 4000
+// (15.6) 66 / 44, of sixteen 193 / 100;  16 / 8 heads (units of 128 tokens), 65 rows of eight sequences of 32768 129 / 100;  8 / 8 heads (256 tokens), the same
+// 82 / 101, 128 rows 115 / 107.  32 rows or fewer would win by 1.5 at best, in large batches, and lose by 3.
+bool many_rows(const PrefillParams& p, int64_t max_n) {
+    if (p.n_q > VS_CACHE_MAX_NEW) return true;
+    const int64_t blocks = (max_n + kBlock - 1) / kBlock;
+    return 2 * p.n_q > p.tok && static_cast<int64_t>(p.batch) * p.q_heads * p.n_q * blocks >= static_cast<int64_t>(12) * kUnitRows * kShares;
+}
+
 size_t part_bytes(const PrefillParams& p) { return static_cast<size_t>(p.shares) * (2 * kPartFloats * sizeof(float) + 2 * kUnitRows * sizeof(float2) + sizeof(Joined)); }
 
 }  // namespace
 
 extern "C" size_t vs_cache_prefill_workspace(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) {
     if (!sizes_ok(batch, q_heads, kv_heads, n_q, max_n)) return 0;
-    if (n_q <= VS_CACHE_MAX_NEW) return vs_cache_attend_workspace(batch, q_heads, kv_heads, static_cast<int>(n_q), max_n);
     PrefillParams p;
     plan(p, batch, q_heads, kv_heads, n_q, max_n);
-    return part_bytes(p);
+    const size_t here = many_rows(p, max_n) ? part_bytes(p) : 0;
+    const size_t there = n_q <= VS_CACHE_MAX_NEW ? vs_cache_attend_workspace(batch, q_heads, kv_heads, static_cast<int>(n_q), max_n) : 0;
+    return here > there ? here : there;                                      // (a smaller max_n may go there)
 }
 
 extern "C" int vs_cache_prefill(const void* q, const vs_cache_t* cache, int batch, int q_heads, int64_t n_q, const int32_t* lens, int64_t max_n,
                                 float scale, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
-    if (n_q > 0 && n_q <= VS_CACHE_MAX_NEW)
+    PrefillParams p;
+    const bool sizes = cache && sizes_ok(batch, q_heads, cache->kv_heads, n_q, max_n);
+    if (sizes) plan(p, batch, q_heads, cache->kv_heads, n_q, max_n);
+    if (n_q > 0 && n_q <= VS_CACHE_MAX_NEW && !(sizes && many_rows(p, max_n)))
         return vs_cache_attend(q, cache, batch, q_heads, static_cast<int>(n_q), lens, max_n, scale, o, lse, ws, ws_bytes, stream);
     if (!q || !o || !vs::aligned16(q) || !vs::aligned16(o) || !vs::aligned16(lse) || !vs::aligned16(ws)) return VS_ERR_INVALID_ARG;
-    PrefillParams p;
     p.c = scale * 1.44269504088896340736f;
     if (q_heads <= 0 || n_q <= 0 || !(scale > 0.0f) || !(p.c < INFINITY)) return VS_ERR_INVALID_ARG;
     const int rc = vs::cache_params(cache, batch, lens, max_n, &p.cache);
     if (rc != VS_OK) return rc;
-    if (!sizes_ok(batch, q_heads, cache->kv_heads, n_q, max_n)) return VS_ERR_UNSUPPORTED;
-    plan(p, batch, q_heads, cache->kv_heads, n_q, max_n);
+    if (!sizes) return VS_ERR_UNSUPPORTED;
     if (!ws || ws_bytes < part_bytes(p)) return VS_ERR_WORKSPACE;
     p.q = static_cast<const uint16_t*>(q);
     p.o = static_cast<uint16_t*>(o);

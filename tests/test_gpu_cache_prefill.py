@@ -79,6 +79,17 @@ def test_few_rows(rows):
     assert torch.equal(got[0], o) and torch.equal(got[1], lse)
 
 
+@pytest.mark.parametrize("hq, hk, rows, lens, n", [(8, 2, 128, [4096] * 9 + [100, 0, 3999], 4096), (32, 4, 33, [13000, 12000], 47700), (4, 2, 65, [31000, 64], 100000)])
+def test_few_rows_of_long_sequences(hq, hk, rows, lens, n):
+    """Up to 128 rows where there is enough work to take this kernel: by the workspace it does."""
+    batch = len(lens)
+    assert vs.cache_prefill_workspace(batch, hq, hk, rows, n) > vs.cache_attend_workspace(batch, hq, hk, rows, n)
+    k, v = kv(12, batch, hk, max(lens))
+    cache = filled(8, k, v, 64, n=n)
+    q = queries(13, batch, hq, rows)
+    near(call(q, cache, lens, n), attention(q, cache, lens, n))
+
+
 def test_missing_pages():
     """Tokens without a page are not attended to: in front, in the middle, behind, all of a sequence's."""
     k, v = kv(13, 4, 2, 640)

@@ -58,12 +58,38 @@ def test_prefill_refused(p):
 
 @pytest.mark.parametrize("rows", [1, 17, 128])
 def test_prefill_of_few_rows_is_the_call_for_few_rows(p, rows):
-    for n in (100, 3000, 131072):
+    for n in (100, 3000):
         assert vs.cache_prefill_workspace(3, 8, 2, rows, n) == vs.cache_attend_workspace(3, 8, 2, rows, n)
     L = binding._load()
     c = ctypes.byref(cache(p))
     assert L.vs_cache_prefill(p, c, 1, 3, rows, p, 100, 0.1, p, None, p, HUGE, None) == -2
     assert L.vs_cache_prefill(p, c, 1, 4, rows, p, 257, 0.1, p, None, p, HUGE, None) == -1
+
+
+@pytest.mark.parametrize("batch, hq, hk, rows", [(1, 32, 8, 128), (16, 32, 8, 40), (5, 12, 6, 65), (2, 8, 8, 128), (1, 4096, 1, 33)])
+def test_prefill_workspace_is_enough_for_smaller_max_n(batch, hq, hk, rows):
+    """Where long sequences go to one kernel and short ones to the other."""
+    most = 0
+    for n in (1, 63, 64, 500, 2000, 4096, 4097, 8000, 16000, 24576, 40000, 131072, 1 << 20):
+        need = vs.cache_prefill_workspace(batch, hq, hk, rows, n)
+        assert need >= most and need >= vs.cache_attend_workspace(batch, hq, hk, rows, n)
+        most = need
+
+
+@pytest.mark.parametrize("rows", [100, 128])
+def test_prefill_of_few_rows_of_long_sequences_refused(p, rows):
+    """Rows for which vs_cache_prefill takes its own kernel, like any others."""
+    L = binding._load()
+    c = cache(p, kv_heads=8, max_pages=2048, pages=2048)
+    need = vs.cache_prefill_workspace(1, 32, 8, rows, 131072)
+    assert need > vs.cache_attend_workspace(1, 32, 8, rows, 131072)
+
+    def call(q=p, hq=32, o=p, ws=p, size=HUGE, scale=0.1, lens=p, n=131072):
+        return L.vs_cache_prefill(q, ctypes.byref(c), 1, hq, rows, lens, n, scale, o, p, ws, size, None)
+
+    for kw, code in ((dict(q=None), -1), (dict(o=p + 4), -1), (dict(lens=p + 2), -1), (dict(n=131073), -1), (dict(scale=0.0), -1), (dict(hq=33), -2),
+                     (dict(size=need - 1), -3), (dict(ws=None), -3)):
+        assert call(**kw) == code, kw
 
 
 def test_weigh_refused(p):
