@@ -2,9 +2,9 @@
 // their order, at the front of the same cache or of another one.
 // Weights become unsigned numbers in their order (first and last tokens above all, NaN below all); the smallest one that stays is found by three counts
 // of 11, 11 and 10 bits, and of those that equal it the first ones stay.
-//   select_kernel  up to 32768 tokens: a workgroup has a head, its keys in registers, the counts in LDS
+//   select_kernel  up to 32768 tokens: a workgroup has a head, its keys in registers, the counts in LDS (8 us for 1088 tokens, 12 for 16384)
 //   count_kernel, emit_kernel  more: workgroups share a head.  Each writes the counts of its tokens, the next kernel adds up those of the head; three
-//                  counts, then the numbers are written
+//                  counts, then the numbers are written (131072 tokens of 8 heads: 5.4, 8.2, 8.3 and 9.7 us, of each 5 to start and to read what the last left)
 //   gather_kernel  a workgroup for each block of 64 tokens that stay: codes and scales of 64 tokens from wherever they are
 //   put_kernel     a cache that is made smaller in place: blocks go through the workspace, so that all are read before one is written
 // Moving a token moves codes, nothing is rounded again.
@@ -15,8 +15,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kAlways = 0xffffffffu, kNever = 0;      // keys of tokens that stay in any case, and that are not there
 constexpr int kBins = 2048, kRounds = 3;
-// Tokens up to which one workgroup has a head.  Alone / shared, us with the tokens that stay read back: 8 heads, 16384 tokens to 2048 28.4 / 42.7, 20000 35.1 / 43.0, four sequences
-// of 20000 40.3 / 48.2, 16 of them 75.9 / 93.9, 32768 40.8 / 43.5.
+// Tokens up to which one workgroup has a head.  Alone / shared, us with the tokens that stay read back: 8 heads, to 2048 tokens from 10000 22.6 / 40.5, 20000 32.5 / 41.4,
+// 32768 35.3 / 41.9 (64 keys a lane would be the next), four sequences of 32768 41.9 / 48.4, 16 of 32768 86 / 113.
 constexpr int kAlone = 32768;
 constexpr int kAtOnce = 8;                                 // blocks of a wavefront that are asked for at once
 constexpr int kCountThreads = 1024, kCountBlocks = 128, kMaxChunks = 32;   // workgroups that share a head: blocks of each at least, and their number
@@ -50,27 +50,36 @@ __device__ __forceinline__ uint32_t key_of(float w) {
     return x & 0x80000000u ? ~x : x | 0x80000000u;
 }
 
-// Keys of R blocks from `block` on (those from `end` on have none), a token of each for every lane: all that they need is asked for at once.
+// Keys of R blocks from `block` on (those from `end` on have none), a token of each for every lane: all that they need is asked for at once, and waited for
+// where the keys are made.
 template <int R>
-__device__ __forceinline__ void load_keys(const EvictParams& p, int b, const float* weights, int n, int block, int end, int lane, uint32_t (&key)[R]) {
+struct Keys {
     float w[R];
+    int block, page;                                      // page of block `lane`
+    bool mine;
+    __device__ __forceinline__ void ask(const EvictParams& p, int b, const float* weights, int n, int from, int end, int lane) {
+        block = from;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const int j = (block + i) * kBlock + lane;
-        w[i] = j < n ? weights[j] : 0.0f;
+        for (int i = 0; i < R; ++i) {
+            const int j = (block + i) * kBlock + lane;
+            w[i] = j < n ? weights[j] : 0.0f;
+        }
+        mine = lane < R && block + lane < end;
+        page = 0;
+        if (mine) {
+            const int64_t entry = static_cast<int64_t>(b) * p.from.max_pages + (block + lane) / p.from.page_blocks;
+            page = p.from.table ? p.from.table[entry] : static_cast<int>(entry);
+        }
     }
-    bool paged = false;                                    // of block `lane`
-    if (lane < R && block + lane < end) {
-        const int64_t entry = static_cast<int64_t>(b) * p.from.max_pages + (block + lane) / p.from.page_blocks;
-        paged = cache_paged(p.from, p.from.table ? p.from.table[entry] : static_cast<int>(entry));
-    }
-    const uint64_t there = __ballot(paged);
+    __device__ __forceinline__ void make(const EvictParams& p, int n, int lane, uint32_t (&key)[R]) const {
+        const uint64_t there = __ballot(mine && cache_paged(p.from, page));
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const int j = (block + i) * kBlock + lane;
-        key[i] = (there >> i & 1) == 0 || j >= n ? kNever : j < p.n_sink || j >= n - p.n_recent ? kAlways : key_of(w[i]);
+        for (int i = 0; i < R; ++i) {
+            const int j = (block + i) * kBlock + lane;
+            key[i] = (there >> i & 1) == 0 || j >= n ? kNever : j < p.n_sink || j >= n - p.n_recent ? kAlways : key_of(w[i]);
+        }
     }
-}
+};
 
 // inclusive sum over the lanes up to this one
 __device__ __forceinline__ int wave_scan(int x) {
@@ -83,8 +92,10 @@ __device__ __forceinline__ int wave_scan(int x) {
     return x;
 }
 
-// Counts in LDS: bin d at 64 (d % 32) + d / 32, so that a lane's 32 bins, read one after the other, are no two in one bank with its neighbours'.
-__device__ __forceinline__ int bin_at(uint32_t d) { return static_cast<int>(64 * (d & 31) + (d >> 5)); }
+// Counts in LDS: bin d at d + d / 32.  Neighbouring bins, which weights of one size go to, are in different banks, and so are the bins that the lanes read at once,
+// 32 apart.
+constexpr int kHist = kBins + kBins / 32;
+__device__ __forceinline__ int bin_at(uint32_t d) { return static_cast<int>(d + (d >> 5)); }
 
 struct Found {
     int digit, need, total;        // digit that the `need`-th largest key has, how many with that digit stay, all keys
@@ -95,13 +106,13 @@ __device__ __forceinline__ Found find_digit(const int* hist, int need, int lane)
     int sum = 0;
     const int mine = 63 - lane;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) sum += hist[64 * i + mine];
+    for (int i = 0; i < 32; ++i) sum += hist[33 * mine + i];
     const int upto = wave_scan(sum);
     Found x;
     x.total = __builtin_amdgcn_readlane(upto, 63);
     const int l = __popcll(__ballot(upto < need));         // the lane that has it (need between 1 and the total)
     const int before = __builtin_amdgcn_readlane(upto - sum, l & 63);
-    const int count = lane < 32 ? hist[64 * (31 - lane) + 63 - l] : 0;     // its bins, the largest first
+    const int count = lane < 32 ? hist[33 * (63 - l) + 31 - lane] : 0;     // its bins, the largest first
     const int within = wave_scan(count);
     const int k = __popcll(__ballot(before + within < need));
     x.digit = 2047 - 32 * l - k;
@@ -131,7 +142,7 @@ struct Emit {
 // A wavefront has the tokens from 64 R * its number on, R of each lane.
 template <int T, int R>
 __global__ __launch_bounds__(T) void select_kernel(EvictParams p) {
-    __shared__ int hist[kRounds][kBins];
+    __shared__ int hist[kRounds][kHist];
     __shared__ int more_of[T / 64], same_of[T / 64];
     __shared__ Found found[kRounds];
     const int unit = blockIdx.x, b = unit / p.from.kv_heads;
@@ -139,10 +150,12 @@ __global__ __launch_bounds__(T) void select_kernel(EvictParams p) {
     const int n = cache_length_scalar(p.from, b);
     const float* const weights = p.weights + unit * p.stride;
     uint32_t key[R];
-    load_keys<R>(p, b, weights, n, wave * R, (n + kBlock - 1) / kBlock, lane, key);
+    Keys<R> of;
+    of.ask(p, b, weights, n, wave * R, (n + kBlock - 1) / kBlock, lane);
 #pragma unroll
     for (int round = 0; round < kRounds; ++round)
-        for (int i = threadIdx.x; i < kBins; i += T) hist[round][i] = 0;
+        for (int i = threadIdx.x; i < kHist; i += T) hist[round][i] = 0;
+    of.make(p, n, lane, key);
     __syncthreads();
     uint32_t prefix = 0;
     int need = p.keep, count = 0;
@@ -156,7 +169,7 @@ __global__ __launch_bounds__(T) void select_kernel(EvictParams p) {
             if (round == 0) {                              // no more than there are
                 int all = 0;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) all += hist[0][64 * i + lane];
+                for (int i = 0; i < 32; ++i) all += hist[0][33 * lane + i];
                 need = min(need, __builtin_amdgcn_readlane(wave_scan(all), 63));
             }
             Found x = {0, 0, 0};
@@ -205,39 +218,46 @@ __device__ __forceinline__ int32_t* chunk_hist(const EvictParams& p, int round, 
     return p.hist + ((static_cast<int64_t>(round) * gridDim.y + unit) * p.chunks + chunk) * kBins;
 }
 
-// The counts of a round of all of the head's workgroups into `hist`, those in front of this one into `before` (if it is wanted).
-__device__ __forceinline__ void add_up(const EvictParams& p, int round, int unit, int live, int* hist, int* before) {
-    for (int d = threadIdx.x; d < kBins; d += kCountThreads) {             // (the order of the bins is theirs)
-        int sum = 0, front = 0;
-        for (int c = 0; c < live; c += 8) {
-            int x[8];
+// The counts of a round of all of the head's workgroups into `hist`, this one's or (FRONT) those in front of it into `other`.
+template <bool FRONT>
+__device__ __forceinline__ void add_up(const EvictParams& p, int round, int unit, int live, int* hist, int* other) {
+    static_assert(kBins == 2 * kCountThreads, "a thread has two bins");
+    const int d = 2 * threadIdx.x;
+    int2 sum = make_int2(0, 0), some = sum;
+    for (int c = 0; c < live; c += kMaxChunks / 2) {
+        int2 x[kMaxChunks / 2];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = chunk_hist(p, round, unit, min(c + k, live - 1))[d];
+        for (int k = 0; k < kMaxChunks / 2; ++k) x[k] = *reinterpret_cast<const int2*>(chunk_hist(p, round, unit, min(c + k, live - 1)) + d);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                if (c + k < static_cast<int>(blockIdx.x)) front += x[k];
-                if (c + k < live) sum += x[k];
-            }
+        for (int k = 0; k < kMaxChunks / 2; ++k) {
+            const bool in = FRONT ? c + k < static_cast<int>(blockIdx.x) : c + k == static_cast<int>(blockIdx.x);
+            some.x += in ? x[k].x : 0;
+            some.y += in ? x[k].y : 0;
+            sum.x += c + k < live ? x[k].x : 0;
+            sum.y += c + k < live ? x[k].y : 0;
         }
-        hist[d] = sum;
-        if (before) before[d] = front;
     }
+    hist[bin_at(d)] = sum.x;
+    hist[bin_at(d) + 1] = sum.y;                           // (an even bin and the next one stand together)
+    other[bin_at(d)] = some.x;
+    other[bin_at(d) + 1] = some.y;
 }
 
 // What round `round` is about: keys that begin with prefix, need of them stay.  By all threads of the workgroup; the first count's total is count.
-__device__ __forceinline__ void find_round(const EvictParams& p, int round, int unit, int live, int* hist, int* before, Found* found, uint32_t* prefix, int* need,
+template <bool FRONT>
+__device__ __forceinline__ void find_round(const EvictParams& p, int round, int unit, int live, int* hist, int* other, Found* found, uint32_t* prefix, int* need,
                                            int* count) {
     const int lane = threadIdx.x & 63;
-    add_up(p, round, unit, live, hist, before);
     int2 last = make_int2(0, p.keep);
     if (round > 0) last = p.state[(round - 1) * gridDim.y + unit];
+    add_up<FRONT>(p, round, unit, live, hist, other);
     __syncthreads();
     if (threadIdx.x < 64) {
         int want = last.y;
         if (round == 0) {
             int all = 0;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) all += hist[64 * i + lane];
+            for (int i = 0; i < 32; ++i) all += hist[33 * lane + i];
             want = min(want, __builtin_amdgcn_readlane(wave_scan(all), 63));
         }
         Found x = {0, 0, 0};
@@ -255,8 +275,8 @@ __device__ __forceinline__ void find_round(const EvictParams& p, int round, int 
 __device__ __forceinline__ int bins_above(const int* hist, int digit, int* scratch) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int sum = 0;
-    for (int at = threadIdx.x; at < kBins; at += kCountThreads)
-        if (32 * (at & 63) + (at >> 6) > digit) sum += hist[at];
+    for (int d = threadIdx.x; d < kBins; d += kCountThreads)
+        if (d > digit) sum += hist[bin_at(d)];
     sum = __builtin_amdgcn_readlane(wave_scan(sum), 63);
     __syncthreads();
     if (lane == 0) scratch[wave] = sum;
@@ -269,7 +289,7 @@ __device__ __forceinline__ int bins_above(const int* hist, int digit, int* scrat
 // Workgroup (chunk, unit): counts of its tokens in round ROUND; what the rounds before found is added up first.
 template <int ROUND>
 __global__ __launch_bounds__(kCountThreads) void count_kernel(EvictParams p) {
-    __shared__ int hist[kBins], scratch[kCountThreads / 64];
+    __shared__ int hist[kHist], own[kHist], scratch[kCountThreads / 64];
     __shared__ Found found;
     const int unit = blockIdx.y, b = unit / p.from.kv_heads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -280,76 +300,77 @@ __global__ __launch_bounds__(kCountThreads) void count_kernel(EvictParams p) {
         return;
     }
     const float* const weights = p.weights + unit * p.stride;
+    Keys<kAtOnce> of;
+    of.ask(p, b, weights, n, first + kAtOnce * wave, last, lane);
     uint32_t prefix = 0;
     int need = p.keep, count = 0;
     if constexpr (ROUND > 0) {
-        find_round(p, ROUND - 1, unit, live, hist, nullptr, &found, &prefix, &need, &count);
+        find_round<false>(p, ROUND - 1, unit, live, hist, own, &found, &prefix, &need, &count);
         if (blockIdx.x == 0 && threadIdx.x == 0) {
             p.state[(ROUND - 1) * gridDim.y + unit] = make_int2(static_cast<int>(prefix), need);
             if (ROUND == 1 && unit == b * p.from.kv_heads) p.count[b] = count;
         }
-        for (int d = threadIdx.x; d < kBins; d += kCountThreads) hist[d] = chunk_hist(p, ROUND - 1, unit, blockIdx.x)[d];
-        __syncthreads();
-        const int above = bins_above(hist, found.digit, scratch);
+        const int above = bins_above(own, found.digit, scratch);
         if (threadIdx.x == 0) p.above[((ROUND - 1) * gridDim.y + unit) * p.chunks + blockIdx.x] = above;
-        __syncthreads();
     }
-    for (int d = threadIdx.x; d < kBins; d += kCountThreads) hist[d] = 0;
+    for (int d = threadIdx.x; d < kHist; d += kCountThreads) hist[d] = 0;
     __syncthreads();
     for (int block = first + kAtOnce * wave; block < last; block += kAtOnce * (kCountThreads / 64)) {
         uint32_t key[kAtOnce];
-        load_keys<kAtOnce>(p, b, weights, n, block, last, lane, key);
+        of.make(p, n, lane, key);
+        of.ask(p, b, weights, n, block + kAtOnce * (kCountThreads / 64), last, lane);
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i)
             if (key[i] != kNever && (ROUND == 0 || key[i] >> shift_of(ROUND - 1) == prefix)) atomicAdd(&hist[bin_at(digit_of(key[i], ROUND))], 1);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < kBins; d += kCountThreads) chunk_hist(p, ROUND, unit, blockIdx.x)[d] = hist[d];
+    for (int d = threadIdx.x; d < kBins; d += kCountThreads) chunk_hist(p, ROUND, unit, blockIdx.x)[d] = hist[bin_at(d)];
 }
 
 __global__ __launch_bounds__(kCountThreads) void emit_kernel(EvictParams p) {
-    __shared__ int hist[kBins], before[kBins], scratch[kCountThreads / 64], more_of[kCountThreads / 64], same_of[kCountThreads / 64];
+    __shared__ int hist[kHist], before[kHist], scratch[kCountThreads / 64], more_of[kCountThreads / 64], same_of[kCountThreads / 64];
     __shared__ Found found;
     const int unit = blockIdx.y, b = unit / p.from.kv_heads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = cache_length_scalar(p.from, b), blocks = (n + kBlock - 1) / kBlock, live = (blocks + p.chunk_blocks - 1) / p.chunk_blocks;
     const int first = blockIdx.x * p.chunk_blocks, last = min(first + p.chunk_blocks, blocks);
+    // a wavefront's share of the workgroup's blocks
+    const float* const weights = p.weights + unit * p.stride;
+    const int each = (last - first + kCountThreads / 64 - 1) / (kCountThreads / 64), from = min(first + wave * each, last), to = min(from + each, last);
+    Keys<kAtOnce> of;
+    if (first < last) of.ask(p, b, weights, n, from, to, lane);
     const int count = p.count[b];
     int32_t* const kept = p.kept ? p.kept + static_cast<int64_t>(unit) * p.keep : nullptr;
     if (kept && blockIdx.x == 0)
         for (int i = count + threadIdx.x; i < p.keep; i += kCountThreads) kept[i] = -1;
     if (first >= last || count == 0) return;
+    Emit out;
+    {                                                      // (a lane for each workgroup in front: there are kMaxChunks at most)
+        const bool front = lane < static_cast<int>(blockIdx.x);
+        const int x = front ? p.above[unit * p.chunks + lane] : 0, y = front ? p.above[(gridDim.y + unit) * p.chunks + lane] : 0;
+        out.at = __builtin_amdgcn_readlane(wave_scan(x + y), 63);
+    }
     uint32_t prefix;
     int need, unused;
-    find_round(p, 2, unit, live, hist, before, &found, &prefix, &need, &unused);
-    Emit out;
+    find_round<true>(p, 2, unit, live, hist, before, &found, &prefix, &need, &unused);
     out.index = p.index + static_cast<int64_t>(unit) * p.keep;
     out.kept = kept;
     out.least = prefix;
     out.need = need;
-    out.at = bins_above(before, found.digit, scratch);
+    out.at += bins_above(before, found.digit, scratch);
     out.ties = before[bin_at(found.digit)];
-    {                                                      // (a lane for each workgroup in front: there are kMaxChunks at most)
-        const bool front = lane < static_cast<int>(blockIdx.x);
-        const int x = front ? p.above[unit * p.chunks + lane] : 0, y = front ? p.above[(gridDim.y + unit) * p.chunks + lane] : 0;
-        out.at += __builtin_amdgcn_readlane(wave_scan(x + y), 63);
-    }
-    // a wavefront's share of the workgroup's blocks
-    const float* const weights = p.weights + unit * p.stride;
-    const int each = (last - first + kCountThreads / 64 - 1) / (kCountThreads / 64), from = min(first + wave * each, last), to = min(from + each, last);
-    auto for_keys = [&](auto f) __attribute__((always_inline)) {
-        for (int block = from; block < to; block += kAtOnce) {
-            uint32_t key[kAtOnce];
-            load_keys<kAtOnce>(p, b, weights, n, block, to, lane, key);
-#pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) f((block + i) * kBlock + lane, key[i]);
-        }
-    };
+    // the keys are in registers, where the wavefront has no more blocks than it asks for at once
+    uint32_t key[kAtOnce];
     int more = 0, same = 0;
-    for_keys([&](int, uint32_t key) {
-        more += __popcll(__ballot(key > prefix));
-        same += __popcll(__ballot(key == prefix));
-    });
+    for (int block = from; block < to; block += kAtOnce) {
+        if (block > from) of.ask(p, b, weights, n, block, to, lane);
+        of.make(p, n, lane, key);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            more += __popcll(__ballot(key[i] > prefix));
+            same += __popcll(__ballot(key[i] == prefix));
+        }
+    }
     if (lane == 0) {
         more_of[wave] = more;
         same_of[wave] = same;
@@ -360,7 +381,14 @@ __global__ __launch_bounds__(kCountThreads) void emit_kernel(EvictParams p) {
         out.ties += same_of[w];
     }
     out.at += min(out.ties, need);
-    for_keys([&](int j, uint32_t key) { out.take(j, key, lane); });
+    for (int block = from; block < to; block += kAtOnce) {
+        if (each > kAtOnce) {
+            of.ask(p, b, weights, n, block, to, lane);
+            of.make(p, n, lane, key);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) out.take((block + i) * kBlock + lane, key[i], lane);
+    }
 }
 
 // block `block` of sequence b, head h; null where the page table names no page.  (cache_block for a block that differs from lane to lane)
@@ -377,11 +405,14 @@ __device__ __forceinline__ bool unmoved(const EvictParams& p, int unit, int bloc
     return p.same && p.index[static_cast<int64_t>(unit) * p.keep + last] == last;
 }
 
-// Blocks of which the codes of V and all scales go through LDS.  0 / 2 / 4 / 8 of them, us: 64 sequences of up to 1088 tokens to 1024, read back 140 / 126 / 132 / 134, 16 of
-// 4160 to 4096 135 / 117 / 122 / 127, 12 of up to 12001 to 2000 59.1 / 57.0 / 59.9 / 60.5, one of 131072 to 1024 69.6 / 72.9 / 73.2 / 70.4.
+// Blocks of which the codes of V and all scales go through LDS.  0 / 2 / 4 / 8 of them, us: 64 sequences of up to 1088 tokens to 1024, read back 114 / 107 / 106 / 123, 16 of
+// 4160 to 4096 112 / 103 / 103 / 118, 12 of up to 12001 to 2000 44.3 / 44.7 / 44.8 / 49.2, one of 131072 to 16384 63 / 63 / 63 / 67 (8 take the room of other workgroups).
 constexpr int kSpan = 2;
 constexpr int kHeldBytes = kBlockBytes - kVCodes;
 
+// Bound by latency and memory: the numbers, then the page table, then the codes.  1024 of up to 1088 tokens of 64 sequences 47 us, 3.1 TB/s; where few tokens of a
+// block stay, the block's V is read for them (a token's codes lie in every 16 bytes of a half of it): 16384 of 131072 18 us for 90 MB.  Workgroups of a head are
+// gridDim.x apart: on one XCD where the number of heads is a multiple of eight, so that a block that two of them read comes from memory once (47 against 49 us).
 // K's rows come from where they are.  Of V a word is eight tokens of a channel: a thread puts its four words (two channels, 16 tokens) together from 16 pieces
 // of 16 bytes, each with both channels of one token.  Where the tokens stand in no more than kSpan blocks, which is so while most of them stay, those
 // blocks' codes of V and scales are read once, into LDS.
@@ -390,20 +421,24 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictParams p) {
     __shared__ const uint8_t* from[kBlock];
     __shared__ int place[kBlock];
     __shared__ const uint8_t* source[kSpan];
-    const int unit = blockIdx.y, b = unit / p.from.kv_heads, h = unit - b * p.from.kv_heads, block = blockIdx.x;
+    const int unit = blockIdx.x, b = unit / p.from.kv_heads, h = unit - b * p.from.kv_heads, block = blockIdx.y;
+    const int64_t head = static_cast<int64_t>(unit) * p.keep;
+    // numbers of its tokens, asked for together with how many there are (behind `count` they are whatever the workspace held, and not used)
+    const int slot = block * kBlock + (threadIdx.x & (kBlock - 1));
+    const int number = slot < p.keep ? p.index[head + slot] : 0;
     const int count = p.count[b];
     if (!p.block_stage && !p.weight_stage && block == 0 && h == 0 && threadIdx.x == 0) p.lens_out[b] = count;
     if (block * kBlock >= count) return;
-    const int64_t head = static_cast<int64_t>(unit) * p.keep;
     uint8_t* const there = cache_block(p.to, b, h, block);
     uint8_t* const to = p.block_stage ? p.block_stage + (static_cast<int64_t>(unit) * p.blocks + block) * kBlockBytes : there;
     const int tokens = min(count - block * kBlock, kBlock);
-    const int j0 = p.index[head + block * kBlock] / kBlock, j1 = p.index[head + block * kBlock + tokens - 1] / kBlock;     // blocks of the first and the last
+    const int j0 = __builtin_amdgcn_readfirstlane(number) / kBlock, j1 = __builtin_amdgcn_readlane(number, tokens - 1) / kBlock;     // blocks of the first and the last
+    const bool still = __builtin_amdgcn_readlane(number, tokens - 1) == block * kBlock + tokens - 1;       // all tokens are where they were
     const bool near = tokens == kBlock && j1 - j0 < kSpan;
     if (threadIdx.x < kBlock) {
-        const int i = block * kBlock + threadIdx.x;
+        const int i = slot;
         if (threadIdx.x < tokens) {
-            const int j = p.index[head + i];
+            const int j = number;
             from[threadIdx.x] = block_of_lane(p.from, b, h, j / kBlock);
             place[threadIdx.x] = (j / kBlock - j0) * kBlock + j % kBlock;
             if (p.weights_out) {
@@ -420,7 +455,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictParams p) {
         source[k] = near && j0 + k <= j1 ? block_of_lane(p.from, b, h, j0 + k) : nullptr;
     }
     __syncthreads();
-    if (!there || unmoved(p, unit, block, count)) return;
+    if (!there || (p.same && still)) return;
     const int token = threadIdx.x >> 2, quarter = threadIdx.x & 3;
     const uint4 x = *reinterpret_cast<const uint4*>(from[token] + 64 * (place[token] & 63) + 16 * quarter);
     // words (channel, u) of tokens 32 u + 4 c + 0 .. 3 and 16 more: channels 32 p + m and 16 more, u = 0, 1
@@ -470,7 +505,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictParams p) {
 }
 
 __global__ __launch_bounds__(kThreads) void put_kernel(EvictParams p) {
-    const int unit = blockIdx.y, b = unit / p.from.kv_heads, h = unit - b * p.from.kv_heads, block = blockIdx.x;
+    const int unit = blockIdx.x, b = unit / p.from.kv_heads, h = unit - b * p.from.kv_heads, block = blockIdx.y;
     const int count = p.count[b];
     if (block == 0 && h == 0 && threadIdx.x == 0) p.lens_out[b] = count;
     if (block * kBlock >= count) return;
@@ -585,10 +620,10 @@ extern "C" int vs_cache_evict(const vs_cache_t* cache, const float* weights, int
         hipLaunchKernelGGL((select_kernel<1024, 32>), dim3(y), dim3(1024), 0, s, p);
     }
     VS_LAUNCH_CHECK();
-    hipLaunchKernelGGL(gather_kernel, dim3(p.blocks, static_cast<unsigned>(units)), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL(gather_kernel, dim3(y, p.blocks), dim3(kThreads), 0, s, p);
     VS_LAUNCH_CHECK();
     if (p.block_stage || p.weight_stage) {
-        hipLaunchKernelGGL(put_kernel, dim3(p.blocks, static_cast<unsigned>(units)), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL(put_kernel, dim3(y, p.blocks), dim3(kThreads), 0, s, p);
         VS_LAUNCH_CHECK();
     }
     return VS_OK;
