@@ -224,10 +224,10 @@ __device__ __forceinline__ void no_keys(const PrefillParams& p, const Place& at,
     }
 }
 
-// What bounds it: a step of 64 keys x 256 rows is 64 matrix instructions of 32 cycles a wavefront, 2048, and takes about 2650: the vector instructions between them
-// (exponentials and their sums 1100, the turning of codes into 16 bits 400) share its issue slots.  2048 rows of 131072, 32 / 8 heads: 3650 us, 1.20 PFLOP/s
-// (a large product in bf16 reaches 1.39 here).  512 of 32768: 254 us.  Small calls are bound by their start (codes on their way, the search of a share's
-// place) and the join: 300 rows of 1201, 8 / 2 heads, 24.5 us for 5 us of products.
+// What bounds it is power, behind it the vector instructions: a step of 64 keys x 256 rows is 64 matrix instructions of 32 cycles a wavefront, 2048 of about 3400
+// cycles, and the clock is at 1.9 GHz.  A loop of matrix instructions alone reaches 1.77 PFLOP/s on numbers like these, one with a softmax's exponentials and
+// operands from LDS 1.2, whatever its order.  2048 rows of 131072, 32 / 8 heads: 3650 us, 1.20 PFLOP/s; 512 of 32768 252 us.  Small calls are bound by their start
+// (codes on their way, the search of a share's place) and the join: 300 rows of 1201, 8 / 2 heads, 23 us for 5 us of products.
 // Eight row blocks for a workgroup: the turning of a block is shared by 256 rows; 160 KB of LDS hold one workgroup, whose wavefronts have 512 registers each.
 //
 // Softmax, products and the turning into 16 bits in one instruction stream, written out in issue order (one wavefront a SIMD hides nothing): the two row

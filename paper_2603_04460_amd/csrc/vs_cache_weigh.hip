@@ -22,7 +22,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kWaves = 4;
 constexpr int kFewRows = 16;
 constexpr int kRing = 8;                                   // tiles of rows in LDS
-constexpr int kAhead = 4;                                  // tiles that are asked for in advance
+constexpr int kAhead = 4;                                  // tiles that are asked for in advance (6: the same)
 constexpr int kTileBytes = 32 * 256;
 
 struct WeighParams {
@@ -165,9 +165,12 @@ __device__ __forceinline__ void lds_load4(uint32_t at, const void* base, uint32_
 
 // Workgroup (x, unit, part): wavefronts take blocks 4 i + wave of the workgroup's p.blocks groups of four; part: a stretch of the tiles of rows.
 // A tile of rows is in LDS as it is in memory, but for its 16-byte chunks: chunk c of row r stands at c ^ (r % 16), so that 16 lanes that read a
-// chunk of 16 rows use all banks.  Where all of a part's tiles fit in LDS they are read once; otherwise each is asked for kAhead tiles ahead.
+// chunk of 16 rows use all banks.  Where all of a part's tiles fit in LDS they are read once; otherwise two at a time are asked for, kAhead tiles ahead.
 // The two halves of a group's keys run half a step apart: between the products of one stand the exponentials of the other.  Operands of the next
 // tile are read behind the last products of this one's.
+// What bounds it is power: the clock falls under this load, and a loop of these instructions alone, with operands from LDS and numbers like these, takes 220 ns
+// for 32 x 32 scores and weights on a SIMD with one wavefront or two (1.2 PFLOP/s; without exponentials and LDS 1.77).  2048 tokens of 131072, 32 / 8 heads: 2100 us,
+// 256 ns;  1024 of 32749 284 us;  64 of 131072 72 us, where eight tiles have to pay for a block's conversion and sums.
 template <bool RESIDENT>
 __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams p) {
     __shared__ __align__(16) uint8_t tile_of[kRing][kTileBytes];
@@ -182,33 +185,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)tile_of));
     const uint32_t lds1 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)lse_of));
 
-    // Tiles that some row of which sees a key of the group: of a run those from `skip` on
+    // A tile of 32 rows: the run's rows from `at` on.
     struct Tile {
-        int run, at;
+        int64_t row;                                       // of the call
+        int at;
     };
-    auto tile_number = [&](int i) { return Tile{i / p.tiles, i % p.tiles}; };
+    auto tile_number = [&](int i) { return Tile{static_cast<int64_t>(unit) * p.rows + i / p.tiles * p.run_rows + i % p.tiles * 32, i % p.tiles * 32}; };
+    // the next one; of a run those from row `skip` on
     auto forward = [&](Tile& t, int skip) __attribute__((always_inline)) {
-        if (++t.at == p.tiles) {
-            ++t.run;
+        t.at += 32;
+        t.row += 32;
+        if (t.at >= p.run_rows) {
+            t.row += p.run_rows - t.at + skip;
             t.at = skip;
         }
     };
-    auto rows_of = [&](const Tile& t) __attribute__((always_inline)) { return static_cast<int64_t>(unit) * p.rows + t.run * p.run_rows; };
+    const uint32_t chunk0 = 16 * ((lane & 15) ^ ((8 * wave + (lane >> 4)) & 15)), chunk1 = chunk0 ^ 64;    // (row + 4: bit 2 of the row, which is clear in the first)
+    const int row_mine = 8 * wave + (lane >> 4);
     auto request = [&](const Tile& t, int slot) __attribute__((always_inline)) {
-        const int64_t r = rows_of(t) + 32 * t.at;
-        const int most = p.run_rows - 1 - 32 * t.at;       // (the last tile's rows behind the last one: that one again, masked)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int row = 8 * wave + 4 * k + (lane >> 4), chunk = (lane & 15) ^ (row & 15);
-            lds_load16(static_cast<uint32_t>(256 * min(row, most) + 16 * chunk), p.q + r * 128, lds0 + slot * kTileBytes + 1024 * (2 * wave + k));
-        }
-        lds_load4(static_cast<uint32_t>(4 * min(col, most)), p.lse + r, lds1 + 256 * (kWaves * slot + wave));
+        const int most = p.run_rows - 1 - t.at;            // (the last tile's rows behind the last one: that one again, masked)
+        const uint16_t* const from = p.q + t.row * 128;
+        lds_load16(256 * min(row_mine, most) + chunk0, from, lds0 + slot * kTileBytes + 2048 * wave);
+        lds_load16(256 * min(row_mine + 4, most) + chunk1, from, lds0 + slot * kTileBytes + 2048 * wave + 1024);
+        lds_load4(static_cast<uint32_t>(4 * min(col, most)), p.lse + t.row, lds1 + 256 * (kWaves * slot + wave));
     };
 
-    struct Step {
-        Tile tile;
-        int slot, next;
-    };
     struct Held {
         uint4 k[2][2];
         uint32_t scale[2];                                 // of groups 2 half, 2 half + 1: words of tokens 16 t + col % 16
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
                 asm volatile("" : "+v"(sum[u][e]));        // (at this place)
             }
         };
-        // Products of the tile at `slot` with keys 32 u ..; OTHER: weights of the other 32 keys (of this tile for u = 1, of the one in front for u = 0)
+        // Products of the tile whose operands are there with keys 32 u ..; OTHER: weights of the other 32 keys (of this tile for u = 1, of the one in front for u = 0)
         auto products = [&](auto half_of, auto other, int next_slot) __attribute__((always_inline)) {
             constexpr int U = decltype(half_of)::value;
 #pragma unroll
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
         };
         // exponents as they are, where the row sees the key
         auto mask = [&](int u, const Tile& t) __attribute__((always_inline)) {
-            const int in_run = 32 * t.at + col, row = p.runs == 1 ? in_run % p.n_q : in_run;
+            const int in_run = t.at + col, row = p.runs == 1 ? in_run % p.n_q : in_run;
             const int before = (in_run < p.run_rows ? base + row : -1) - first - 4 * half - 32 * u;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
         using O = std::integral_constant<int, 1>;
         auto step = [&](auto old, const Tile& t, int slot, int next_slot) __attribute__((always_inline)) {
             const float lse = lse_of[slot][wave][lane];
-            const bool masked = edge || 32 * t.at + 32 > p.run_rows;
+            const bool masked = edge || t.at + 32 > p.run_rows;
             products(Z{}, old, 0);
             const RowConst row = row_const(p, lse);
             high = row.high;
@@ -317,52 +318,54 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
             products(O{}, std::true_type{}, next_slot);
             if (masked) mask(1, t);
         };
-        // tiles 0, 1, ..: begin(i) in front of the products of the i-th (its tile, its slot and the next one's), more: is there another one
-        auto run = [&](auto begin, auto more) __attribute__((always_inline)) {
-            Step x = begin(0);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) read(x.slot, j);
-            step(std::false_type{}, x.tile, x.slot, x.next);
-            for (int i = 1; more(i); ++i) {
-                x = begin(i);
-                step(std::true_type{}, x.tile, x.slot, x.next);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) weigh(1, j);
-        };
         if constexpr (RESIDENT) {
             Tile t = tile_number(i0);
-            run([&](int i) __attribute__((always_inline)) {
-                if (i > 0) forward(t, 0);
-                return Step{t, i, i0 + i + 1 < i1 ? i + 1 : 0};
-            }, [&](int i) __attribute__((always_inline)) { return i0 + i < i1; });
-        } else {
-            // rows in front of the group's first key see nothing of it
-            const int skip = p.runs == 1 ? 0 : min(max(group * kWaves * kBlock - base, 0) >> 5, p.tiles - 1);
-            Tile t = tile_number(i0);
-            t.at = max(t.at, skip);
-            auto here = [&](const Tile& x) __attribute__((always_inline)) { return x.run * p.tiles + x.at < i1; };
-            Tile ahead = t, now = t;
-            __syncthreads();                               // the group before this one is out of the ring
-            auto ask = [&](int i) __attribute__((always_inline)) {         // for the i-th tile (behind the last one: the first again)
-                request(here(ahead) ? ahead : t, i & (kRing - 1));
-                if (here(ahead)) forward(ahead, skip);
-            };
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) ask(i);
-            if (here(t))
-                run([&](int i) __attribute__((always_inline)) {
-                    if (i > 0) forward(now, skip);
-                    // tiles i and i + 1 are there, tile i - 1 has been read
-                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(3 * (kAhead - 2)) : "memory");
-                    ask(i + kAhead);
-                    return Step{now, i & (kRing - 1), (i + 1) & (kRing - 1)};
-                }, [&](int) __attribute__((always_inline)) {
-                    Tile x = now;
-                    forward(x, skip);
-                    return here(x);
-                });
+            for (int j = 0; j < 8; ++j) read(0, j);
+            step(std::false_type{}, t, 0, i0 + 1 < i1 ? 1 : 0);
+            for (int i = 1; i < i1 - i0; ++i) {
+                forward(t, 0);
+                step(std::true_type{}, t, i, i0 + i + 1 < i1 ? i + 1 : 0);
+            }
+        } else {
+            // (the first tile has none in front: weights of 2^-inf)
+            by = 0.0f;
+            used = INFINITY;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[1][e] = 0.0f;
+            // rows in front of the group's first key see nothing of it: of a run the tiles from `skip` on
+            const int skip = p.runs == 1 ? 0 : min(max(group * kWaves * kBlock - base, 0) >> 5, p.tiles - 1);
+            const int at0 = max(i0 % p.tiles, skip), last_run = (i1 - 1) / p.tiles - i0 / p.tiles, last = (i1 - 1) % p.tiles;
+            const int count = last_run == 0 ? last + 1 - at0 : p.tiles - at0 + (last_run - 1) * (p.tiles - skip) + max(last + 1 - skip, 0);
+            if (count > 0) {
+                Tile now = tile_number(i0 / p.tiles * p.tiles + at0), ahead = now;
+                int asked = 0;
+                auto ask = [&]() __attribute__((always_inline)) {          // for the next two tiles (behind the last one: that one again)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        request(ahead, asked & (kRing - 1));
+                        if (++asked < count) forward(ahead, 32 * skip);
+                    }
+                };
+                __syncthreads();                           // the group before this one is out of the ring
+                for (int i = 0; i < kAhead; i += 2) ask();
+                asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(3 * (kAhead - 1)) : "memory");
+#pragma unroll
+                for (int j = 0; j < 8; ++j) read(0, j);
+                for (int i = 0; i < count; i += 2) {
+                    // tiles i, i + 1 and i + 2 are there, tile i - 1 has been read
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(3 * (kAhead - 3)) : "memory");
+                    ask();
+                    step(std::true_type{}, now, i & (kRing - 1), (i + 1) & (kRing - 1));
+                    forward(now, 32 * skip);
+                    if (i + 1 >= count) break;
+                    step(std::true_type{}, now, (i + 1) & (kRing - 1), (i + 2) & (kRing - 1));
+                    forward(now, 32 * skip);
+                }
+            }
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) weigh(1, j);
         // key 32 u + 8 (e / 4) + 4 half + e % 4 to a lane: first over 16 lanes, then over the two rows of 16
         float total[2];
 #pragma unroll
