@@ -416,15 +416,21 @@ void plan(WeighParams& p, int batch, int q_heads, int kv_heads, int64_t n_q, int
         p.blocks = static_cast<int>(each < 1 ? 1 : each < 16 ? each : 16);
         return;
     }
-    // short runs would leave tiles half empty; long ones leave out what their first rows do not see
-    p.runs = n_q >= 256 ? static_cast<int>(q_heads / kv_heads) : 1;
+    // A run for each head leaves out what its first rows do not see, at the price of a last tile that is not full.  All heads in one / one for each, us: 400 tokens of
+    // 32768 126 / 129, 200 of 32768 70 / 76, 256 of 2000 12.6 / 12.3, 160 of 32768 57.4 / 56.8.
+    const int64_t groups = (blocks + kWaves - 1) / kWaves;
+    p.runs = n_q * n_q >= 2 * ((32 - n_q % 32) % 32) * groups * kWaves * kBlock ? static_cast<int>(q_heads / kv_heads) : 1;
     p.run_rows = p.runs == 1 ? p.rows : p.n_q;
     p.tiles = (p.run_rows + 31) / 32;
-    const int64_t groups = (blocks + kWaves - 1) / kWaves, all = static_cast<int64_t>(p.runs) * p.tiles;
+    const int64_t all = static_cast<int64_t>(p.runs) * p.tiles;
     // Two workgroups run on a compute unit, the older one faster: with fewer than 16 for each the last ones run alone.  512 / 2048 / 4096 / 8192 workgroups, us:
     // 1024 tokens of 32749 335 / 303 / 293 / 298, 128 of 32768 48.2 / 46.4 / 46.2 / -, 4096 of 4096 177 / 171 / 178 / 178.
     int64_t parts = (4096 + units * groups - 1) / (units * groups);
     if (parts > (all + 7) / 8) parts = (all + 7) / 8;      // of eight tiles at least
+    // .. of four, up to two workgroups a compute unit.  Eight / four / two tiles at least, us: 300 tokens of 300 12.1 / 10.2 / 10.2, 128 of 2000 12.3 / 10.2 / 10.5,
+    // 400 of 2000 16.8 / 15.9 / 16.1, 32 of 2000 7.1 / 7.4 / 10.4;  four for all: 1000 of 1000 18.2 / 19.8.
+    const int64_t few = 512 / (units * groups), most = (all + 3) / 4;
+    if (parts < few) parts = few < most ? few : most;
     if (parts > 64) parts = 64;
     p.parts = static_cast<int>(parts);
     const int64_t each = all <= kRing ? units * groups / 1024 : 1;
@@ -437,7 +443,7 @@ size_t part_bytes(const WeighParams& p, int64_t units) { return p.parts > 1 ? st
 
 extern "C" size_t vs_cache_weigh_workspace(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n) {
     if (!sizes_ok(batch, q_heads, kv_heads, n_q, max_n)) return 0;
-    // (fewer keys are shared by more workgroups: the most that any length up to max_n takes)
+    // (fewer groups of blocks are shared by more workgroups: the most that any length up to max_n takes)
     size_t most = 0;
     const int64_t units = static_cast<int64_t>(batch) * kv_heads;
     for (int64_t n = kBlock * kWaves;; n += kBlock * kWaves) {

@@ -1,6 +1,7 @@
 """Host side of the calls on held tokens (chunk attention, weights, eviction): refusals and sizes, nothing is launched; and the plain eviction."""
 import ctypes
 import math
+import random
 
 import numpy as np
 import pytest
@@ -74,6 +75,16 @@ def test_prefill_workspace_is_enough_for_smaller_max_n(batch, hq, hk, rows):
         need = vs.cache_prefill_workspace(batch, hq, hk, rows, n)
         assert need >= most and need >= vs.cache_attend_workspace(batch, hq, hk, rows, n)
         most = need
+
+
+def test_workspaces_are_enough_for_smaller_max_n():
+    rng = random.Random(3)
+    for _ in range(400):
+        hk = rng.choice([1, 2, 8])
+        sizes = rng.choice([1, 1, 2, 5, 60]), hk * rng.choice([1, 2, 4, 8]), hk, rng.randint(1, rng.choice([40, 300, 4000]))
+        n = rng.randint(1, 20000)
+        for f in (vs.cache_prefill_workspace, vs.cache_weigh_workspace):
+            assert f(*sizes, rng.randint(1, n)) <= f(*sizes, n), (f.__name__, sizes, n)
 
 
 @pytest.mark.parametrize("rows", [100, 128])
