@@ -98,10 +98,10 @@ constexpr int kHist = kBins + kBins / 32;
 __device__ __forceinline__ int bin_at(uint32_t d) { return static_cast<int>(d + (d >> 5)); }
 
 struct Found {
-    int digit, need, total;        // digit that the `need`-th largest key has, how many with that digit stay, all keys
+    int digit, need, total;        // digit that the `need`-th largest key has, how many with that digit stay, how many stay in all
 };
 
-// By one wavefront: lane l has the bins 2047 - 32 l down to 2016 - 32 l.
+// By one wavefront: lane l has the bins 2047 - 32 l down to 2016 - 32 l.  No more than there are can be needed.
 __device__ __forceinline__ Found find_digit(const int* hist, int need, int lane) {
     int sum = 0;
     const int mine = 63 - lane;
@@ -109,7 +109,9 @@ __device__ __forceinline__ Found find_digit(const int* hist, int need, int lane)
     for (int i = 0; i < 32; ++i) sum += hist[33 * mine + i];
     const int upto = wave_scan(sum);
     Found x;
-    x.total = __builtin_amdgcn_readlane(upto, 63);
+    need = min(need, __builtin_amdgcn_readlane(upto, 63));
+    if (need <= 0) return {0, 0, 0};
+    x.total = need;
     const int l = __popcll(__ballot(upto < need));         // the lane that has it (need between 1 and the total)
     const int before = __builtin_amdgcn_readlane(upto - sum, l & 63);
     const int count = lane < 32 ? hist[33 * (63 - l) + 31 - lane] : 0;     // its bins, the largest first
@@ -139,10 +141,12 @@ struct Emit {
     }
 };
 
-// A wavefront has the tokens from 64 R * its number on, R of each lane.
+// A wavefront has the tokens from 64 R * its number on, R of each lane.  Bound by latency: the keys, then three times counts, a barrier, a search by one wavefront
+// and a barrier.  256 threads with 8 keys / 512 with 4 / 1024 with 2, us with the tokens that stay moved and read back: 600 tokens of one sequence 15.9 / 15.3 / 15.3, 64 of up to
+// 1088 106.0 / 104.8 / 105.2.
 template <int T, int R>
 __global__ __launch_bounds__(T) void select_kernel(EvictParams p) {
-    __shared__ int hist[kRounds][kHist];
+    __shared__ __align__(16) int hist[kRounds][kHist];
     __shared__ int more_of[T / 64], same_of[T / 64];
     __shared__ Found found[kRounds];
     const int unit = blockIdx.x, b = unit / p.from.kv_heads;
@@ -152,9 +156,8 @@ __global__ __launch_bounds__(T) void select_kernel(EvictParams p) {
     uint32_t key[R];
     Keys<R> of;
     of.ask(p, b, weights, n, wave * R, (n + kBlock - 1) / kBlock, lane);
-#pragma unroll
-    for (int round = 0; round < kRounds; ++round)
-        for (int i = threadIdx.x; i < kHist; i += T) hist[round][i] = 0;
+    static_assert(kRounds * kHist % 4 == 0, "");
+    for (int i = threadIdx.x; i < kRounds * kHist / 4; i += T) reinterpret_cast<int4*>(hist[0])[i] = make_int4(0, 0, 0, 0);
     of.make(p, n, lane, key);
     __syncthreads();
     uint32_t prefix = 0;
@@ -166,15 +169,7 @@ __global__ __launch_bounds__(T) void select_kernel(EvictParams p) {
             if (key[i] != kNever && (round == 0 || key[i] >> shift_of(round - 1) == prefix)) atomicAdd(&hist[round][bin_at(digit_of(key[i], round))], 1);
         __syncthreads();
         if (wave == 0) {
-            if (round == 0) {                              // no more than there are
-                int all = 0;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) all += hist[0][33 * lane + i];
-                need = min(need, __builtin_amdgcn_readlane(wave_scan(all), 63));
-            }
-            Found x = {0, 0, 0};
-            if (need > 0) x = find_digit(hist[round], need, lane);
-            if (round == 0) x.total = need;
+            const Found x = find_digit(hist[round], need, lane);
             if (lane == 0) found[round] = x;
         }
         __syncthreads();
@@ -253,16 +248,7 @@ __device__ __forceinline__ void find_round(const EvictParams& p, int round, int 
     add_up<FRONT>(p, round, unit, live, hist, other);
     __syncthreads();
     if (threadIdx.x < 64) {
-        int want = last.y;
-        if (round == 0) {
-            int all = 0;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) all += hist[33 * lane + i];
-            want = min(want, __builtin_amdgcn_readlane(wave_scan(all), 63));
-        }
-        Found x = {0, 0, 0};
-        if (want > 0) x = find_digit(hist, want, lane);
-        if (round == 0) x.total = want;
+        const Found x = find_digit(hist, last.y, lane);
         if (lane == 0) *found = x;
     }
     __syncthreads();
@@ -609,7 +595,7 @@ extern "C" int vs_cache_evict(const vs_cache_t* cache, const float* weights, int
         VS_LAUNCH_CHECK();
         hipLaunchKernelGGL(emit_kernel, grid, dim3(kCountThreads), 0, s, p);
     } else if (max_n <= 2048) {
-        hipLaunchKernelGGL((select_kernel<256, 8>), dim3(y), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((select_kernel<512, 4>), dim3(y), dim3(512), 0, s, p);
     } else if (max_n <= 4096) {
         hipLaunchKernelGGL((select_kernel<512, 8>), dim3(y), dim3(512), 0, s, p);
     } else if (max_n <= 8192) {
