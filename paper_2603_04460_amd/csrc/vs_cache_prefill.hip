@@ -29,9 +29,11 @@ constexpr float kGrownSum = 32768.0f;                      // 2^(8 + 7): no weig
 constexpr float kSafe = 1024.0f;                           // scores (log2 units) up to which a product and a difference in one rounding are good enough
 constexpr int kPartFloats = kUnitRows * 128 + 1088;          // (4352 bytes more: parts a power of two apart would all begin in the same memory channels)
 constexpr int kShares = 256;                               // a workgroup for every compute unit
-// A unit's start and end take 7 us, a step 2.6.  Without them in the division the workgroups with many short units end last: six prompts of up to 9001 tokens,
-// 32 / 8 heads, 470 us with 0, 424 with 3.
-constexpr int kStart = 3;                                  // steps that a unit's start and end count for
+// What a unit's start and end (about 12 us) count for in the division, in steps (1.8 us); kEmpty: all of a unit whose rows have no position (zeros).  kStart of 3 / 5 / 6 /
+// 7 / 8 / 10, us: 32 / 8 heads, 1000 rows of six prompts of up to 9001 tokens - / 392 / 384 / 380 / 383 / 387, 512 of twelve of up to 3000 133 / 125 / 118 / 117 / 118 / 122,
+// 2000 of four of up to 2000 102 / 89 / 82 / 83 / 81 / 83, 512 of one of 32768 250.8 / 250.1 / 249.3 / 248.6 / 251.6 / 250.9.  kEmpty of 1 / 2 / 3 / 6 (with 6): the first
+// 447 / 385 / 390 / 396, 4000 rows of eight prompts of up to 4000 482 / 393 / 404 / 458.
+constexpr int kStart = 7, kEmpty = 2;
 constexpr int kAhead = 4;                                  // parts that are asked for at once
 // Small calls: shorter shares against more parts to join.  Us with 2 / 3 / 6 / 8: 8 / 2 heads, 300 rows of 1201 26.0 / 26.5 / 30.3 / 35.0, 32 / 8 heads, 130 of 1000
 // 29.6 / 28.5 / 31.9 / 35.7 (with 4 26.5 and 29.3).
@@ -55,7 +57,9 @@ struct PrefillParams {
 };
 
 // ---- the work of a call in a row: steps by sequence, head chunk, unit, block, which the workgroups divide evenly ----
-// A unit of sequence b has kStart steps in front (its start and end cost as much) and one for each block up to its last row's position.
+// A unit of sequence b has start() steps in front (its start and end cost as much) and one for each block up to its last row's position.
+__device__ __forceinline__ int start(int blocks) { return blocks > 0 ? kStart : kEmpty; }
+
 struct Sequence {
     int len, base, first;                  // base: position of row 0;  first: blocks up to row 0, may be negative
     __device__ __forceinline__ Sequence(const PrefillParams& p, int length) {
@@ -69,9 +73,12 @@ struct Sequence {
     // steps of the units in front of `tile` (tile < tiles: none of them is the last one)
     __device__ __forceinline__ int64_t before(const PrefillParams& p, int tile) const {
         const int64_t z = min(max(-first, 0) / p.tok_blocks, tile), t = tile;      // units that end in front of position 0
-        return kStart * t + (t - z) * first + p.tok_blocks * ((t * (t + 1) - z * (z + 1)) >> 1);
+        return kEmpty * z + kStart * (t - z) + (t - z) * first + p.tok_blocks * ((t * (t + 1) - z * (z + 1)) >> 1);
     }
-    __device__ __forceinline__ int64_t steps(const PrefillParams& p) const { return before(p, p.tiles - 1) + kStart + blocks(p, p.tiles - 1); }
+    __device__ __forceinline__ int64_t steps(const PrefillParams& p) const {
+        const int last = blocks(p, p.tiles - 1);
+        return before(p, p.tiles - 1) + start(last) + last;
+    }
 };
 
 // inclusive sum over the lanes up to this one
@@ -96,7 +103,7 @@ __device__ __forceinline__ int64_t lane64(int64_t x, int l) {
 }
 
 struct Place {
-    int b = 0, head = 0, tile = 0, step = 0, blocks = 0;       // head: of the sequence's head chunks;  step: of the unit, which has kStart + blocks
+    int b = 0, head = 0, tile = 0, step = 0, blocks = 0;       // head: of the sequence's head chunks;  step: of the unit, which has start(blocks) + blocks
     int len = 0, base = 0;
     __device__ __forceinline__ void next(const PrefillParams& p) {                 // the unit behind this one
         step = 0;
@@ -214,11 +221,13 @@ __device__ __forceinline__ int row_of_key(int key) { return (key & 0x27) | ((key
 
 // Rows in front of their sequence.
 __device__ __forceinline__ void no_keys(const PrefillParams& p, const Place& at, int tid) {
-    const int g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc);
-    for (int i = tid; i < kUnitRows * 16; i += kThreads) {
-        const int w = i >> 9, row = at.tile * p.tok + 32 * (w / p.hc) + ((i >> 4) & 31);
+    const int g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc), shift = 31 - __builtin_clz(p.hc);        // (hc is a power of two)
+    const int64_t head0 = at.b * p.q_heads + g * p.group + hchunk * p.hc;
+#pragma unroll
+    for (int k = 0; k < kUnitRows * 16 / kThreads; ++k) {
+        const int i = k * kThreads + tid, w = i >> 9, row = at.tile * p.tok + 32 * (w >> shift) + ((i >> 4) & 31);
         if (row >= p.n_q) continue;
-        const int64_t r = static_cast<int64_t>(at.b * p.q_heads + g * p.group + hchunk * p.hc + w % p.hc) * p.n_q + row;
+        const int64_t r = (head0 + (w & (p.hc - 1))) * p.n_q + row;
         reinterpret_cast<uint4*>(p.o + r * 128)[i & 15] = make_uint4(0, 0, 0, 0);
         if (p.lse && (i & 15) == 0) p.lse[r] = -INFINITY;
     }
@@ -247,8 +256,9 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
     const int64_t mine = some ? min(per, total - per * share) : 0;
     if (tid == 0) {
         // (the first of them has the unit's first block)
-        const bool ends = some && at.step > kStart && kStart + at.blocks - at.step <= mine;
-        *(joined(p) + share) = {ends ? share + 1 - static_cast<int>((per * share - at.step + kStart) / per) : 0, at.b, at.head, at.tile, at.base, {0, 0, 0}};
+        const int front = start(at.blocks);
+        const bool ends = some && at.step > front && front + at.blocks - at.step <= mine;
+        *(joined(p) + share) = {ends ? share + 1 - static_cast<int>((per * share - at.step + front) / per) : 0, at.b, at.head, at.tile, at.base, {0, 0, 0}};
     }
     if (tid < 2) lds.event[tid] = -1;
     if (tid == 0) lds.any_far = -1;
@@ -284,12 +294,12 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
     int64_t left = mine;
 
     for (; left > 0; at.next(p)) {
-        const int end = at.step + static_cast<int>(min(left, static_cast<int64_t>(kStart + at.blocks - at.step)));
+        const int front = start(at.blocks), end = at.step + static_cast<int>(min(left, static_cast<int64_t>(front + at.blocks - at.step)));
         left -= end - at.step;
         const int b = at.b, g = at.head / (p.group / p.hc), hchunk = at.head - g * (p.group / p.hc), len = at.len;
-        const int first_block = max(at.step - kStart, 0), nst = max(end - kStart, 0) - first_block;
+        const int first_block = max(at.step - front, 0), nst = max(end - front, 0) - first_block;
         if (nst == 0) {                                                    // the start alone, or (rows without a position) no more than that
-            if (at.blocks == 0 && end == kStart) no_keys(p, at, tid);
+            if (at.blocks == 0) no_keys(p, at, tid);
             continue;
         }
         // ---- the unit's rows ----
