@@ -235,7 +235,7 @@ __device__ __forceinline__ void no_keys(const PrefillParams& p, const Place& at,
 
 // What bounds it is power, behind it the vector instructions: a step of 64 keys x 256 rows is 64 matrix instructions of 32 cycles a wavefront, 2048 of about 3400
 // cycles, and the clock is at 1.9 GHz.  A loop of matrix instructions alone reaches 1.77 PFLOP/s on numbers like these, one with a softmax's exponentials and
-// operands from LDS 1.2, whatever its order.  2048 rows of 131072, 32 / 8 heads: 3650 us, 1.20 PFLOP/s; 512 of 32768 252 us.  Small calls are bound by their start
+// operands from LDS 1.2, whatever its order.  2048 rows of 131072, 32 / 8 heads: 3590 us, 1.21 PFLOP/s; 512 of 32768 250 us.  Small calls are bound by their start
 // (codes on their way, the search of a share's place) and the join: 300 rows of 1201, 8 / 2 heads, 23 us for 5 us of products.
 // Eight row blocks for a workgroup: the turning of a block is shared by 256 rows; 160 KB of LDS hold one workgroup, whose wavefronts have 512 registers each.
 //
