@@ -5,8 +5,8 @@
 // A block of 64 keys is turned into 16-bit numbers in LDS by all four wavefronts: K in bf16 with its scales (exact); V in fp16.  A wavefront has the
 // 32 channels of V that share scales and holds their unit 2^(R - 127), R at least the largest scale byte so far: an element is code 2^(E - R + 13), exact
 // for E from R - 27 to R.  What lies below, and groups that are not finite, stays out of the tile; a unit that has such blocks goes over them once more at its end
-// (bf16, weights in two terms; NaN to the rows that see it).  When R grows, everybody's sums are scaled.  Weights are held as 128 p (up to 2^15: the running maximum may be exceeded by 2^8) in fp16,
-// 11 significant bits, which is why V is fp16: weights of 8 bits would double the rounding error of the output.
+// (bf16, weights in two terms; NaN to the rows that see it).  When R grows, everybody's sums are scaled.  Weights are held as 128 p (up to 2^15: the running
+// maximum may be exceeded by 2^8) in fp16, 11 significant bits, which is why V is fp16: weights of 8 bits would double the rounding error of the output.
 // The rows of a K tile stand in LDS in the order (bits 3 and 4 of a key's number exchanged) in which a lane of S^T holds the weights that
 // the second product wants beside one word of V's codes, eight tokens of a channel: a word becomes one 16-byte operand.
 #include <float.h>

@@ -170,7 +170,7 @@ __device__ __forceinline__ void lds_load4(uint32_t at, const void* base, uint32_
 // tile are read behind the last products of this one's.
 // What bounds it is power: the clock falls under this load, and a loop of these instructions alone, with operands from LDS and numbers like these, takes 220 ns
 // for 32 x 32 scores and weights on a SIMD with one wavefront or two (1.2 PFLOP/s; without exponentials and LDS 1.77).  2048 tokens of 131072, 32 / 8 heads: 2100 us,
-// 256 ns;  1024 of 32749 284 us;  64 of 131072 72 us, where eight tiles have to pay for a block's conversion and sums.
+// 256 ns;  1024 of 32749 284 us;  64 of 131072 69 us, where eight tiles have to pay for a block's conversion and sums.
 template <bool RESIDENT>
 __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams p) {
     __shared__ __align__(16) uint8_t tile_of[kRing][kTileBytes];
@@ -433,8 +433,12 @@ void plan(WeighParams& p, int batch, int q_heads, int kv_heads, int64_t n_q, int
     if (parts < few) parts = few < most ? few : most;
     if (parts > 64) parts = 64;
     p.parts = static_cast<int>(parts);
-    const int64_t each = all <= kRing ? units * groups / 1024 : 1;
-    p.blocks = static_cast<int>(each < 1 ? 1 : each < 16 ? each : 16);
+    // Rows that stay in LDS are worth several groups for a workgroup: all that there are at once on the card (512) where that fills 85 % of them and the one sequence is as
+    // long as it may be, else small ones that even out.  Groups for 1024 / for 512, us: 64 tokens of 131072 (all of 512) 70.2 / 68.9, 32 of 32768 (all) 14.2 / 12.4, 64 of 70000 (86 %)
+    // 46.1 / 42.3, of 36000 (73 %) 25.4 / 26.9, of 20000 (62 %) 17.3 / 19.5, 33 of seven sequences of up to 10000 17.1 / 31.2.
+    const int64_t once = (units * groups + 511) / 512;
+    const int64_t each = all > kRing ? 1 : batch == 1 && units * groups * 100 >= 85 * 512 * once ? once : units * groups / 1024 < 16 ? units * groups / 1024 : 16;
+    p.blocks = static_cast<int>(each < 1 ? 1 : each);
 }
 
 size_t part_bytes(const WeighParams& p, int64_t units) { return p.parts > 1 ? static_cast<size_t>(p.parts * units * p.padded) * sizeof(float) : 0; }

@@ -53,6 +53,13 @@ def test_pages(page, n, rows):
     near(call(q, lse, cache, [n], n), weights(q, lse, cache, [n], n, None, 1.0, rows), [n])
 
 
+@pytest.mark.parametrize("hq, hk, rows, n", [(8, 2, 20, 131072), (8, 8, 17, 280000)])
+def test_many_groups_of_a_workgroup(hq, hk, rows, n):
+    """Long sequences whose few tiles of rows stay in LDS for several groups of keys."""
+    cache, q, lse = inputs(61, hq, hk, rows, [n], 256)
+    near(call(q, lse, cache, [n], n), weights(q, lse, cache, [n], n, None, 1.0, rows), [n])
+
+
 @pytest.mark.parametrize("rows", [1, 7, 40])
 def test_sum_of_a_row_is_one(rows):
     """What the rows of a head give away is as much as there are rows that see something."""
