@@ -814,24 +814,35 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
     }
 }
 
-// The parts of a unit that several workgroups shared.  Workgroup (x, s): the unit that share s ends, if others began it; half the channels of its row block
-// x / 2.  The first part stands in its share's second slot, the others in their shares' first.
+// The parts of a unit that several workgroups shared.  Workgroup (x, s): the unit that share s ends, if others began it; channels of one of its row blocks.  The
+// first part stands in its share's second slot, the others in their shares' first.  WAYS 4: each wavefront takes every fourth part, their sums meet in LDS; 1: a
+// wavefront takes all parts of its channels.  us with 1 / 4: 4 / 1 heads, 300 rows of 8000 (19 parts) 38.1 / 34.7, 200 of 2000 (8) 23.0 / 21.7, one head, 267 rows of 61864
+// (128) 60.5 / 42.8;  32 / 8 heads, six prompts of up to 9001 (two or three; four times the workgroups find nothing to do) 398.6 / 405.5.
+template <int WAYS>
 __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillParams p) {
     const int share = blockIdx.y;
     const Joined at = joined(p)[share];
     const int parts = at.parts, first = share + 1 - parts;
     if (parts <= 1) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
-    const int w = blockIdx.x >> 1, piece = 8 * (blockIdx.x & 1) + 2 * wave;                // and the next: channels 8 piece + 4 half ..
+    const int x0 = blockIdx.x * 4 / WAYS + (WAYS == 1 ? wave : 0), w = x0 >> 3, piece = 2 * (x0 & 7);       // and the next: channels 8 piece + 4 half ..
     const int row = at.tile * p.tok + 32 * (w / p.hc) + col;
     float m = -INFINITY, l = 0.0f;
     float4 y[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
-    for (int i = 0; i < parts; i += kAhead) {
+    // adds sums z (of weights that are large by x.x, their own sum x.y)
+    auto add = [&](float2 x, const float4 (&z)[2]) __attribute__((always_inline)) {
+        if (x.y == 0.0f) return;                                           // (a sum that is not a number has to stay one)
+        const float h = __builtin_amdgcn_exp2f(x.x - m);
+        l = fmaf(x.y, h, l);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) y[j] = make_float4(fmaf(z[j].x, h, y[j].x), fmaf(z[j].y, h, y[j].y), fmaf(z[j].z, h, y[j].z), fmaf(z[j].w, h, y[j].w));
+    };
+    for (int i = WAYS == 1 ? 0 : wave; i < parts; i += WAYS * kAhead) {
         float4 z[kAhead][2];
         float2 x[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const int part = min(i + k, parts - 1);
+            const int part = min(i + WAYS * k, parts - 1);
             const int64_t slot = part == 0 ? 2 * first + 1 : 2 * (first + part);
             x[k] = part_stat(p)[slot * kUnitRows + 32 * w + col];
             const float4* const from = reinterpret_cast<const float4*>(p.part + slot * kPartFloats) + 64 * (16 * w + piece) + lane;
@@ -841,7 +852,7 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillPar
         float most = m;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (i + k >= parts) x[k] = make_float2(-INFINITY, 0.0f);       // the last one again: no weight
+            if (i + WAYS * k >= parts) x[k] = make_float2(-INFINITY, 0.0f);   // the last one again: no weight
             most = fmaxf(most, x[k].x);
         }
         const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - most);
@@ -850,12 +861,24 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillPar
 #pragma unroll
         for (int j = 0; j < 2; ++j) y[j] = make_float4(y[j].x * f, y[j].y * f, y[j].z * f, y[j].w * f);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (x[k].y == 0.0f) continue;                                  // (a sum that is not a number has to stay one)
-            const float h = __builtin_amdgcn_exp2f(x[k].x - m);
-            l = fmaf(x[k].y, h, l);
+        for (int k = 0; k < kAhead; ++k) add(x[k], z[k]);
+    }
+    if constexpr (WAYS > 1) {
+        __shared__ float sums[WAYS][10][64];
+        const float mine[10] = {m, l, y[0].x, y[0].y, y[0].z, y[0].w, y[1].x, y[1].y, y[1].z, y[1].w};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) y[j] = make_float4(fmaf(z[k][j].x, h, y[j].x), fmaf(z[k][j].y, h, y[j].y), fmaf(z[k][j].z, h, y[j].z), fmaf(z[k][j].w, h, y[j].w));
+        for (int i = 0; i < 10; ++i) sums[wave][i][lane] = mine[i];
+        __syncthreads();
+        if (wave != 0) return;
+        l = 0.0f;
+        y[0] = y[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int k = 1; k < WAYS; ++k) m = fmaxf(m, sums[k][0][lane]);
+#pragma unroll
+        for (int k = 0; k < WAYS; ++k) {
+            auto of = [&](int i) { return sums[k][i][lane]; };
+            const float4 z[2] = {make_float4(of(2), of(3), of(4), of(5)), make_float4(of(6), of(7), of(8), of(9))};
+            add(make_float2(of(0), of(1)), z);
         }
     }
     if (row >= p.n_q) return;
@@ -946,7 +969,9 @@ extern "C" int vs_cache_prefill(const void* q, const vs_cache_t* cache, int batc
     hipLaunchKernelGGL(prefill_kernel, dim3(p.shares), dim3(kThreads), sizeof(Lds), s, p);
     VS_LAUNCH_CHECK();
     if (p.shares > 1) {
-        hipLaunchKernelGGL(prefill_join_kernel, dim3(kUnitRows / 32 * 2, p.shares), dim3(kThreads), 0, s, p);
+        const bool few = p.shares > 4 * static_cast<int64_t>(batch) * p.heads * p.tiles;       // units: more than four parts each
+        if (few) hipLaunchKernelGGL(prefill_join_kernel<4>, dim3(kUnitRows / 32 * 8, p.shares), dim3(kThreads), 0, s, p);
+        else hipLaunchKernelGGL(prefill_join_kernel<1>, dim3(kUnitRows / 32 * 2, p.shares), dim3(kThreads), 0, s, p);
         VS_LAUNCH_CHECK();
     }
     return VS_OK;

@@ -224,6 +224,17 @@ def test_many_sequences():
     near(call(q, cache, lens, 150), attention(q, cache, lens, 150))
 
 
+@pytest.mark.parametrize("hq, hk, rows, n", [(1, 1, 267, 9000), (4, 1, 130, 20000), (3, 3, 400, 5000)])
+def test_many_parts(hq, hk, rows, n):
+    """Few units of many keys: dozens of workgroups share each; a row that is not a number stays alone."""
+    k, v = kv(41, 1, hk, n)
+    cache = filled(41, k, v, 64)
+    cache.table[0, 3:40] = -1
+    q = queries(42, 1, hq, rows)
+    q[0, 0, 77] = float("nan")
+    near(call(q, cache, [n], n), attention(q, cache, [n], n))
+
+
 def test_stream():
     """On a stream of its own, beside another call with another workspace."""
     k, v = kv(35, 1, 2, 2000)
