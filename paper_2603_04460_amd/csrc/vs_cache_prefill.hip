@@ -4,8 +4,9 @@
 //   S^T = K Q^T (keys x rows, bf16),  O^T = V^T P^T (channels x rows, fp16), 32 x 32 x 16 matrix instructions
 // A block of 64 keys is turned into 16-bit numbers in LDS by all four wavefronts: K in bf16 with its scales (exact); V in fp16.  A wavefront has the
 // 32 channels of V that share scales and holds their unit 2^(R - 127), R at least the largest scale byte so far: an element is code 2^(E - R + 13), exact
-// for E from R - 27 to R.  What lies below, and groups that are not finite, stays out of the tile; a unit that has such blocks goes over them once more at its end
-// (bf16, weights in two terms; NaN to the rows that see it).  When R grows, everybody's sums are scaled.  Weights are held as 128 p (up to 2^15: the running
+// for E from R - 27 to R.  Where a value of a block lies below, or a group is not finite, all of the block stays out of the tile in these 32 channels: a bit for the block and
+// the channels says so, and the unit goes over such blocks once more at its end (bf16, weights in two terms; NaN to the rows that see it).  So which of the two has a value is
+// settled once, whatever R becomes behind it.  When R grows, everybody's sums are scaled.  Weights are held as 128 p (up to 2^15: the running
 // maximum may be exceeded by 2^8) in fp16, 11 significant bits, which is why V is fp16: weights of 8 bits would double the rounding error of the output.
 // The rows of a K tile stand in LDS in the order (bits 3 and 4 of a key's number exchanged) in which a lane of S^T holds the weights that
 // the second product wants beside one word of V's codes, eight tokens of a channel: a word becomes one 16-byte operand.
@@ -205,7 +206,7 @@ struct Lds {
     int unit_of[2][4];                     // R of the buffer's block
     int event[2];                          // last step (its number in the workgroup's life) that had a new R
     int any_far;                           // last step with values out of the products' range
-    uint32_t far[VS_MAX_SEQ / kBlock / 32];                // a bit for every stage that has some
+    uint32_t far[4][VS_MAX_SEQ / kBlock / 32];             // for a wavefront's channels: a bit for every stage that has some
 };
 
 // 16 or 4 bytes a lane from base + at straight to LDS, lane after lane from `to` on (the kernel itself waits for them)
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
     }
     if (tid < 2) lds.event[tid] = -1;
     if (tid == 0) lds.any_far = -1;
-    for (int w = tid; w < VS_MAX_SEQ / kBlock / 32; w += kThreads) lds.far[w] = 0;
+    for (int w = tid; w < 4 * (VS_MAX_SEQ / kBlock / 32); w += kThreads) (&lds.far[0][0])[w] = 0;
 
     // a thread's piece of a block: 32 channels of a key, and of V the words of eight tokens 4 c .. of two channels of the wavefront's 32
     const int key = tid >> 2, quarter = tid & 3, c = lane >> 4, m = lane & 15;
@@ -387,10 +388,10 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                     x = e_of - unit_mine + kSpan + 1;
                 }
                 fits = in && e_of < 255 && x > 0;
-                const uint64_t far = __ballot(in && e_of > 0 && !fits);
-                if (far) {
+                if (__ballot(in && e_of > 0 && !fits)) {                   // zeros for all of the stage: R may grow before the unit ends
+                    fits = false;
                     lds.any_far = steps_done;
-                    if (lane == 0) atomicOr(&lds.far[st >> 5], 1u << (st & 31));
+                    if (lane == 0) lds.far[wave][st >> 5] |= 1u << (st & 31);
                 }
             }
             lds.unit_of[st & 1][wave] = unit_mine;
@@ -686,9 +687,11 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
         // ---- what the products of V do not have (and nothing that was asked for beyond the last stage is on its way any more) ----
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (__builtin_expect(__builtin_amdgcn_readfirstlane(lds.any_far) == steps_done, 0)) {
-            for (int w = 0; 32 * w < nst; ++w)
-                for (uint32_t bits = __builtin_amdgcn_readfirstlane(lds.far[w]); bits; bits &= bits - 1) {
-                    const int st = 32 * w + __builtin_ctz(bits), live = live_of(st);
+            for (int w = 0; 32 * w < nst; ++w) {
+                const uint32_t bits_mine = __builtin_amdgcn_readfirstlane(lds.far[wave][w]);
+                for (uint32_t bits = __builtin_amdgcn_readfirstlane(lds.far[0][w] | lds.far[1][w] | lds.far[2][w] | lds.far[3][w]); bits; bits &= bits - 1) {
+                    const int bit = __builtin_ctz(bits), st = 32 * w + bit, live = live_of(st);
+                    const bool mine = bits_mine >> bit & 1;                // (else the tile had this wavefront's channels)
                     const uint8_t* const from = cache_block(p.cache, b, g, first_block + st);     // (a block without a page has no bit)
                     raw_k = *reinterpret_cast<const u32x4*>(from + k_code);
                     raw_s = *reinterpret_cast<const uint32_t*>(from + k_scale);
@@ -709,7 +712,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                             for (int j = 0; j < 2; ++j) {
                                 const int which = 4 * u + k, E = static_cast<int>((raw_e[which >> 1] >> (8 * (2 * (which & 1) + j))) & 255);
                                 const int up = E - unit_mine + kTop + 127;                        // exponent of the scale in fp32
-                                const bool far = 16 * (which >> 1) + 4 * c + 2 * (which & 1) + j < live && E < 255 && E < unit_mine - kSpan && up > 0;
+                                const bool far = 16 * (which >> 1) + 4 * c + 2 * (which & 1) + j < live && mine && E > 0 && E < 255 && up > 0;
                                 x[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw_v[i], __uint_as_float(static_cast<uint32_t>(far ? up : 127) << 23), decltype(k)::value));
                                 if (!far) x[j] = 0;
                             }
@@ -769,8 +772,9 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                     });
                     __syncthreads();
                 }
+            }
             __syncthreads();                                               // (every wavefront has seen the bits)
-            for (int w = tid; 32 * w < nst; w += kThreads) lds.far[w] = 0;
+            for (int w = lane; 32 * w < nst; w += 64) lds.far[wave][w] = 0;
         }
 
         // ---- results ----
