@@ -3,9 +3,10 @@
 // K of a block of 64 tokens comes straight from memory into the registers of the matrix operands, is turned into bf16 by the conversions (scales among
 // it, exact) and stays there while the rows pass by: S = K Q^T, keys x rows.  A lane keeps the sums of its keys over its rows, which meet across the lanes
 // once at the end: no key belongs to two wavefronts, no atomics, the same call gives the same bits.
-// The exponent is scale s - lse near zero for every weight that counts, of terms that are not: what the products' factor c = scale log2(e) loses by its
-// rounding is put into lse's factor (c / scale), and what is left of lse's product goes to the row as a factor, which costs nothing since the sum is a
-// multiply-add.
+// The exponent scale s - lse is near zero for every weight that counts, its terms are not: it is a multiply-add, in one rounding, times log2(e).  The kernel for many
+// rows saves the product: what its factor c = scale log2(e) loses by its rounding is put into lse's factor (c / scale), and what is left of lse's product goes to the row
+// as a factor of its weights, which costs nothing since the sum is a multiply-add.  Past kFar that factor would come to leave the range of fp32, and make NaN of weights that
+// are zero: tiles with such an lse have the product, as masked ones do, whose scores are gone over once more in any case.
 //   weigh_few_kernel   up to 16 rows of a KV head: 16 x 16 x 32 products, the rows in registers; bound by the memory (68 + 8 bytes a token)
 //   weigh_many_kernel  more: 32 x 32 x 16 products, four wavefronts of 64 keys share the rows, which come to LDS in tiles of 32
 //   weigh_add_kernel   few keys and many rows: workgroups share the rows, their sums meet here, in the order of the rows
@@ -39,13 +40,20 @@ struct WeighParams {
     int runs, run_rows, tiles;     // rows are taken in `runs` runs (all of them, or a head each) of run_rows rows, `tiles` tiles each
     int blocks;                    // of a wavefront
     int fresh;                     // last tokens that have no weight yet
+    float scale;
     float c, ratio, ratio_low;     // scale log2(e); c / scale in two terms
     float decay;
 };
 
 __device__ __forceinline__ bf16x8 operand(uint4 x) { return __builtin_bit_cast(bf16x8, x); }
 
-// A row's weights are 2^(c s - high) factor; a row without a key (lse = -inf) has none.
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kFar = 4194304.0f;                         // 2^22: up to here what is left of lse's product is below 1
+
+// A row without a key (lse = -inf) has no weights.
+__device__ __forceinline__ float lse_for(float lse) { return lse == -INFINITY ? INFINITY : lse; }
+
+// A row's weights are 2^(c s - high) factor, where its lse is not far.
 struct RowConst {
     float high, factor;
 };
@@ -53,8 +61,7 @@ struct RowConst {
 __device__ __forceinline__ RowConst row_const(const WeighParams& p, float lse) {
     RowConst x;
     x.high = lse * p.ratio;
-    x.factor = fabsf(x.high) < INFINITY ? __builtin_amdgcn_exp2f(-fmaf(lse, p.ratio_low, fmaf(lse, p.ratio, -x.high))) : 1.0f;
-    if (lse == -INFINITY) x.high = INFINITY;
+    x.factor = __builtin_amdgcn_exp2f(-fmaf(lse, p.ratio_low, fmaf(lse, p.ratio, -x.high)));
     return x;
 }
 
@@ -118,7 +125,7 @@ __global__ __launch_bounds__(64 * kWaves) void weigh_few_kernel(WeighParams p) {
     bf16x8 q[4];                                           // channels 32 c + 8 j ..
 #pragma unroll
     for (int j = 0; j < 4; ++j) q[j] = operand(*reinterpret_cast<const uint4*>(p.q + r * 128 + 32 * c + 8 * j));
-    RowConst row_of = row_const(p, p.lse[r]);
+    const float lse = lse_for(p.lse[r]);
     const int limit = col < p.rows ? len - p.n_q + row % p.n_q : -1;       // last key that the row sees
     for (;; block += kWaves) {
         Held next;
@@ -141,9 +148,9 @@ __global__ __launch_bounds__(64 * kWaves) void weigh_few_kernel(WeighParams p) {
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float y = fmaf(s[t][i], p.c, -row_of.high);
+                float y = fmaf(s[t][i], p.scale, -lse) * kLog2e;
                 if (16 * t + i > before) y = -INFINITY;
-                v[4 * t + i] = __builtin_amdgcn_exp2f(y) * row_of.factor;
+                v[4 * t + i] = __builtin_amdgcn_exp2f(y);
             }
         float mine = sum_to_lane(v, lane);
         if (!x.paged) mine = 0.0f;
@@ -263,9 +270,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
         const bool edge = first + kBlock - 1 > base;
 
         f32x16 s[2];                                       // scores of the group's first and second 32 keys
-        float high = 0.0f, used = 0.0f, factor = 0.0f, by = 0.0f;          // of the tile that is weighed: weights 2^(by s - used) factor
+        float used = 0.0f, factor = 0.0f, by = 0.0f;       // of the tile that is weighed: weights 2^(by s - used) factor
+        float lse = 0.0f;                                  // of the tile whose operands are there
         auto read = [&](int slot, int j) __attribute__((always_inline)) {
             y[j] = operand(*reinterpret_cast<const uint4*>(tile_of[slot] + (chunk_at ^ (16 * j))));
+            if (j == 0) lse = lse_of[slot][wave][lane];    // (there when `step` looks at it)
         };
         auto weigh = [&](int u, int j) __attribute__((always_inline)) {    // elements 2 j and 2 j + 1
 #pragma unroll
@@ -293,39 +302,44 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        // exponents as they are, where the row sees the key
-        auto mask = [&](int u, const Tile& t) __attribute__((always_inline)) {
+        // exponents as they are, where the row sees the key, for rows of any lse
+        auto mask = [&](int u, const Tile& t, float lse) __attribute__((always_inline)) {
             const int in_run = t.at + col, row = p.runs == 1 ? in_run % p.n_q : in_run;
             const int before = (in_run < p.run_rows ? base + row : -1) - first - 4 * half - 32 * u;
+            lse = lse_for(lse);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                s[u][e] = fmaf(s[u][e], p.c, -high);
+                s[u][e] = fmaf(s[u][e], p.scale, -lse) * kLog2e;
                 if (8 * (e >> 2) + (e & 3) > before) s[u][e] = -INFINITY;
             }
         };
         using Z = std::integral_constant<int, 0>;
         using O = std::integral_constant<int, 1>;
-        auto step = [&](auto old, const Tile& t, int slot, int next_slot) __attribute__((always_inline)) {
-            const float lse = lse_of[slot][wave][lane];
-            const bool masked = edge || t.at + 32 > p.run_rows;
+        auto step = [&](auto old, const Tile& t, int next_slot) __attribute__((always_inline)) {
+            const float lse_now = lse;
+            const bool masked = edge || t.at + 32 > p.run_rows || __ballot(fabsf(lse_now) > kFar) != 0;
             products(Z{}, old, 0);
-            const RowConst row = row_const(p, lse);
-            high = row.high;
+            const RowConst row = row_const(p, lse_now);
+            by = p.c;
+            used = row.high;
             factor = row.factor;
-            if (masked) mask(0, t);
-            by = masked ? 1.0f : p.c;
-            used = masked ? 0.0f : high;
+            if (__builtin_expect(masked, 0)) {
+                mask(0, t, lse_now);
+                by = 1.0f;
+                used = 0.0f;
+                factor = 1.0f;
+            }
             products(O{}, std::true_type{}, next_slot);
-            if (masked) mask(1, t);
+            if (masked) mask(1, t, lse_now);
         };
         if constexpr (RESIDENT) {
             Tile t = tile_number(i0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) read(0, j);
-            step(std::false_type{}, t, 0, i0 + 1 < i1 ? 1 : 0);
+            step(std::false_type{}, t, i0 + 1 < i1 ? 1 : 0);
             for (int i = 1; i < i1 - i0; ++i) {
                 forward(t, 0);
-                step(std::true_type{}, t, i, i0 + i + 1 < i1 ? i + 1 : 0);
+                step(std::true_type{}, t, i0 + i + 1 < i1 ? i + 1 : 0);
             }
         } else {
             // (the first tile has none in front: weights of 2^-inf)
@@ -356,10 +370,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams 
                     // tiles i, i + 1 and i + 2 are there, tile i - 1 has been read
                     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(3 * (kAhead - 3)) : "memory");
                     ask();
-                    step(std::true_type{}, now, i & (kRing - 1), (i + 1) & (kRing - 1));
+                    step(std::true_type{}, now, (i + 1) & (kRing - 1));
                     forward(now, 32 * skip);
                     if (i + 1 >= count) break;
-                    step(std::true_type{}, now, (i + 1) & (kRing - 1), (i + 2) & (kRing - 1));
+                    step(std::true_type{}, now, (i + 2) & (kRing - 1));
                     forward(now, 32 * skip);
                 }
             }
@@ -466,7 +480,8 @@ extern "C" int vs_cache_weigh(const void* q, const float* lse, const vs_cache_t*
     if (!q || !lse || !weights || !vs::aligned16(q) || !vs::aligned16(lse) || !vs::aligned4(old) || !vs::aligned4(weights) || !vs::aligned16(ws))
         return VS_ERR_INVALID_ARG;
     WeighParams p;
-    p.c = scale * 1.44269504088896340736f;
+    p.scale = scale;
+    p.c = scale * kLog2e;
     if (q_heads <= 0 || n_q <= 0 || fresh < 0 || !(scale > 0.0f) || !(p.c < INFINITY) || !(p.c >= FLT_MIN) || !(decay >= 0.0f && decay <= 1.0f)) return VS_ERR_INVALID_ARG;
     const int rc = vs::cache_params(cache, batch, lens, max_n, &p.cache);
     if (rc != VS_OK) return rc;
