@@ -54,17 +54,6 @@ __device__ __forceinline__ TwoTerms two_terms(float a, float b) {
 // position of the first key of a block without a page: no row sees it
 constexpr int kNowhere = 1 << 30;
 
-// inclusive sum over the lanes up to this one
-__device__ __forceinline__ int wave_scan(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);    // last of a row of 16 to the next row
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);    // last of the lower half to the upper
-    return x;
-}
-
 // The blocks of all sequences and KV heads in a row (sequence, head, block) are divided evenly among the workers, whatever the
 // lengths are; a worker may end one head and go on with the next.  A (worker, head) pair has the slot `worker + head's
 // number` for its part: from one pair of the row to the next at least one of the two grows.

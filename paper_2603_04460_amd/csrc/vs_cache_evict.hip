@@ -81,17 +81,6 @@ struct Keys {
     }
 };
 
-// inclusive sum over the lanes up to this one
-__device__ __forceinline__ int wave_scan(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);    // last of a row of 16 to the next row
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);    // last of the lower half to the upper
-    return x;
-}
-
 // Counts in LDS: bin d at d + d / 32.  Neighbouring bins, which weights of one size go to, are in different banks, and so are the bins that the lanes read at once,
 // 32 apart.
 constexpr int kHist = kBins + kBins / 32;

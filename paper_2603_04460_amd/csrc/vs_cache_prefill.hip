@@ -41,7 +41,6 @@ constexpr int kAhead = 4;                                  // parts that are ask
 constexpr int kSteps = 2;                                  // of a workgroup, if there are so few
 constexpr int kTop = 13;                                   // fp16 exponent of a code with E = R: 6 * 2^13 < 65504
 constexpr int kSpan = 27;                                  // E from R - 27 (2^-14 in fp16) to R
-constexpr uint32_t kLargeUnit = 200;                       // R, from 15 on, up to which any E outside shows in the upper half of the byte E - R + 15
 
 struct PrefillParams {
     CacheParams cache;
@@ -185,12 +184,6 @@ __device__ __forceinline__ float half_max(float x) {
 // wavefront maximum of whole numbers >= 0
 __device__ __forceinline__ int wave_max_int(int x) { return __builtin_amdgcn_readfirstlane(static_cast<int>(wave_max(static_cast<float>(x)))); }
 
-// f(integral_constant<int, FROM>), .., f(integral_constant<int, TO - 1>)
-template <int FROM, int TO, class F>
-__device__ __forceinline__ void unroll(F f) {
-    static_for<TO - FROM>([&](auto i) __attribute__((always_inline)) { f(std::integral_constant<int, FROM + decltype(i)::value>{}); });
-}
-
 // K in LDS: chunk (eight channels) after chunk, 64 rows of 16 bytes each; a chunk's pad spreads the four chunks that four lanes write over the banks.
 // V: word (eight tokens) after word, 128 channels of 16 bytes each.  Every read is 512 bytes in a row for a half of the wavefront.
 constexpr int kChunkBytes = 64 * 16 + 16, kKBytes = 16 * kChunkBytes, kWordBytes = 128 * 16, kVBytes = 8 * kWordBytes;
@@ -208,15 +201,6 @@ struct Lds {
     int any_far;                           // last step with values out of the products' range
     uint32_t far[4][VS_MAX_SEQ / kBlock / 32];             // for a wavefront's channels: a bit for every stage that has some
 };
-
-// 16 or 4 bytes a lane from base + at straight to LDS, lane after lane from `to` on (the kernel itself waits for them)
-__device__ __forceinline__ void lds_load16(uint32_t at, const void* base, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
-}
-
-__device__ __forceinline__ void lds_load4(uint32_t at, const void* base, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
-}
 
 __device__ __forceinline__ int row_of_key(int key) { return (key & 0x27) | ((key >> 1) & 8) | ((key << 1) & 16); }
 
@@ -586,7 +570,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                 }
                 VS_FENCE();
             }
-            unroll<0, 6>([&](auto index) __attribute__((always_inline)) {
+            static_for<16>([&](auto index) __attribute__((always_inline)) {
                 constexpr int j = decltype(index)::value;
                 if constexpr (HAS_Q) qmfma(j >> 1, j & 1);
                 VS_FENCE();
@@ -595,16 +579,7 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
                 if constexpr (HAS_S) exp_share(j);
                 VS_FENCE();
             });
-            unroll<6, 16>([&](auto index) __attribute__((always_inline)) {
-                constexpr int j = decltype(index)::value;
-                if constexpr (HAS_Q) qmfma(j >> 1, j & 1);
-                VS_FENCE();
-                if constexpr (MR == 0 && HAS_P) read_v(j);
-                turn(index);
-                if constexpr (HAS_S) exp_share(j);
-                VS_FENCE();
-            });
-            unroll<0, 16>([&](auto index) __attribute__((always_inline)) {
+            static_for<16>([&](auto index) __attribute__((always_inline)) {
                 constexpr int j = decltype(index)::value;
                 if constexpr (HAS_S && j == 15)
                     if (!search) look_again();
@@ -674,13 +649,13 @@ __global__ __launch_bounds__(kThreads, 1) void prefill_kernel(const PrefillParam
         bool search = true;
         slot(R0{}, T{}, T{}, T{}, true, 1, 0);                             // X(1): softmax of block 1 for stage 0
         for (int i = 1; i < nst; ++i) {
-                if (search) {
-                    const float least = fminf(m_run[0], m_run[1]), largest = fmaxf(m_run[0], m_run[1]);
-                    ready = __all(least * p.c >= -kSafe && largest * p.c <= kSafe);
-                }
-                search = !(ready && (there & 2) && (first_block + i) * kBlock + kBlock - 1 <= sure);
-                slot(R1{}, T{}, T{}, T{}, search, i, i);
-                slot(R0{}, T{}, T{}, T{}, search, i + 1, i);
+            if (search) {
+                const float least = fminf(m_run[0], m_run[1]), largest = fmaxf(m_run[0], m_run[1]);
+                ready = __all(least * p.c >= -kSafe && largest * p.c <= kSafe);
+            }
+            search = !(ready && (there & 2) && (first_block + i) * kBlock + kBlock - 1 <= sure);
+            slot(R1{}, T{}, T{}, T{}, search, i, i);
+            slot(R0{}, T{}, T{}, T{}, search, i + 1, i);
         }
         slot(R1{}, F{}, T{}, F{}, true, nst, nst);                          // Y(nst): P V of block 1
 

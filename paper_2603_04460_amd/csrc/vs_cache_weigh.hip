@@ -161,15 +161,6 @@ __global__ __launch_bounds__(64 * kWaves) void weigh_few_kernel(WeighParams p) {
     }
 }
 
-// 16 or 4 bytes a lane from base + at straight to LDS, lane after lane from `to` on (the kernel itself waits for them)
-__device__ __forceinline__ void lds_load16(uint32_t at, const void* base, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
-}
-
-__device__ __forceinline__ void lds_load4(uint32_t at, const void* base, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
-}
-
 // Workgroup (x, unit, part): wavefronts take blocks 4 i + wave of the workgroup's p.blocks groups of four; part: a stretch of the tiles of rows.
 // A tile of rows is in LDS as it is in memory, but for its 16-byte chunks: chunk c of row r stands at c ^ (r % 16), so that 16 lanes that read a
 // chunk of 16 rows use all banks.  Where all of a part's tiles fit in LDS they are read once; otherwise two at a time are asked for, kAhead tiles ahead.
