@@ -300,8 +300,9 @@ int vs_sparse_prefill_counters(const void* ws, size_t ws_bytes, void* stream, in
  * One convention holds for the calls below: `lens` [batch] int32 (device) is the number of tokens that each sequence
  * holds, the new ones among them, and a call's `rows` (or n_q) rows of a sequence are its LAST tokens: row r is position
  * lens[b] - rows + r.  One array serves a whole decoding step; a slot with lens 0 is idle; a batch of prompts of different
- * lengths is padded in front (rows of negative position have no token).  `lens` and page tables may begin at any element of an
- * array (4-byte alignment).
+ * lengths is padded in front (rows of negative position have no token).  So only a sequence that holds no more than `rows` tokens can have fewer new ones than the
+ * others: in one that holds more, all rows are tokens, and vs_cache_write writes them all, vs_cache_weigh adds the queries of them all.  Sequences that go on by
+ * different numbers of tokens take a call for each number.  `lens` and page tables may begin at any element of an array (4-byte alignment).
  */
 
 /* Rows of 128 bf16 elements: head h of token t at data + t * token_stride + h * head_stride (strides in elements, multiples of 8,
@@ -415,9 +416,11 @@ int vs_cache_attend(const void* q, const vs_cache_t* cache, int batch, int q_hea
  * The same attention for any number of new tokens (1 .. VS_MAX_SEQ), a chunk of a prompt for instance; sequences of a batch may differ in length, prompts
  * shorter than n_q are padded in front.  Layouts, masks, rows without a key (zeros, lse = -inf) and missing pages as for vs_cache_attend, whose kernels take
  * up to VS_CACHE_MAX_NEW rows, within its limits, where there is little work (by batch, q_heads, n_q and max_n, not by lens).
- * Arithmetic otherwise: K is exact in bf16; V in fp16 in units of the largest scale so far of its 32 channels, and what is below 2^-27 of that or not finite in
- * bf16, exact too; P in fp16 (11 significant bits); fp32 accumulation and softmax.  The same call always gives the same bits.
- * A key whose weight is below 2^-31 of the row's largest counts as zero in the output, V below 2^-126 of the largest of its 32 channels, too.  Scores have to lie
+ * Arithmetic otherwise: K is exact in bf16; V in fp16 in units of the largest scale so far of its 32 channels, and 64 tokens with one below 2^-27 of that or not finite
+ * among them in bf16, exact too; P in fp16, 11 significant bits down to 2^-21 of the row's largest weight and steps of 2^-31 of it below, where vs_cache_attend's kernels have 15
+ * bits of every weight (the output's own rounding is 2^-8; which of the two a call of up to VS_CACHE_MAX_NEW rows has goes by its sizes, as above); fp32 accumulation and
+ * softmax.  The same call always gives the same bits.
+ * So a key whose weight is below 2^-32 of the row's largest counts as zero in the output; V below 2^-126 of the largest of its 32 channels, too.  Scores have to lie
  * within fp32's range, and V within 2^96.  At most 4096 query heads.  Workspace: vs_cache_prefill_workspace; the answer for max_n is enough for every smaller
  * max_n of the same call.
  */
@@ -437,7 +440,8 @@ int vs_cache_prefill(const void* q, const vs_cache_t* cache, int batch, int q_he
  *   decay   0 .. 1; with 0 `old` is not read
  *   weights [batch, kv_heads, stride] fp32 out, stride >= max_n
  * A row without a key (lse = -inf; padding in front of a prompt, too) adds nothing.  A token of a missing page gets nothing and keeps decay * old.  scale * log2(e) has to be a normal fp32 number.
- * Arithmetic: K is exact in bf16; bf16 MFMA, fp32 exponentials and sums in a fixed order: the same call always gives the same bits.
+ * Arithmetic: K is exact in bf16; bf16 MFMA, fp32 exponentials and sums in a fixed order: the same call always gives the same bits.  lse may be of any size; it is
+ * taken as it is, and what its own rounding to fp32 left out (128 and more from 2^31 on) is missing in the exponents.
  * At most 4096 query heads and 2^30 - 1 rows of a KV head (q_heads / kv_heads * n_q).  Workspace: vs_cache_weigh_workspace; the answer for max_n is enough for every smaller max_n of the same call.
  */
 size_t vs_cache_weigh_workspace(int batch, int q_heads, int kv_heads, int64_t n_q, int64_t max_n);

@@ -16,7 +16,8 @@ constexpr int kThreads = 256;
 constexpr uint32_t kAlways = 0xffffffffu, kNever = 0;      // keys of tokens that stay in any case, and that are not there
 constexpr int kBins = 2048, kRounds = 3;
 // Tokens up to which one workgroup has a head.  Alone / shared, us with the tokens that stay read back: 8 heads, to 2048 tokens from 10000 22.6 / 40.5, 20000 32.5 / 41.4,
-// 32768 35.3 / 41.9 (64 keys a lane would be the next), four sequences of 32768 41.9 / 48.4, 16 of 32768 86 / 113.
+// 32768 35.3 / 41.9 (64 keys a lane would be the next), four sequences of 32768 41.9 / 48.4, 16 of 32768 86 / 113.  The more heads the more sharing costs, and past the line there
+// is no other form: eight heads to 4000 tokens, not read back, 64 sequences of 32768 386, of 40000 578 (130 of them bytes).
 constexpr int kAlone = 32768;
 constexpr int kAtOnce = 8;                                 // blocks of a wavefront that are asked for at once
 constexpr int kCountThreads = 1024, kCountBlocks = 128, kMaxChunks = 32;   // workgroups that share a head: blocks of each at least, and their number

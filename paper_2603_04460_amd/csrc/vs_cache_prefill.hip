@@ -7,7 +7,7 @@
 // for E from R - 27 to R.  Where a value of a block lies below, or a group is not finite, all of the block stays out of the tile in these 32 channels: a bit for the block and
 // the channels says so, and the unit goes over such blocks once more at its end (bf16, weights in two terms; NaN to the rows that see it).  So which of the two has a value is
 // settled once, whatever R becomes behind it.  When R grows, everybody's sums are scaled.  Weights are held as 128 p (up to 2^15: the running
-// maximum may be exceeded by 2^8) in fp16, 11 significant bits, which is why V is fp16: weights of 8 bits would double the rounding error of the output.
+// maximum may be exceeded by 2^8) in fp16, 11 significant bits down to 2^-21 of the maximum, which is why V is fp16: weights of 8 bits would double the rounding error of the output.
 // The rows of a K tile stand in LDS in the order (bits 3 and 4 of a key's number exchanged) in which a lane of S^T holds the weights that
 // the second product wants beside one word of V's codes, eight tokens of a channel: a word becomes one 16-byte operand.
 #include <float.h>
@@ -218,10 +218,10 @@ __device__ __forceinline__ void no_keys(const PrefillParams& p, const Place& at,
     }
 }
 
-// What bounds it is power, behind it the vector instructions: a step of 64 keys x 256 rows is 64 matrix instructions of 32 cycles a wavefront, 2048 of about 3400
-// cycles, and the clock is at 1.9 GHz.  A loop of matrix instructions alone reaches 1.77 PFLOP/s on numbers like these, one with a softmax's exponentials and
-// operands from LDS 1.2, whatever its order.  2048 rows of 131072, 32 / 8 heads: 3590 us, 1.21 PFLOP/s; 512 of 32768 250 us.  Small calls are bound by their start
-// (codes on their way, the search of a share's place) and the join: 300 rows of 1201, 8 / 2 heads, 23 us for 5 us of products.
+// A step of 64 keys x 256 rows is 64 matrix instructions of 32 cycles a wavefront, 2048 of about 3400 cycles, and the clock is at 1.9 GHz.  What stands beside them is as many
+// vector instructions, 15 % of them the turning of codes into 16 bits: vs_dense_kernel, which has no codes to turn, goes over the same numbers read back at 1.36 PFLOP/s
+// (2048 rows of 131072, 32 / 8 heads: 3220 us, and 136 for reading them back) where this one takes 3590 to 3790 us, 1.15 to 1.21;  512 rows 974 and 977;  512 of 32768 250.
+// Small calls are bound by their start (codes on their way, the search of a share's place) and the join: 300 rows of 1201, 8 / 2 heads, 23 us for 5 us of products.
 // Eight row blocks for a workgroup: the turning of a block is shared by 256 rows; 160 KB of LDS hold one workgroup, whose wavefronts have 512 registers each.
 //
 // Softmax, products and the turning into 16 bits in one instruction stream, written out in issue order (one wavefront a SIMD hides nothing): the two row

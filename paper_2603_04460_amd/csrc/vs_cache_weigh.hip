@@ -168,7 +168,7 @@ __global__ __launch_bounds__(64 * kWaves) void weigh_few_kernel(WeighParams p) {
 // tile are read behind the last products of this one's.
 // What bounds it is power: the clock falls under this load, and a loop of these instructions alone, with operands from LDS and numbers like these, takes 220 ns
 // for 32 x 32 scores and weights on a SIMD with one wavefront or two (1.2 PFLOP/s; without exponentials and LDS 1.77).  2048 tokens of 131072, 32 / 8 heads: 2100 us,
-// 256 ns;  1024 of 32749 284 us;  64 of 131072 69 us, where eight tiles have to pay for a block's conversion and sums.
+// 256 ns;  1024 of 32749 285 to 300 us;  64 of 131072 69 us, where eight tiles have to pay for a block's conversion and sums.
 template <bool RESIDENT>
 __global__ __launch_bounds__(64 * kWaves, 2) void weigh_many_kernel(WeighParams p) {
     __shared__ __align__(16) uint8_t tile_of[kRing][kTileBytes];
